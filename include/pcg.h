@@ -70,7 +70,8 @@ typedef enum {
   PCG_ERR_HIP = -8,                /* a HIP runtime call failed                             */
   PCG_ERR_MISALIGNED = -9,         /* workspace not 256-byte aligned, logits not element-aligned */
   PCG_ERR_CAPACITY = -10,          /* pcg_asg_build: a group or the member array did not fit      */
-  PCG_ERR_SCRATCH_TOO_SMALL = -11  /* pcg_verify_static: the step needs more than PCG_STATIC_SCRATCH_BYTES */
+  PCG_ERR_SCRATCH_TOO_SMALL = -11, /* pcg_verify_static: the step needs more than PCG_STATIC_SCRATCH_BYTES */
+  PCG_ERR_BAD_SCALE = -12          /* attention: scale is not a finite number > 0                 */
 } pcg_status;
 
 #define PCG_MAX_K 64               /* largest number of draft positions per step           */
@@ -475,6 +476,111 @@ int pcg_groups_prepare_weights_host(int32_t V, int32_t G, const int32_t *row_ptr
                                     const int32_t *members, const float *weights,
                                     int32_t chunk_groups, void *blob, size_t blob_bytes,
                                     pcg_prepared *info);
+
+/* ---- the target's forward pass between proposals and verification ------------------------- */
+
+/*
+ * The keys and values of one layer in pages: element i of the key of slot s of page p for shared head h is
+ * k[p * page_stride + s * slot_stride + h * head_stride + i], values likewise in v.  Slot numbers of a slot map are
+ * p * page_size + s.  The structure is HOST, k and v are DEVICE and aligned to 16 bytes; strides are in elements,
+ * positive and multiples of 16 bytes, so that [page, slot, head, dim] and [page, head, slot, dim] are both possible.
+ *   kv_heads   shared (grouped) heads; query head h reads shared head h / (heads / kv_heads)
+ *   head_dim   a multiple of 8 from 8 to 128
+ *   num_pages * page_size < 2^31
+ */
+typedef struct {
+  void *k, *v;
+  pcg_dtype dt;
+  int32_t num_pages, page_size, kv_heads, head_dim;
+  int64_t page_stride, slot_stride, head_stride;
+} pcg_kv_cache;
+
+/*
+ * The pages that B requests hold of a cache (of every layer of it: they all use the same table).  DEVICE:
+ *   block_table  int32, row b at b * table_stride: pages of request b in the order of its tokens, max_blocks at most;
+ *                what stands behind the pages that it holds means nothing
+ *   free_pages   int32 [num_pages], a stack: the pages that nobody holds are its first free_count entries
+ * The rest of the pool's state is an int32 array [3 B + 1]:
+ *   len[B]    tokens in the cache for good        held[B]   pages held
+ *   chunk[B]  tokens that the last pcg_pages_step added behind len, not yet kept or dropped
+ *   free_count
+ * A new pool: the pages 0 .. num_pages - 1 in free_pages, state all zero but free_count = num_pages.
+ * B <= 65536; max_blocks * page_size, num_pages * page_size and B * max_blocks < 2^31.
+ */
+typedef struct {
+  int32_t B, num_pages, page_size, max_blocks;
+  int32_t *block_table;
+  int64_t table_stride;
+  int32_t *free_pages;
+} pcg_pages;
+
+/*
+ * Between two forward passes: what is kept of the last chunk, pages back from those that need fewer, pages for the
+ * next chunk, and where every new token goes.  For every request:
+ *   kept = chunk, or with `commit` min(max(commit[b] + commit_extra, 0), chunk); after pcg_verify commit is its accept_len
+ *          and commit_extra 1 (the token that the chunk began with and the accepted ones)
+ *   len += kept; add (add[b], or add_all with add NULL) new tokens follow; add < 0: the request has ended, len = 0 and
+ *   all of its pages go back (an empty place, to which a later call with add > 0 brings a new request)
+ * and holds ceil((len + add) / page_size) pages afterwards.  Pages that are given back are pushed on the stack in the
+ * order of requests and blocks; then pages are taken from its top in the same order.
+ * A request is refused, and then gets no new token in this step (chunk = 0) and keeps the pages that it holds, if
+ * it needs more than max_blocks pages; if the running sum of new tokens of the requests that are not so refused, up to it
+ * and with it, is larger than max_tokens; or if it takes pages and the running sum of pages taken by
+ * those not refused so far, up to it and with it, is larger than the stack then holds (no later request gets pages either).
+ *   state_in, state_out   the state before and after; may be the same array, must not overlap otherwise
+ *   q_start     DEVICE int32 [B + 1]: request b's new tokens are rows q_start[b] .. q_start[b + 1] of the batch
+ *   slots       DEVICE int32 [max_tokens]: every row's slot, -1 behind the last request's
+ *   positions   DEVICE int32 [max_tokens] or NULL: every row's position in its request, 0 behind the last request's
+ *   refused     DEVICE int32 [1] or NULL: requests that asked for new tokens and were refused
+ * len in state_out is the position of each request's first new token, as pcg_cache_attend takes it.
+ */
+int pcg_pages_step(const pcg_pages *pages, const int32_t *state_in, int32_t *state_out, const int32_t *commit,
+                   int32_t commit_extra, const int32_t *add, int32_t add_all, int64_t max_tokens, int32_t *q_start,
+                   int32_t *slots, int32_t *positions, int32_t *refused, void *hip_stream);
+
+/*
+ * k_new, v_new (DEVICE, T rows of kv_heads * head_dim; row t, head h at t * tok_stride + h * head_stride, strides in elements
+ * and multiples of 16 bytes, 16-byte aligned) to the slots slots[t] of the cache.  Rows whose slot is negative or past the
+ * cache's last are left out.  A slot must not be named twice.  T == 0 is a no-op.
+ */
+int pcg_cache_write(const pcg_kv_cache *cache, const void *k_new, const void *v_new, int64_t T, int64_t k_tok_stride,
+                    int64_t k_head_stride, int64_t v_tok_stride, int64_t v_head_stride, const int32_t *slots,
+                    void *hip_stream);
+
+/*
+ * Attention of the new tokens of B requests over the cache, their own keys and values written before (pcg_cache_write).
+ * Row t of request b (row q_start[b] + t of the batch) is at position p = lens[b] + t and sees the keys j of its request with
+ * p - window < j <= p (window 0: all j <= p):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j
+ * with the softmax's maximum, sum and products in float32; with PCG_BF16 the weights are rounded to bf16 where they
+ * multiply values.  A row that sees no key, or none whose score is above -infinity, gives zeros.  What stands in keys and values that a
+ * row does not see has no effect on it, infinities and NaN included.
+ *   q, out        DEVICE [T, heads, head_dim] of the cache's dtype, strides in elements as in pcg_cache_write; out must not
+ *                 overlap q.  Rows behind q_start[B] are not read and not written.
+ *   block_table   DEVICE as in pcg_pages.  Keys in pages outside [0, num_pages) or past max_blocks read as zeros.
+ *   lens          DEVICE int32 [B]; q_start DEVICE int32 [B + 1], q_start[0] = 0, non-decreasing, q_start[B] <= T
+ *   heads         a multiple of kv_heads
+ *   longest       a bound on the new tokens of a request, which decides how the work is cut; a request may have more, and takes longer
+ *   workspace     DEVICE, >= pcg_cache_attend_workspace_bytes(B, T, heads, kv_heads, head_dim, longest)
+ */
+int pcg_cache_attend(const pcg_kv_cache *cache, const void *q, int64_t q_tok_stride, int64_t q_head_stride, int32_t heads,
+                     int64_t T, const int32_t *block_table, int64_t table_stride, int32_t max_blocks, const int32_t *lens,
+                     const int32_t *q_start, int32_t B, int64_t longest, float scale, int32_t window, void *out,
+                     int64_t out_tok_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes,
+                     void *hip_stream);
+
+size_t pcg_cache_attend_workspace_bytes(int32_t B, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                        int64_t longest);
+
+/*
+ * The same for whole prompts, packed one behind the other: rows q_start[b] .. q_start[b + 1] of q, k and v are request b's
+ * tokens, at positions 0, 1, ..  Types, strides, scale, window and empty rows as above; needs no workspace.
+ */
+int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt, int64_t T, int32_t heads, int32_t kv_heads,
+                      int32_t head_dim, int64_t q_tok_stride, int64_t q_head_stride, int64_t k_tok_stride,
+                      int64_t k_head_stride, int64_t v_tok_stride, int64_t v_head_stride, const int32_t *q_start, int32_t B,
+                      int64_t longest, float scale, int32_t window, void *out, int64_t out_tok_stride,
+                      int64_t out_head_stride, void *hip_stream);
 
 /* ---- per-kernel timing (for the benchmark) ------------------------------------------------ */
 

@@ -43,6 +43,19 @@ class _GroupsStruct(C.Structure):
                 ("weights", C.c_void_p), ("tok_weights", C.c_void_p)]
 
 
+class _PagesStruct(C.Structure):
+    """Mirror of pcg_pages."""
+    _fields_ = [("B", C.c_int32), ("num_pages", C.c_int32), ("page_size", C.c_int32), ("max_blocks", C.c_int32),
+                ("block_table", C.c_void_p), ("table_stride", C.c_int64), ("free_pages", C.c_void_p)]
+
+
+class _KvCacheStruct(C.Structure):
+    """Mirror of pcg_kv_cache."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dt", C.c_int), ("num_pages", C.c_int32), ("page_size", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
+
+
 class Diag(C.Structure):
     """Mirror of pcg_diag (eight uint32 counters)."""
     _fields_ = [(n, C.c_uint32) for n in
@@ -113,6 +126,24 @@ def lib() -> C.CDLL:
         L.pcg_asg_build_exact_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
         L.pcg_asg_build_exact.restype = C.c_int
         L.pcg_asg_build_exact.argtypes = L.pcg_asg_build.argtypes
+        L.pcg_pages_step.restype = C.c_int
+        L.pcg_pages_step.argtypes = [C.POINTER(_PagesStruct), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                     C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.pcg_cache_write.restype = C.c_int
+        L.pcg_cache_write.argtypes = [C.POINTER(_KvCacheStruct), C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64,
+                                      C.c_int64, C.c_int64, C.c_void_p, C.c_void_p]
+        L.pcg_cache_attend_workspace_bytes.restype = C.c_size_t
+        L.pcg_cache_attend_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int64]
+        L.pcg_cache_attend.restype = C.c_int
+        L.pcg_cache_attend.argtypes = [C.POINTER(_KvCacheStruct), C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_int64,
+                                       C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64,
+                                       C.c_float, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_size_t,
+                                       C.c_void_p]
+        L.pcg_prompt_attend.restype = C.c_int
+        L.pcg_prompt_attend.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32,
+                                        C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
+                                        C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_int32, C.c_void_p, C.c_int64,
+                                        C.c_int64, C.c_void_p]
         L.pcg_groups_validate_weights_host.restype = C.c_int
         L.pcg_groups_validate_weights_host.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                                                        C.c_void_p, C.c_double]
@@ -559,6 +590,201 @@ def propose(groups: Groups, draft_logits: torch.Tensor, *, temperature: float = 
           strides[1] if K > 1 else V, float(temperature), seed, offset, prop_tokens.data_ptr(),
           prop_groups.data_ptr(), None if diag is None else diag.data_ptr(), ws.data_ptr(), ws.numel())
     return prop_tokens, prop_groups
+
+
+# ------------------------------------------------- the forward pass between proposals and verification
+
+def _int32(t: torch.Tensor, shape, dev, what: str):
+    """Checks an int32 tensor of that shape on that device, contiguous."""
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {tuple(shape)} on {dev}")
+
+
+@dataclass
+class Pages:
+    """The pages of a K/V cache that B requests hold (pcg_pages and its state): ``block_table`` int32 [B, max_blocks] (rows
+    may be strided), ``free_pages`` int32 [num_pages], a stack whose first ``free_count`` entries nobody holds, and
+    ``state`` int32 [3 B + 1]: tokens in the cache for good, pages held and tokens of the last chunk of every request, then
+    ``free_count``."""
+    block_table: torch.Tensor
+    free_pages: torch.Tensor
+    state: torch.Tensor
+    page_size: int
+
+    def __post_init__(self):
+        t = self.block_table
+        if t.dim() != 2 or t.dtype != torch.int32 or t.shape[0] < 1 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
+        self.B, self.max_blocks = t.shape
+        self.num_pages = self.free_pages.numel()
+        _int32(self.free_pages, (self.num_pages,), t.device, "free_pages")
+        _int32(self.state, (3 * self.B + 1,), t.device, "state")
+        self._struct = _PagesStruct(self.B, self.num_pages, self.page_size, self.max_blocks, t.data_ptr(),
+                                    t.stride(0) if self.B > 1 else self.max_blocks, self.free_pages.data_ptr())
+
+    @classmethod
+    def empty(cls, B: int, num_pages: int, page_size: int, max_blocks: int, device) -> "Pages":
+        """A pool that nobody holds anything of yet; requests get ``max_blocks`` pages at most."""
+        state = torch.zeros(3 * B + 1, dtype=torch.int32, device=device)
+        state[3 * B] = num_pages
+        return cls(torch.zeros((B, max_blocks), dtype=torch.int32, device=device),
+                   torch.arange(num_pages, dtype=torch.int32, device=device), state, page_size)
+
+    @property
+    def lens(self) -> torch.Tensor:
+        """int32 [B]: tokens in the cache for good, the position of the chunk's first token (a view of ``state``)."""
+        return self.state[:self.B]
+
+    @property
+    def held(self) -> torch.Tensor:
+        return self.state[self.B:2 * self.B]
+
+    @property
+    def chunk(self) -> torch.Tensor:
+        return self.state[2 * self.B:3 * self.B]
+
+    @property
+    def free_count(self) -> torch.Tensor:
+        return self.state[3 * self.B:]
+
+
+@dataclass
+class PagesStep:
+    q_start: torch.Tensor      # int32 [B + 1]: rows of the batch of every request
+    slots: torch.Tensor        # int32 [max_tokens], -1 behind the last request's rows
+    positions: torch.Tensor    # int32 [max_tokens], 0 behind the last request's rows
+    refused: torch.Tensor      # int32 [1]
+
+
+def pages_step_outputs(B: int, max_tokens: int, device) -> PagesStep:
+    new = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
+    return PagesStep(new(B + 1), new(max_tokens), new(max_tokens), new(1))
+
+
+def pages_step(pages: Pages, add, *, max_tokens: int, commit: Optional[torch.Tensor] = None, commit_extra: int = 0,
+               state_out: Optional[torch.Tensor] = None, out: Optional[PagesStep] = None) -> PagesStep:
+    """Between two forward passes: keeps ``commit + commit_extra`` tokens of every request's last chunk (all without
+    ``commit``; after ``verify``: ``commit=out.accept_len, commit_extra=1``), adjusts the pages that it holds to ``add``
+    new tokens (an int for all, or int32 [B]; negative: the request has ended) and says where each of them goes.
+    The state is updated in place, or written to ``state_out``."""
+    dev, B = pages.state.device, pages.B
+    if out is None:
+        out = pages_step_outputs(B, max_tokens, dev)
+    if out.slots.numel() < max_tokens or out.positions.numel() < max_tokens or out.q_start.numel() != B + 1:
+        raise ValueError("the outputs have room for another number of rows or requests")
+    each = isinstance(add, torch.Tensor)
+    for t, what in ((commit, "commit"), (add if each else None, "add")):
+        if t is not None:
+            _int32(t, (B,), dev, what)
+    if state_out is None:
+        state_out = pages.state
+    else:
+        _int32(state_out, (3 * B + 1,), dev, "state_out")
+    _call(dev, "pcg_pages_step", lib().pcg_pages_step, C.byref(pages._struct), pages.state.data_ptr(), state_out.data_ptr(),
+          None if commit is None else commit.data_ptr(), commit_extra, add.data_ptr() if each else None,
+          0 if each else add, max_tokens, out.q_start.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(),
+          out.refused.data_ptr())
+    return out
+
+
+@dataclass
+class KvCache:
+    """Keys and values of one layer, [num_pages, page_size, kv_heads, head_dim] each, float32 or bfloat16, the last axis
+    contiguous and the same strides in both ([num_pages, kv_heads, page_size, head_dim] transposed is as good)."""
+    k: torch.Tensor
+    v: torch.Tensor
+
+    def __post_init__(self):
+        k, v = self.k, self.v
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v must be alike: [num_pages, page_size, kv_heads, head_dim]")
+        if k.stride(3) != 1:
+            raise ValueError("the last axis of the cache must be contiguous")
+        self.num_pages, self.page_size, self.kv_heads, self.head_dim = k.shape
+        self._struct = _KvCacheStruct(k.data_ptr(), v.data_ptr(), _dtype_code(k), *k.shape, *k.stride()[:3])
+
+
+def _rows(t: torch.Tensor, like: torch.Tensor, heads: int, head_dim: int, what: str):
+    """Checks rows [T, heads, head_dim] of the dtype and device of `like`; (token stride, head stride)."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{what} must be [T, {heads}, {head_dim}], {like.dtype}, on {like.device}")
+    st = t.stride()
+    if st[2] != 1:
+        raise ValueError(f"the last axis of {what} must be contiguous")
+    return st[0], st[1]
+
+
+def cache_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Keys and values [T, kv_heads, head_dim] of new tokens to their ``slots`` (int32 [T], as pages_step gives them;
+    negative: left out)."""
+    ks = _rows(k, cache.k, cache.kv_heads, cache.head_dim, "k")
+    vs = _rows(v, cache.k, cache.kv_heads, cache.head_dim, "v")
+    if k.shape[0] != v.shape[0]:
+        raise ValueError("k and v must have the same rows")
+    dev = cache.k.device
+    _int32(slots, (k.shape[0],), dev, "slots")
+    _call(dev, "pcg_cache_write", lib().pcg_cache_write, C.byref(cache._struct), k.data_ptr(), v.data_ptr(), k.shape[0], *ks, *vs,
+          slots.data_ptr())
+
+
+def cache_attend_workspace_bytes(B: int, rows: int, heads: int, kv_heads: int, head_dim: int, longest: int) -> int:
+    return lib().pcg_cache_attend_workspace_bytes(B, rows, heads, kv_heads, head_dim, longest)
+
+
+def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor, *,
+                 longest: Optional[int] = None, scale: Optional[float] = None, window: int = 0,
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of new tokens over the cache that holds their own keys and values already: ``q`` [T, heads, head_dim], the
+    rows q_start[b] .. q_start[b + 1] of request b at positions lens[b], lens[b] + 1, .. (pages_step: ``pages.lens``), each
+    seeing the keys up to itself, with ``window`` the last that many of them.  ``longest`` bounds the new tokens of a request
+    (it decides how the work is cut; without it: the mean).  ``scale`` is 1 / sqrt(head_dim) unless given.  Rows of ``out`` behind
+    the last request's stay as they were (zeros where ``out`` is not given)."""
+    T, heads = q.shape[0], q.shape[1]
+    qs = _rows(q, cache.k, heads, cache.head_dim, "q")
+    dev, B = q.device, lens.numel()
+    if out is None:
+        out = torch.zeros((T, heads, cache.head_dim), dtype=q.dtype, device=dev)
+    os_ = _rows(out, cache.k, heads, cache.head_dim, "out")
+    if out.shape[0] != T:
+        raise ValueError("out must have q's rows")
+    if block_table.dim() != 2 or block_table.dtype != torch.int32 or block_table.shape[0] != B or block_table.device != dev or \
+            (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
+    _int32(lens, (B,), dev, "lens")
+    _int32(q_start, (B + 1,), dev, "q_start")
+    if longest is None:
+        longest = -(-T // max(B, 1))
+    if workspace is None:
+        workspace = _workspace(dev, cache_attend_workspace_bytes(B, T, heads, cache.kv_heads, cache.head_dim, longest))
+    _call(dev, "pcg_cache_attend", lib().pcg_cache_attend, C.byref(cache._struct), q.data_ptr(), *qs, heads, T,
+          block_table.data_ptr(), block_table.stride(0), block_table.shape[1], lens.data_ptr(), q_start.data_ptr(), B, longest,
+          cache.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), *os_, workspace.data_ptr(),
+          workspace.numel())
+    return out
+
+
+def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor, *, longest: Optional[int] = None,
+                  scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention of packed prompts: rows q_start[b] .. q_start[b + 1] of ``q`` [T, heads, head_dim], ``k`` and ``v``
+    [T, kv_heads, head_dim] are request b's tokens.  Arguments as for ``cache_attend``."""
+    T, heads, head_dim = q.shape
+    kv_heads = k.shape[1]
+    qs, ks, vs = (_rows(t, q, h, head_dim, w) for t, h, w in ((q, heads, "q"), (k, kv_heads, "k"), (v, kv_heads, "v")))
+    if k.shape[0] != T or v.shape[0] != T:
+        raise ValueError("k and v must have q's rows")
+    dev, B = q.device, q_start.numel() - 1
+    if out is None:
+        out = torch.zeros((T, heads, head_dim), dtype=q.dtype, device=dev)
+    os_ = _rows(out, q, heads, head_dim, "out")
+    if out.shape[0] != T:
+        raise ValueError("out must have q's rows")
+    _int32(q_start, (B + 1,), dev, "q_start")
+    if longest is None:
+        longest = -(-T // max(B, 1))
+    _call(dev, "pcg_prompt_attend", lib().pcg_prompt_attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q), T, heads,
+          kv_heads, head_dim, *qs, *ks, *vs, q_start.data_ptr(), B, longest, head_dim ** -0.5 if scale is None else scale,
+          window, out.data_ptr(), *os_)
+    return out
 
 
 ERR_CAPACITY = -10

@@ -829,6 +829,7 @@ const char *pcg_strerror(int status) {
     case PCG_ERR_CAPACITY: return "a similarity group or the member array needs more room";
     case PCG_ERR_SCRATCH_TOO_SMALL:
       return "the step needs more scratch memory than the library's own array holds (use pcg_verify)";
+    case PCG_ERR_BAD_SCALE: return "scale must be finite and > 0";
     default: return "unknown status";
   }
 }
