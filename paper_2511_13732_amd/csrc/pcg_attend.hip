@@ -8,6 +8,10 @@
 // so a row's maximum and sum stay in one lane pair, scaling a row is one multiplication per register, and
 // the weights never pass through LDS.  One pass with the running maximum and sum of the softmax, in float32;
 // products accumulate in float32.
+//
+// Two kernels.  attend_thick_kernel: 128 rows a workgroup, 32 a wave, the four waves share tiles of keys and values in
+// LDS (prompts, long chunks: bound by the matrix and vector units).  attend_thin_kernel: 32 or 64 rows a workgroup, each wave
+// streams keys of its own (a step's chunks, single tokens: bound by memory).  Keys and values go from memory straight into LDS.
 #include <math.h>
 
 #include "pcg_attend.h"
@@ -20,13 +24,19 @@ namespace {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef short shortx8 __attribute__((ext_vector_type(8)));
 
 constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = kAttendWaves * kWave;
+constexpr int kThickRows = 32 * kAttendWaves;
+constexpr int kThinKeys = 32 * kAttendWaves;      // keys a turn of the four waves takes
+constexpr int kJoinThreads = 1024;
 constexpr float kLag = 8.f;        // how far (in powers of two) a maximum may run ahead of the one in use
 
 // What is read where there is nothing to read: keys behind the last, columns behind D.
@@ -39,363 +49,463 @@ __device__ __forceinline__ void split_by(uint32_t n, uint32_t d, uint32_t magic,
   if (r >= d) { ++q; r -= d; }
 }
 
-__device__ __forceinline__ float other_half(float x) {           // the value of lane ^ 32
-  return __shfl_xor(x, 32);
+// Element i of an array that nothing writes while the kernel runs: by the scalar unit where i is the same in all lanes.
+__device__ __forceinline__ int32_t fixed_at(const int32_t *p, int64_t i) {
+  return ((const __attribute__((address_space(4))) int32_t *) p)[i];
 }
 
-// One unit of work: 32 * WR rows of one shared head of one request.
-struct Unit {
-  int32_t first;       // token of the request's first row in the batch
-  int32_t ctx;         // position of that token
-  int32_t rows;        // rows of the request
-  int32_t r0;          // first row of the unit
-  int32_t b, head;
-};
+// max and sum of a lane and lane ^ 32
+__device__ __forceinline__ float pair_max(float x) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
 
-template <typename T, int DP, int WR>
+// Waits until at most N of this wave's vector-memory operations are still in flight, and keeps reads of what they bring behind.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(N < 64, "the counter has six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+// This wave's reads of LDS are through: what they read may be overwritten.
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// Meets the other waves without waiting for loads in flight.
+__device__ __forceinline__ void bare_barrier() {
+  wait_lds();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <typename T, int DP>
 struct Shape {
   static constexpr bool kBf16 = sizeof(T) == 2;
-  static constexpr int WK = kAttendWaves / WR;
-  static constexpr int KB = WK == 1 && kBf16 ? 2 : 1;           // blocks of 32 keys a wave and tile
-  static constexpr int TK = 32 * KB * WK;                       // keys a tile
+  static constexpr int E = 16 / (int) sizeof(T);                // elements of 16 bytes
   static constexpr int RB = DP * (int) sizeof(T);               // bytes of a key
   static constexpr int CH = RB / 16;
-  static constexpr int NL = TK * CH / kAttendThreads;           // loads of a thread for keys, and for values
+  static constexpr int RPI = kWave / CH;                        // keys that one load of a wave brings
   static constexpr int NQ = RB / 32;                            // 16-byte parts of a row that a lane holds
   static constexpr int NO = DP / 32;
-  static constexpr int kTileBytes = TK * RB;
-  static constexpr int kPartBytes = WK > 1 ? WR * (DP + 2) * 32 * 4 : 0;       // a wave's rows on their way to another
-  static constexpr int kLdsBytes = 2 * kTileBytes > kPartBytes ? 2 * kTileBytes : kPartBytes;
 };
 
-// Where 16-byte chunk `ch` of row `row` lies in a tile of keys or values.  A wave reads the same chunk of
-// 16 consecutive keys at a time: they have to differ modulo 256 bytes.
+// Which 16-byte chunk of key `row` lies at chunk position `pos` of its row in LDS (and the other way round).  A wave reads the
+// same chunk of 16 consecutive keys at a time: they have to differ modulo 256 bytes.
 template <int RB>
-__device__ __forceinline__ int key_at(int row, int ch) {
-  if constexpr (RB >= 256) return row * RB + ((ch ^ (row & 15)) << 4);
-  else return row * RB + ((ch ^ ((row >> 1) & 7)) << 4);
+__device__ __forceinline__ int key_swap(int row, int pos) {
+  if constexpr (RB >= 256) return pos ^ (row & 15);
+  else return pos ^ ((row >> 1) & 7);
 }
 // Values: bf16 reads 64 bytes of four consecutive keys at a time, float32 128 bytes of two keys that are four apart.
 template <int RB, bool BF16>
-__device__ __forceinline__ int value_at(int row, int ch) {
-  if constexpr (!BF16) return row * RB + ((ch ^ (((row >> 2) & 1) << 3)) << 4);
-  else if constexpr (RB >= 256) return row * RB + ((ch ^ ((row & 3) << 2)) << 4);
-  else return row * RB + ((ch ^ (((row >> 1) & 1) << 2)) << 4);
+__device__ __forceinline__ int value_swap(int row, int pos) {
+  if constexpr (!BF16) return pos ^ (((row >> 2) & 1) << 3);
+  else if constexpr (RB >= 256) return pos ^ ((row & 3) << 2);
+  else return pos ^ (((row >> 1) & 1) << 2);
 }
+template <int RB>
+__device__ __forceinline__ int key_at(int row, int ch) { return row * RB + (key_swap<RB>(row, ch) << 4); }
+template <int RB, bool BF16>
+__device__ __forceinline__ int value_at(int row, int ch) { return row * RB + (value_swap<RB, BF16>(row, ch) << 4); }
 
 template <bool BF16>
-__device__ __forceinline__ bool not_finite(uint32_t x) {
-  if constexpr (BF16) return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-  else return (x & 0x7f800000u) == 0x7f800000u;
-}
-
-template <typename T>
-__device__ __forceinline__ float lds_value(const unsigned char *p) {
-  if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t) *reinterpret_cast<const uint16_t *>(p) << 16);
-  else return *reinterpret_cast<const float *>(p);
-}
-
-// Rows of a unit over keys [k_lo, k_hi): O (not yet divided), the row's reference maximum (log2 units) and sum.
-template <typename T, int DP, int WR, bool PAGED>
-__device__ __forceinline__ void attend_keys(const AttendArgs &a, const Unit &u, int32_t k_lo, int32_t k_hi,
-                                            unsigned char *lds, int *flag, const u32x4 (&qf)[Shape<T, DP, WR>::NQ],
-                                            int32_t pos, int32_t min_hi, int32_t max_lo,
-                                            floatx16 (&o)[Shape<T, DP, WR>::NO], float &ref, float &sum) {
-  using S = Shape<T, DP, WR>;
-  constexpr bool kBf16 = S::kBf16;
-  constexpr int E = 16 / (int) sizeof(T);
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, half = lane >> 5, wk = wave / WR;
-  unsigned char *lk = lds, *lv = lds + S::kTileBytes;
-  const int ch = tid % S::CH, row0 = tid / S::CH;
-  const bool in_d = ch * E < a.D;
-  const char *kb = reinterpret_cast<const char *>(a.k) + ((int64_t) u.head * a.k_head + ch * E) * (int) sizeof(T);
-  const char *vb = reinterpret_cast<const char *>(a.v) + ((int64_t) u.head * a.v_head + ch * E) * (int) sizeof(T);
-  const int32_t *table = PAGED ? a.table + (int64_t) u.b * a.table_stride : nullptr;
-
-  u32x4 rk[S::NL], rv[S::NL];
-  auto fetch = [&](int32_t k0) {
+__device__ __forceinline__ bool not_finite(u32x4 x) {
+  bool odd = false;
 #pragma unroll
-    for (int i = 0; i < S::NL; ++i) {
-      const int32_t key = k0 + row0 + i * (kAttendThreads / S::CH);
-      bool there = key < k_hi && in_d;
-      int64_t ok, ov;
-      if constexpr (PAGED) {
-        uint32_t block, slot;
-        split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
-        there = there && block < (uint32_t) a.max_blocks;
-        const int32_t page = there ? table[block] : 0;
-        there = there && (uint32_t) page < (uint32_t) a.num_pages;
-        ok = (int64_t) page * a.k_page + (int64_t) slot * a.k_tok;
-        ov = (int64_t) page * a.v_page + (int64_t) slot * a.v_tok;
-      } else {
-        ok = (int64_t) (u.first + key) * a.k_tok;
-        ov = (int64_t) (u.first + key) * a.v_tok;
-      }
-      const char *none = reinterpret_cast<const char *>(&kZeros);
-      rk[i] = *reinterpret_cast<const u32x4 *>(there ? kb + ok * (int) sizeof(T) : none);
-      rv[i] = *reinterpret_cast<const u32x4 *>(there ? vb + ov * (int) sizeof(T) : none);
-    }
-  };
-
-  fetch(k_lo);
-  for (int32_t k0 = k_lo; k0 < k_hi; k0 += S::TK) {
-    // some row does not see all of the tile's keys
-    const bool edge = k0 + S::TK > min_hi || k0 < max_lo;
-    __syncthreads();
-    if (edge) {
-      bool odd = false;
-#pragma unroll
-      for (int i = 0; i < S::NL; ++i)
-        odd = odd || not_finite<kBf16>(rv[i].x) || not_finite<kBf16>(rv[i].y) || not_finite<kBf16>(rv[i].z) ||
-              not_finite<kBf16>(rv[i].w);
-      if (tid == 0) *flag = 0;
-      __syncthreads();
-      if (odd) *flag = 1;
-    }
-#pragma unroll
-    for (int i = 0; i < S::NL; ++i) {
-      const int row = row0 + i * (kAttendThreads / S::CH);
-      *reinterpret_cast<u32x4 *>(lk + key_at<S::RB>(row, ch)) = rk[i];
-      *reinterpret_cast<u32x4 *>(lv + value_at<S::RB, kBf16>(row, ch)) = rv[i];
-    }
-    __syncthreads();
-    if (k0 + S::TK < k_hi) fetch(k0 + S::TK);
-
-    const int base = wk * 32 * S::KB;        // this wave's keys in the tile
-    floatx16 s[S::KB];
-#pragma unroll
-    for (int kb2 = 0; kb2 < S::KB; ++kb2) {
-      s[kb2] = floatx16{};
-#pragma unroll
-      for (int i = 0; i < S::NQ; ++i) {
-        const u32x4 kf = *reinterpret_cast<const u32x4 *>(lk + key_at<S::RB>(base + kb2 * 32 + l32, 2 * i + half));
-        if constexpr (kBf16) {
-          s[kb2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]),
-                                                           s[kb2], 0, 0, 0);
-        } else {
-          s[kb2] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.x), __uint_as_float(qf[i].x), s[kb2], 0, 0, 0);
-          s[kb2] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.y), __uint_as_float(qf[i].y), s[kb2], 0, 0, 0);
-          s[kb2] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.z), __uint_as_float(qf[i].z), s[kb2], 0, 0, 0);
-          s[kb2] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.w), __uint_as_float(qf[i].w), s[kb2], 0, 0, 0);
-        }
-      }
-    }
-    // register 4 j + i of block kb2 is key base + 32 kb2 + 8 j + 4 half + i
-    if (edge) {
-      const int32_t lo = a.window > 0 ? pos - a.window : -1;     // sees keys in (lo, pos]
-#pragma unroll
-      for (int kb2 = 0; kb2 < S::KB; ++kb2)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int32_t key = k0 + base + kb2 * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-          if (key > pos || key <= lo) s[kb2][r] = -INFINITY;
-        }
-    }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int kb2 = 0; kb2 < S::KB; ++kb2)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb2][r]);
-    mx = fmaxf(mx, other_half(mx)) * a.c;
-    if (__builtin_amdgcn_ballot_w64(mx > ref + kLag) != 0) {
-      const float now = fmaxf(ref, mx);
-      const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
-      ref = now;
-      sum *= f;
-#pragma unroll
-      for (int n = 0; n < S::NO; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[n][r] *= f;
-    }
-    const float minus = ref == -INFINITY ? 0.f : -ref;
-#pragma unroll
-    for (int kb2 = 0; kb2 < S::KB; ++kb2)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[kb2][r] = __builtin_amdgcn_exp2f(fmaf(s[kb2][r], a.c, minus));
-        sum += s[kb2][r];
-      }
-    if (edge && *flag) {
-      // A value that is not finite stands in the tile, and not all rows see all keys: one key at a time, and only where its
-      // weight is not zero (zero times such a value would be NaN).
-#pragma unroll
-      for (int kb2 = 0; kb2 < S::KB; ++kb2) {
-#pragma nounroll
-        for (int n = 0; n < 16; ++n) {
-          const float mine = s[kb2][0], theirs = other_half(mine);
-#pragma unroll
-          for (int r = 0; r < 15; ++r) s[kb2][r] = s[kb2][r + 1];
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            const float w = hh == half ? mine : theirs;
-            const int row = base + kb2 * 32 + (n >> 2) * 8 + hh * 4 + (n & 3);
-#pragma unroll
-            for (int m = 0; m < S::NO; ++m)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const int d = m * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-                const float x = lds_value<T>(lv + value_at<S::RB, kBf16>(row, d / E) + d % E * (int) sizeof(T));
-                o[m][r] = w != 0.f ? fmaf(w, x, o[m][r]) : o[m][r];
-              }
-          }
-        }
-      }
-    } else if constexpr (kBf16) {
-      // The weights are rounded to bf16 here (half a step, at most 2^-8 of each): the products take bf16 operands, and the
-      // values that they multiply carry the same step.  Their sum above is of the unrounded ones.
-#pragma unroll
-      for (int kb2 = 0; kb2 < S::KB; ++kb2)
-#pragma unroll
-        for (int c16 = 0; c16 < 2; ++c16) {
-          uint32_t pw[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const floatx2 two = {s[kb2][c16 * 8 + 2 * e], s[kb2][c16 * 8 + 2 * e + 1]};
-            pw[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
-          }
-          const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pw[0], pw[1], pw[2], pw[3]});
-          // lane 16 p + x of a half reads 4 elements of key x / 4, columns 16 p + 4 (x % 4), and gets back column
-          // 16 p + x of the four keys
-          const int row = base + kb2 * 32 + c16 * 16 + half * 4 + ((lane & 15) >> 2);
-#pragma unroll
-          for (int m = 0; m < S::NO; ++m) {
-            const int d = m * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-            typedef __attribute__((address_space(3))) shortx4 lds4;
-            const shortx4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds4 *) (lv + value_at<S::RB, true>(row, d >> 3) + (d & 4) * 2));
-            const shortx4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds4 *) (lv + value_at<S::RB, true>(row + 8, d >> 3) + (d & 4) * 2));
-            typedef short shortx8 __attribute__((ext_vector_type(8)));
-            const shortx8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-            o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf, o[m], 0, 0, 0);
-          }
-        }
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = base + (r >> 2) * 8 + half * 4 + (r & 3);
-#pragma unroll
-        for (int m = 0; m < S::NO; ++m) {
-          const int d = m * 32 + l32;
-          const float x = *reinterpret_cast<const float *>(lv + value_at<S::RB, false>(row, d >> 2) + (d & 3) * 4);
-          o[m] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[0][r], o[m], 0, 0, 0);
-        }
-      }
-    }
+  for (int i = 0; i < 4; ++i) {
+    odd = odd || (x[i] & 0x7f800000u) == 0x7f800000u;
+    if constexpr (BF16) odd = odd || (x[i] & 0x7f80u) == 0x7f80u;
   }
+  return odd;
 }
 
-// Finds the unit that workgroup `index` works on: the requests' row blocks, one after the other.  False: none.
+// A block of rows of one shared head of one request.
+struct Unit {
+  int32_t b, head;
+  int32_t first;       // token of the request's first row in the batch
+  int32_t rows;        // rows of the request
+  int32_t ctx;         // position of its first row's token
+  int32_t r0;          // first row of the block
+  int32_t k_lo, k_hi;  // keys that some row sees, from a multiple of 32
+  int32_t min_hi;      // all rows see keys [max_lo, min_hi)
+  int32_t max_lo;
+};
+
+// The same in all lanes: in scalar registers from here on.
+__device__ __forceinline__ int32_t scalar(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t scalar(int64_t x) {
+  return (int64_t) ((uint64_t) (uint32_t) scalar((int32_t) (x >> 32)) << 32 | (uint32_t) scalar((int32_t) x));
+}
+__device__ __forceinline__ Unit scalar(const Unit &u) {
+  return Unit{scalar(u.b), scalar(u.head), scalar(u.first), scalar(u.rows), scalar(u.ctx),
+              scalar(u.r0), scalar(u.k_lo), scalar(u.k_hi), scalar(u.min_hi), scalar(u.max_lo)};
+}
+
 template <int R>
-__device__ __forceinline__ bool find_unit(const AttendArgs &a, int32_t index, Unit &u) {
-  const int lane = threadIdx.x & (kWave - 1);
-  int32_t before = 0;
-  for (int32_t b0 = 0; b0 < a.B; b0 += kWave) {
-    const int32_t b = b0 + lane;
-    int32_t first = 0, n = 0;
-    if (b < a.B) {
-      first = max(a.q_start[b], 0);
-      n = max(min(a.q_start[b + 1], a.T) - first, 0);
-    }
-    const int32_t blocks = (int32_t) (((int64_t) n * a.G + R - 1) / R);
-    int32_t upto = blocks;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int32_t x = __shfl_up(upto, d);
-      if (lane >= d) upto += x;
-    }
-    const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > index);
-    if (past) {
-      const int l = __ffsll((long long) past) - 1;
-      u.b = b0 + l;
-      u.first = __builtin_amdgcn_readlane(first, l);
-      const int32_t nn = __builtin_amdgcn_readlane(n, l);
-      u.rows = nn * a.G;
-      u.r0 = (index - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(blocks, l))) * R;
-      u.ctx = a.lens ? min(max(a.lens[u.b], 0), a.max_ctx) : 0;
-      return true;
-    }
-    before += __builtin_amdgcn_readlane(upto, kWave - 1);
-  }
-  return false;
+__device__ __forceinline__ void unit_keys(const AttendArgs &a, Unit &u) {
+  const int32_t t_first = u.r0 / a.G, t_last = (min(u.r0 + R, u.rows) - 1) / a.G;
+  u.k_hi = u.ctx + t_last + 1;
+  u.min_hi = u.ctx + t_first + 1;
+  u.k_lo = a.window > 0 ? max(0, u.min_hi - a.window) & ~31 : 0;
+  u.max_lo = a.window > 0 ? u.k_hi - a.window : 0;
 }
 
-template <typename T, int DP, int WR, bool PAGED>
-__global__ __launch_bounds__(kAttendThreads) void attend_kernel(AttendArgs a) {
-  using S = Shape<T, DP, WR>;
-  constexpr int R = 32 * WR;
-  constexpr int E = 16 / (int) sizeof(T);
-  __shared__ __align__(16) unsigned char lds[S::kLdsBytes];
-  __shared__ int flag;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, half = lane >> 5, wr = wave % WR, wk = wave / WR;
-  Unit u;
-  if (!find_unit<R>(a, (int32_t) (blockIdx.x / (uint32_t) a.heads_kv), u)) return;
-  u.head = (int32_t) (blockIdx.x % (uint32_t) a.heads_kv);
+// First row and tokens of request b.  Whatever q_start holds, nothing outside the batch is named.
+__device__ __forceinline__ int32_t request_tokens(const AttendArgs &a, int32_t b, int32_t &first) {
+  first = max(fixed_at(a.q_start, b), 0);
+  return max(min(fixed_at(a.q_start, b + 1), a.T) - first, 0);
+}
+__device__ __forceinline__ int32_t request_ctx(const AttendArgs &a, int32_t b) {
+  return a.lens ? min(max(fixed_at(a.lens, b), 0), a.max_ctx) : 0;
+}
 
-  const int32_t r = u.r0 + wr * 32 + l32;
-  const bool mine = r < u.rows;
-  uint32_t t, g;
-  split_by((uint32_t) (mine ? r : 0), (uint32_t) a.G, a.magic_G, t, g);
-  const int32_t pos = u.ctx + (int32_t) t;
-  const int32_t head = u.head * a.G + (int32_t) g;
-  u32x4 qf[S::NQ];
-  {
-    const T *q = reinterpret_cast<const T *>(a.q) + (int64_t) (u.first + (int32_t) t) * a.q_tok + (int64_t) head * a.q_head;
-#pragma unroll
-    for (int i = 0; i < S::NQ; ++i) {
-      const int d = (2 * i + half) * E;
-      qf[i] = *(mine && d < a.D ? reinterpret_cast<const u32x4 *>(q + d) : &kZeros);
-    }
+// Brings ROWS keys or values of a unit, beginning at key k0, into LDS: loads of 16 bytes a lane, 1024 bytes of LDS in a row each,
+// dealt to NW waves.  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
+// multiple of 32) share a page, which the scalar unit looks up; 2: pages of any size.  Columns behind D get the row's first ones: keys are cleared there
+// where they are used (scores), values make columns that nobody stores.
+template <typename T, int DP, int ROWS, int NW, int PAGES>
+struct Loader {
+  using S = Shape<T, DP>;
+  static constexpr int NI = ROWS / S::RPI / NW;                       // loads of a wave
+  static constexpr int kStep = S::RPI * NW;                           // keys from one of its loads to the next
+  static constexpr int NK = kStep < 16 ? 16 / kStep : 1;              // after so many the order of chunks repeats
+  static constexpr int NV = kStep < (S::kBf16 ? 4 : 8) ? (S::kBf16 ? 4 : 8) / kStep : 1;
+  const AttendArgs &a;
+  const Unit &u;
+  const int lane, wave;
+  const int32_t *table;
+  const char *kb, *vb;
+  uint32_t koff[NK], voff[NV];       // of this lane from the first of a load's keys
+
+  template <bool VALUES>
+  __device__ __forceinline__ int chunk(int row) const {
+    const int pos = lane % S::CH;
+    const int ch = VALUES ? value_swap<S::RB, S::kBf16>(row, pos) : key_swap<S::RB>(row, pos);
+    return ch * S::E < a.D ? ch : 0;
   }
-  const int32_t t_first = u.r0 / a.G, t_last = (min(u.r0 + R, u.rows) - 1) / a.G;
-  const int32_t k_hi = u.ctx + t_last + 1, min_hi = u.ctx + t_first + 1;
-  const int32_t k_lo = a.window > 0 ? max(0, min_hi - a.window) : 0;
-  const int32_t max_lo = a.window > 0 ? k_hi - a.window : 0;
+  __device__ __forceinline__ Loader(const AttendArgs &a_, const Unit &u_, int lane_, int wave_)
+      : a(a_), u(u_), lane(lane_), wave(wave_), table(PAGES ? a_.table + (int64_t) u_.b * a_.table_stride : nullptr) {
+    kb = reinterpret_cast<const char *>(a.k) + (int64_t) u.head * a.k_head * (int) sizeof(T);
+    vb = reinterpret_cast<const char *>(a.v) + (int64_t) u.head * a.v_head * (int) sizeof(T);
+    const int row_in = lane / S::CH;
+#pragma unroll
+    for (int j = 0; j < NK; ++j)
+      koff[j] = (uint32_t) (row_in * (int32_t) a.k_tok + chunk<false>(j * kStep + wave * S::RPI + row_in) * S::E) * (uint32_t) sizeof(T);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      voff[j] = (uint32_t) (row_in * (int32_t) a.v_tok + chunk<true>(j * kStep + wave * S::RPI + row_in) * S::E) * (uint32_t) sizeof(T);
+  }
 
-  floatx16 o[S::NO];
+  template <bool VALUES>
+  __device__ __forceinline__ void load(int32_t k0, unsigned char *tile) const {
+    const char *base = VALUES ? vb : kb;
+    const int64_t tok = VALUES ? a.v_tok : a.k_tok, page_stride = VALUES ? a.v_page : a.k_page;
+    bool whole = PAGES < 2 && k0 + ROWS <= u.k_hi;
+    if (whole) {
+      constexpr int kShared = kStep < 16 ? 16 / kStep : 1;      // loads of this wave from the same 16 keys
+      const char *from[NI / kShared];
 #pragma unroll
-  for (int n = 0; n < S::NO; ++n) o[n] = floatx16{};
-  float ref = -INFINITY, sum = 0.f;
-  attend_keys<T, DP, WR, PAGED>(a, u, k_lo, k_hi, lds, &flag, qf, pos, min_hi, max_lo, o, ref, sum);
-  sum += other_half(sum);
-
-  if constexpr (S::WK > 1) {
-    // the waves that had the other keys of these rows, one after the other, through LDS
-    float *part = reinterpret_cast<float *>(lds) + wr * (DP + 2) * 32;
-#pragma unroll
-    for (int w = 1; w < S::WK; ++w) {
-      __syncthreads();
-      if (wk == w) {
-#pragma unroll
-        for (int n = 0; n < S::NO; ++n)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) part[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] = o[n][i];
-        if (half == 0) {
-          part[DP * 32 + l32] = ref;
-          part[(DP + 1) * 32 + l32] = sum;
+      for (int j = 0; j < NI / kShared; ++j) {
+        const int32_t key = k0 + j * kShared * kStep + wave * S::RPI;
+        if constexpr (PAGES) {
+          uint32_t block, slot;
+          split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
+          const int32_t page = fixed_at(table, min(block, (uint32_t) a.max_blocks - 1));
+          whole = whole && (uint32_t) page < (uint32_t) a.num_pages && block < (uint32_t) a.max_blocks;
+          from[j] = base + ((int64_t) page * page_stride + (int64_t) slot * tok) * (int) sizeof(T);
+        } else {
+          from[j] = base + (int64_t) (u.first + key) * tok * (int) sizeof(T);
         }
       }
-      __syncthreads();
-      if (wk == 0) {
-        const float theirs = part[DP * 32 + l32], now = fmaxf(ref, theirs);
-        const float f0 = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
-        const float f1 = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(theirs - now);
-        ref = now;
-        sum = sum * f0 + part[(DP + 1) * 32 + l32] * f1;
+      if (whole) {
 #pragma unroll
-        for (int n = 0; n < S::NO; ++n)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            o[n][i] = o[n][i] * f0 + part[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] * f1;
+        for (int j = 0; j < NI; ++j)
+          put(from[j / kShared] + (j % kShared) * kStep * tok * (int) sizeof(T) + (VALUES ? voff[j % NV] : koff[j % NK]),
+              tile + (j * NW + wave) * 1024);
+        return;
       }
     }
-    if (wk != 0) return;
+    // the last tile, pages of odd sizes, pages outside the cache
+    constexpr int kAtOnce = NI < 4 ? NI : 4;
+#pragma unroll 1
+    for (int j0 = 0; j0 < NI; j0 += kAtOnce) {
+      int64_t from[kAtOnce];
+      bool there[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int32_t key = k0 + (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
+        there[i] = key < u.k_hi;
+        if constexpr (PAGES) {
+          uint32_t block, slot;
+          split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
+          there[i] = there[i] && block < (uint32_t) a.max_blocks;
+          const int32_t page = there[i] ? fixed_at(table, block) : -1;
+          there[i] = (uint32_t) page < (uint32_t) a.num_pages;
+          from[i] = (int64_t) page * page_stride + (int64_t) slot * tok;
+        } else {
+          from[i] = (int64_t) (u.first + key) * tok;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int row = (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
+        put(there[i] ? base + (from[i] + chunk<VALUES>(row) * S::E) * (int) sizeof(T) : reinterpret_cast<const char *>(&kZeros),
+            tile + ((j0 + i) * NW + wave) * 1024);
+      }
+    }
   }
-  if (!mine) return;
+  static __device__ __forceinline__ void put(const char *from, unsigned char *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *) from,
+                                     (__attribute__((address_space(3))) void *) to, 16, 0, 0);
+  }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void multiply(floatx16 &s, u32x4 x, u32x4 y) {
+  if constexpr (BF16) {
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), s, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(y[e]), s, 0, 0, 0);
+  }
+}
+
+// The 16-byte chunk of a key that a lane multiplies in step i.  CUT: there is nothing behind D.
+template <typename T, int DP, bool CUT>
+__device__ __forceinline__ u32x4 key_chunk(const unsigned char *lk, int base, int lane, int i, int32_t D) {
+  using S = Shape<T, DP>;
+  const int ch = 2 * i + (lane >> 5);
+  const u32x4 x = *reinterpret_cast<const u32x4 *>(lk + key_at<S::RB>(base + (lane & 31), ch));
+  if constexpr (CUT) return ch * S::E < D ? x : u32x4{0, 0, 0, 0};
+  return x;
+}
+
+// Scores of 32 keys, the first at row `base` of the tile: register 4 j + i is key base + 8 j + 4 half + i.  Queries in
+// registers, or of RB blocks of rows in LDS, laid out as keys are.
+template <typename T, int DP, bool CUT, int KB>
+__device__ __forceinline__ void scores(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], int32_t D,
+                                       floatx16 (&s)[KB]) {
+  using S = Shape<T, DP>;
+#pragma unroll
+  for (int k = 0; k < KB; ++k) {
+    s[k] = floatx16{};
+#pragma unroll
+    for (int i = 0; i < S::NQ; ++i) multiply<S::kBf16>(s[k], key_chunk<T, DP, CUT>(lk, 32 * k, lane, i, D), qf[i]);
+  }
+}
+template <typename T, int DP, bool CUT, int RB>
+__device__ __forceinline__ void scores(const unsigned char *lk, const unsigned char *lq, int lane, int32_t D, floatx16 (&s)[RB]) {
+  using S = Shape<T, DP>;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) s[rb] = floatx16{};
+#pragma unroll
+  for (int i = 0; i < S::NQ; ++i) {
+    const u32x4 kf = key_chunk<T, DP, CUT>(lk, 0, lane, i, D);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+      multiply<S::kBf16>(s[rb], kf,
+                         *reinterpret_cast<const u32x4 *>(lq + key_at<S::RB>(rb * 32 + (lane & 31), 2 * i + (lane >> 5))));
+    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);         // not all operands in registers at a time
+  }
+}
+
+// Keys that the row at position `pos` does not see: beyond it, or at `lo` and before.
+__device__ __forceinline__ void hide(floatx16 &s, int32_t key0, int half, int32_t pos, int32_t lo) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int32_t key = key0 + (r >> 2) * 8 + half * 4 + (r & 3);
+    if (key > pos || key <= lo) s[r] = -INFINITY;
+  }
+}
+
+// Scores of KB blocks of keys to weights 2^(c s - ref), their sum added; ref follows the rows' maxima where one runs more than
+// kLag ahead of it (the weights then stay below 2^kLag, and sums and outputs are rarely rescaled).
+template <int KB, int NO>
+__device__ __forceinline__ void weigh(floatx16 (&s)[KB], float c, float &ref, float &sum, floatx16 (&o)[NO]) {
+  float m[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) m[r & 1] = fmaxf(m[r & 1], s[k][r]);
+  const float mx = pair_max(fmaxf(m[0], m[1])) * c;
+  if (__builtin_amdgcn_ballot_w64(mx > ref + kLag) != 0) {
+    const float now = fmaxf(ref, mx);
+    const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
+    ref = now;
+    sum *= f;
+#pragma unroll
+    for (int n = 0; n < NO; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[n][r] *= f;
+  }
+  const float minus = ref == -INFINITY ? 0.f : -ref;
+  float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[k][r] = __builtin_amdgcn_exp2f(fmaf(s[k][r], c, minus));
+      z[r & 3] += s[k][r];
+    }
+  sum += (z[0] + z[1]) + (z[2] + z[3]);
+}
+
+// Operand of the product of weights and values: the weights of one 16 keys (bf16) or of two (float32) in a lane.
+// The weights are rounded to bf16 here (half a step, at most 2^-8 of each): the products take bf16 operands, and the
+// values that they multiply carry the same step.  Their sum is of the unrounded ones.
+__device__ __forceinline__ bf16x8 weights_of(const floatx16 &p, int c16) {
+  u32x4 pw;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const floatx2 two = {p[c16 * 8 + 2 * e], p[c16 * 8 + 2 * e + 1]};
+    pw[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+  }
+  return __builtin_bit_cast(bf16x8, pw);
+}
+// Values of 16 keys, the first at row `base`, columns 32 m ..: lane x of 16 reads 4 elements of key x / 4, columns
+// 4 (x % 4), and gets back column x of the four keys.
+template <int RB>
+__device__ __forceinline__ shortx8 values_of(const unsigned char *lv, int base, int lane, int m) {
+  const int row = base + (lane >> 5) * 4 + ((lane & 15) >> 2);
+  const int d = m * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+  typedef __attribute__((address_space(3))) shortx4 lds4;
+  const shortx4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *) (lv + value_at<RB, true>(row, d >> 3) + (d & 4) * 2));
+  const shortx4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *) (lv + value_at<RB, true>(row + 8, d >> 3) + (d & 4) * 2));
+  return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Value of register r's key (of 32 from row `base`), column 32 m + lane % 32.
+template <int RB>
+__device__ __forceinline__ float value_of(const unsigned char *lv, int base, int lane, int r, int m) {
+  const int row = base + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3), d = m * 32 + (lane & 31);
+  return *reinterpret_cast<const float *>(lv + value_at<RB, false>(row, d >> 2) + (d & 3) * 4);
+}
+
+// Adds weights times values of 32 keys, the first at row `base` of the tile, for RB blocks of rows.
+template <typename T, int DP, int RB>
+__device__ __forceinline__ void add_values(const unsigned char *lv, int base, int lane, const floatx16 (&p)[RB],
+                                           floatx16 (&o)[RB][Shape<T, DP>::NO]) {
+  using S = Shape<T, DP>;
+  if constexpr (S::kBf16) {
+#pragma unroll
+    for (int c16 = 0; c16 < 2; ++c16) {
+      bf16x8 pf[RB];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) pf[rb] = weights_of(p[rb], c16);
+#pragma unroll
+      for (int m = 0; m < S::NO; ++m) {
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, values_of<S::RB>(lv, base + c16 * 16, lane, m));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) o[rb][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[rb], o[rb][m], 0, 0, 0);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int m = 0; m < S::NO; ++m) {
+        const float x = value_of<S::RB>(lv, base, lane, r, m);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) o[rb][m] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[rb][r], o[rb][m], 0, 0, 0);
+      }
+  }
+}
+
+// Zero times a value that is not finite would be NaN in the rows that do not see the value.  Where not all rows see all keys of a
+// tile, such values are therefore taken out of it (`threads` threads, this one `index`, `bytes` of values) and, if there were
+// any, put back afterwards where they are seen (add_odd_values).
+template <bool BF16>
+__device__ __forceinline__ bool clear_odd_values(unsigned char *lv, int bytes, int index, int threads) {
+  bool odd = false;
+  for (int i = index * 16; i < bytes; i += threads * 16) {
+    u32x4 x = *reinterpret_cast<const u32x4 *>(lv + i);
+    if (!not_finite<BF16>(x)) continue;
+    odd = true;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (BF16) {
+        if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+        if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
+      } else if ((x[e] & 0x7f800000u) == 0x7f800000u) {
+        x[e] = 0;
+      }
+    }
+    *reinterpret_cast<u32x4 *>(lv + i) = x;
+  }
+  return odd;
+}
+
+// Adds the values that are not finite among keys [k0, k1) to the rows that see them.  (Their weights are positive, or so small that
+// they became zero, and then the product is NaN by the formula as well as here for a NaN.)
+template <typename T, int DP, bool PAGED>
+__device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Unit &u, int32_t k0, int32_t k1, int half, int32_t pos,
+                                               int32_t lo, floatx16 (&o)[DP / 32]) {
+#pragma nounroll
+  for (int32_t key = k0; key < k1; ++key) {
+    int64_t at = (int64_t) (u.first + key) * a.v_tok;
+    if constexpr (PAGED) {
+      uint32_t block, slot;
+      split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
+      if (block >= (uint32_t) a.max_blocks) return;
+      const int32_t page = fixed_at(a.table, (int64_t) u.b * a.table_stride + block);
+      if ((uint32_t) page >= (uint32_t) a.num_pages) continue;
+      at = (int64_t) page * a.v_page + (int64_t) slot * a.v_tok;
+    }
+    const T *v = reinterpret_cast<const T *>(a.v) + at + (int64_t) u.head * a.v_head;
+    const bool seen = key <= pos && key > lo;
+#pragma unroll
+    for (int m = 0; m < DP / 32; ++m)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int d = m * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
+        float x = 0.f;
+        if (d < a.D) {
+          if constexpr (sizeof(T) == 2) x = __uint_as_float((uint32_t) v[d] << 16);
+          else x = v[d];
+        }
+        if (seen && !(fabsf(x) < INFINITY)) o[m][r] += x;
+      }
+  }
+}
+
+// Where a row's query and output are, and its position.
+struct Row {
+  bool there;
+  int32_t pos;
+  int64_t token, head;
+};
+__device__ __forceinline__ Row row_at(const AttendArgs &a, const Unit &u, int32_t r) {
+  Row w;
+  w.there = r < u.rows;
+  uint32_t t, g;
+  split_by((uint32_t) (w.there ? r : 0), (uint32_t) a.G, a.magic_G, t, g);
+  w.pos = u.ctx + (int32_t) t;
+  w.token = u.first + (int32_t) t;
+  w.head = u.head * a.G + (int32_t) g;
+  return w;
+}
+
+template <typename T, int DP>
+__device__ __forceinline__ void load_query(const AttendArgs &a, const Row &w, int half, u32x4 (&qf)[Shape<T, DP>::NQ]) {
+  using S = Shape<T, DP>;
+  const T *q = reinterpret_cast<const T *>(a.q) + w.token * a.q_tok + w.head * a.q_head;
+#pragma unroll
+  for (int i = 0; i < S::NQ; ++i) {
+    const int d = (2 * i + half) * S::E;
+    qf[i] = *(w.there && d < a.D ? reinterpret_cast<const u32x4 *>(q + d) : &kZeros);
+  }
+}
+
+// A row's output from its half in this lane: d = 32 n + 8 j + 4 half + i in register 4 j + i of o[n].
+template <typename T, int DP>
+__device__ __forceinline__ void store_row(const AttendArgs &a, const Row &w, int half, const floatx16 (&o)[Shape<T, DP>::NO],
+                                          float sum) {
+  using S = Shape<T, DP>;
+  if (!w.there) return;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  T *out = reinterpret_cast<T *>(a.out) + (int64_t) (u.first + (int32_t) t) * a.o_tok + (int64_t) head * a.o_head;
+  T *out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
 #pragma unroll
   for (int n = 0; n < S::NO; ++n)
 #pragma unroll
@@ -404,39 +514,642 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(AttendArgs a) {
       if (d >= a.D) continue;
       if constexpr (S::kBf16) {
         const floatx2 x = {o[n][4 * j] * inv, o[n][4 * j + 1] * inv}, y = {o[n][4 * j + 2] * inv, o[n][4 * j + 3] * inv};
-        *reinterpret_cast<uint2 *>(out + d) = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2)),
-                                                         __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2)));
+        *reinterpret_cast<u32x2 *>(out + d) = u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2)),
+                                                    __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2))};
       } else {
-        *reinterpret_cast<float4 *>(out + d) = make_float4(o[n][4 * j] * inv, o[n][4 * j + 1] * inv, o[n][4 * j + 2] * inv,
-                                                           o[n][4 * j + 3] * inv);
+        *reinterpret_cast<floatx4 *>(out + d) = floatx4{o[n][4 * j] * inv, o[n][4 * j + 1] * inv, o[n][4 * j + 2] * inv,
+                                                        o[n][4 * j + 3] * inv};
       }
     }
 }
 
-template <typename T, int DP, int WR, bool PAGED>
-hipError_t go(const AttendArgs &a, hipStream_t stream) {
-  const int64_t units = (int64_t) a.T * a.G / (32 * WR) + a.B;
-  attend_kernel<T, DP, WR, PAGED><<<dim3((uint32_t) (units * a.heads_kv)), kAttendThreads, 0, stream>>>(a);
-  return hipGetLastError();
+// ---- parts of a unit whose keys are split over workgroups ------------------------------------------------------------------
+
+// Outputs (not divided), reference maxima and sums of R rows.
+template <int DP, int R>
+struct Part {
+  float o[R][DP];
+  float ref[R], sum[R];
+};
+
+// What attend_join_kernel finds at the workgroup that began a split unit: its parts are this workgroup's slot 1 and slot 0 of
+// the parts - 1 that follow.
+struct Join {
+  int32_t parts, b, head, r0;
+};
+
+template <int DP, int R>
+__device__ __forceinline__ void store_part(Part<DP, R> *p, int row, int half, bool there, const floatx16 (&o)[DP / 32], float ref,
+                                           float sum) {
+  if (!there) return;
+#pragma unroll
+  for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<floatx4 *>(&p->o[row][n * 32 + j * 8 + half * 4]) =
+          floatx4{o[n][4 * j], o[n][4 * j + 1], o[n][4 * j + 2], o[n][4 * j + 3]};
+  if (half == 0) {
+    p->ref[row] = ref;
+    p->sum[row] = sum;
+  }
+}
+
+// Tiles of TK keys of the unit that begins at row r0.
+template <int R, int TK>
+__device__ __forceinline__ int32_t unit_tiles(const AttendArgs &a, Unit &u) {
+  unit_keys<R>(a, u);
+  return (u.k_hi - u.k_lo + TK - 1) / TK;
+}
+
+// The tiles of all units (requests, their shared heads, their row blocks, in this order) are cut into `runs` equal runs, one a
+// workgroup: run i is tiles [total i / runs, total (i + 1) / runs).
+struct Run {
+  int64_t total, runs, end, left;
+};
+
+// Finds run `index` of at most `count` runs of at least `least` tiles: its first unit and the tile in it.
+// Every workgroup adds the requests up by itself: for 64 of them that takes a microsecond, less than a launch ahead would.
+template <int R, int TK>
+__device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t index, int32_t count, int32_t least, unsigned char *lds, Unit &u,
+                                        int32_t &tile) {
+  int64_t *wave_sum = reinterpret_cast<int64_t *>(lds);
+  int32_t *found = reinterpret_cast<int32_t *>(wave_sum + kAttendWaves);
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int32_t each = (a.B + kAttendThreads - 1) / kAttendThreads, b0 = min(tid * each, a.B), b1 = min(b0 + each, a.B);
+  auto request = [&](int32_t b, Unit &v) {
+    v.b = b;
+    v.rows = request_tokens(a, b, v.first) * a.G;
+    v.ctx = request_ctx(a, b);
+  };
+  auto tiles_of = [&](int32_t b) -> int64_t {        // of one shared head
+    Unit v;
+    request(b, v);
+    int64_t sum = 0;
+    for (v.r0 = 0; v.r0 < v.rows; v.r0 += R) sum += unit_tiles<R, TK>(a, v);
+    return sum;
+  };
+  int64_t mine = 0;
+  for (int32_t b = b0; b < b1; ++b) mine += tiles_of(b);
+  mine *= a.heads_kv;
+  int64_t upto = mine;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int64_t x = __shfl_up(upto, d);
+    if (lane >= d) upto += x;
+  }
+  if (lane == kWave - 1) wave_sum[wave] = upto;
+  __syncthreads();
+  Run run;
+  run.total = 0;
+#pragma unroll
+  for (int w = 0; w < kAttendWaves; ++w) {
+    const int64_t x = wave_sum[w];
+    if (w < wave) upto += x;
+    run.total += x;
+  }
+  run.total = scalar(run.total);
+  run.runs = min((int64_t) count, (run.total + least - 1) / least);
+  run.left = 0;
+  if (index >= run.runs) return run;
+  const int64_t begin = scalar(run.total * index / run.runs);
+  run.end = scalar(run.total * (index + 1) / run.runs);
+  run.left = run.end - begin;
+  if (upto - mine <= begin && begin < upto) {
+    int64_t ahead = begin - (upto - mine);
+    for (int32_t b = b0; b < b1; ++b) {
+      const int64_t one = tiles_of(b);
+      if (ahead >= one * a.heads_kv) {
+        ahead -= one * a.heads_kv;
+        continue;
+      }
+      Unit v;
+      request(b, v);
+      const int32_t head = (int32_t) (ahead / one);
+      ahead -= head * one;
+      for (v.r0 = 0; v.r0 < v.rows; v.r0 += R) {
+        const int32_t t = unit_tiles<R, TK>(a, v);
+        if (ahead < t) break;
+        ahead -= t;
+      }
+      found[0] = b;
+      found[1] = head;
+      found[2] = v.r0;
+      found[3] = (int32_t) ahead;
+      break;
+    }
+  }
+  __syncthreads();
+  u.b = __builtin_amdgcn_readfirstlane(found[0]);
+  u.head = __builtin_amdgcn_readfirstlane(found[1]);
+  u.r0 = __builtin_amdgcn_readfirstlane(found[2]);
+  tile = __builtin_amdgcn_readfirstlane(found[3]);
+  __syncthreads();                      // the tiles of the first piece come here
+  request(u.b, u);
+  return run;
+}
+
+// The unit behind u.
+template <int R>
+__device__ __forceinline__ void next_unit(const AttendArgs &a, Unit &u) {
+  u.r0 += R;
+  if (u.r0 < u.rows) return;
+  u.r0 = 0;
+  if (++u.head < a.heads_kv) return;
+  u.head = 0;
+  do {
+    if (++u.b >= a.B) return;
+    u.rows = request_tokens(a, u.b, u.first) * a.G;
+  } while (u.rows == 0);
+  u.ctx = request_ctx(a, u.b);
+}
+
+// Calls work(unit, first tile, tiles, part) for every unit or piece of one in this workgroup's run; part: NULL where the unit is
+// whole.  A workgroup has two places for parts: 1 for the unit that it begins and does not finish, 0 for one that another began.
+template <int DP, int R, int TK, typename Work>
+__device__ __forceinline__ void work_on_run(const AttendArgs &a, int32_t least, unsigned char *lds, Join *join, Part<DP, R> *parts,
+                                            Work work) {
+  const int32_t index = (int32_t) blockIdx.x, count = (int32_t) gridDim.x;
+  Unit u;
+  int32_t tile = 0;
+  Run run = find_run<R, TK>(a, index, count, least, lds, u, tile);
+  run.left = scalar(run.left);
+  run.runs = scalar(run.runs);
+  Join j{0, 0, 0, 0};
+  while (run.left > 0) {
+    u = scalar(u);
+    const int32_t all = scalar(unit_tiles<R, TK>(a, u));
+    const int32_t tiles = (int32_t) min((int64_t) (all - tile), run.left);
+    Part<DP, R> *part = tiles == all ? nullptr : parts + 2 * (int64_t) index + (tile == 0);
+    if (part && tile == 0) {
+      // run i begins ahead of this unit's end, tile `end`, if total i < end runs
+      const int64_t end = run.end + all - tiles;
+      j.parts = (int32_t) ((end * run.runs + run.total - 1) / run.total) - index;
+      j.b = u.b;
+      j.head = u.head;
+      j.r0 = u.r0;
+    }
+    work(u, tile, tiles, part);
+    run.left -= tiles;
+    tile = 0;
+    if (run.left > 0) next_unit<R>(a, u);
+  }
+  if (threadIdx.x == 0) join[index] = j;
+}
+
+// ---- 128 rows a workgroup ----------------------------------------------------------------------------------------------
+
+template <typename T, int DP>
+struct Thick {
+  using S = Shape<T, DP>;
+  static constexpr int KB = S::kBf16 ? 2 : 1;
+  static constexpr int TK = 32 * KB;
+  static constexpr int kTile = TK * S::RB;
+  static constexpr int kLds = 4 * kTile;            // keys and values, two of each
+};
+
+template <typename T, int DP, int PAGES>
+__device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
+                                            int *odd, Part<DP, kThickRows> *part) {
+  using S = Shape<T, DP>;
+  using W = Thick<T, DP>;
+  int tid = threadIdx.x;
+  asm("" : "+v"(tid));                  // what follows from it is formed here, not kept in registers from piece to piece
+  const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, half = lane >> 5;
+  const Loader<T, DP, W::TK, kAttendWaves, PAGES> loader(a, u, lane, wave);
+  int32_t k0 = u.k_lo + tile * W::TK;
+  const int32_t end = min(u.k_hi, k0 + tiles * W::TK);
+  unsigned char *cur = lds, *nxt = lds + 2 * W::kTile;
+  auto load = [&](int32_t k, unsigned char *to) {
+    loader.template load<false>(k, to);
+    loader.template load<true>(k, to + W::kTile);
+  };
+  bare_barrier();                       // nobody reads the piece before any more
+  load(k0, cur);
+  if (tid == 0) *odd = 0;               // read behind a barrier of the loop: a piece has a tile
+
+  const int32_t row = wave * 32 + l32;
+  const Row w = row_at(a, u, u.r0 + row);
+  u32x4 qf[S::NQ];
+  load_query<T, DP>(a, w, half, qf);
+  // rows of this wave, and the positions of its first and last
+  const int32_t last = min(u.r0 + wave * 32 + 32, u.rows) - 1;
+  const int32_t pos_first = u.ctx + (u.r0 + wave * 32) / a.G, pos_last = last >= u.r0 + wave * 32 ? u.ctx + last / a.G : -1;
+  const int32_t lo = a.window > 0 ? w.pos - a.window : -1;
+
+  floatx16 o[S::NO];
+#pragma unroll
+  for (int n = 0; n < S::NO; ++n) o[n] = floatx16{};
+  float ref = -INFINITY, sum = 0.f;
+  const int32_t begin = k0;
+  auto at_edge = [&](int32_t k) { return k + W::TK > u.min_hi || k < u.max_lo; };
+  for (; k0 < end; k0 += W::TK) {
+    wait_vm<0>();                       // this wave's part of the tile is in; past the barrier everyone's is
+    bare_barrier();
+    if (k0 + W::TK < end) load(k0 + W::TK, nxt);
+    if (at_edge(k0)) {
+      if (clear_odd_values<S::kBf16>(cur + W::kTile, W::kTile, tid, kAttendThreads)) *odd = 1;
+      bare_barrier();
+    }
+    if (k0 <= pos_last) {
+      const unsigned char *lk = cur, *lv = cur + W::kTile;
+      floatx16 s[W::KB];
+      if (a.D == DP) scores<T, DP, false>(lk, lane, qf, DP, s);
+      else scores<T, DP, true>(lk, lane, qf, a.D, s);
+      if (k0 + W::TK - 1 > pos_first || k0 < u.max_lo) {
+#pragma unroll
+        for (int k = 0; k < W::KB; ++k) hide(s[k], k0 + 32 * k, half, w.pos, lo);
+      }
+      weigh<W::KB, S::NO>(s, a.c, ref, sum, o);
+#pragma unroll
+      for (int k = 0; k < W::KB; ++k)
+        add_values<T, DP, 1>(lv, 32 * k, lane, reinterpret_cast<const floatx16(&)[1]>(s[k]),
+                             reinterpret_cast<floatx16(&)[1][S::NO]>(o));
+    }
+    unsigned char *x = cur;
+    cur = nxt;
+    nxt = x;
+  }
+  bare_barrier();
+  if (*odd) {
+    for (k0 = begin; k0 < end; k0 += W::TK)
+      if (at_edge(k0)) add_odd_values<T, DP, PAGES != 0>(a, u, k0, min(k0 + W::TK, u.k_hi), half, w.pos, lo, o);
+  }
+  sum = pair_sum(sum);
+  if (part) store_part<DP, kThickRows>(part, row, half, w.there, o, ref, sum);
+  else store_row<T, DP>(a, w, half, o, sum);
+}
+
+template <typename T, int DP, int PAGES>
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_thick_kernel(AttendArgs a, int32_t least, Join *join,
+                                                                         Part<DP, kThickRows> *parts) {
+  __shared__ __align__(16) unsigned char lds[Thick<T, DP>::kLds];
+  __shared__ int odd;
+  work_on_run<DP, kThickRows, Thick<T, DP>::TK>(a, least, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
+    thick_piece<T, DP, PAGES>(a, u, tile, tiles, lds, &odd, part);
+  });
+}
+
+// Unit `rank` of all requests' row blocks, the ones furthest down their prompt first: they have the most keys, and what is
+// begun last should be short.
+__device__ __forceinline__ bool find_prompt_unit(const AttendArgs &a, int32_t rank, Unit &u) {
+  const int lane = threadIdx.x & (kWave - 1);
+  auto blocks_of = [&](int32_t b) -> int32_t {
+    int32_t first;
+    return b < a.B ? (request_tokens(a, b, first) * a.G + kThickRows - 1) / kThickRows : 0;
+  };
+  const int32_t here = blocks_of(lane);
+  // units at block `level` (from 1) or further down
+  auto at_least = [&](int32_t level) -> int32_t {
+    int32_t n = max(0, here - level + 1);
+    for (int32_t b = lane + kWave; b < a.B; b += kWave) n += max(0, blocks_of(b) - level + 1);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
+    return n;
+  };
+  if (rank >= at_least(1)) return false;
+  int32_t most = here;
+  for (int32_t b = lane + kWave; b < a.B; b += kWave) most = max(most, blocks_of(b));
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) most = max(most, __shfl_xor(most, d));
+  int32_t lo = 1, hi = most + 1;       // at_least(lo) > rank >= at_least(hi)
+  while (hi - lo > 1) {
+    const int32_t mid = (lo + hi) >> 1;
+    if (at_least(mid) > rank) lo = mid;
+    else hi = mid;
+  }
+  int32_t ahead = rank - at_least(lo + 1);
+  for (int32_t b0 = 0; b0 < a.B; b0 += kWave) {
+    const uint64_t who = __builtin_amdgcn_ballot_w64((b0 ? blocks_of(b0 + lane) : here) >= lo);
+    const int32_t n = __popcll(who);
+    if (ahead >= n) {
+      ahead -= n;
+      continue;
+    }
+    const uint64_t me = __builtin_amdgcn_ballot_w64(((who >> lane) & 1) && __popcll(who & (((uint64_t) 1 << lane) - 1)) == ahead);
+    u.b = b0 + __ffsll((long long) me) - 1;
+    break;
+  }
+  u.b = __builtin_amdgcn_readfirstlane(u.b);
+  u.rows = request_tokens(a, u.b, u.first) * a.G;
+  u.ctx = 0;
+  u.r0 = (lo - 1) * kThickRows;
+  return true;
 }
 
 template <typename T, int DP>
-hipError_t go_rows(const AttendArgs &a, int64_t longest, hipStream_t stream) {
-  const int64_t rows = longest * a.G;
-  if constexpr (DP * sizeof(T) <= 256) {
-    if (rows <= 32) return a.table ? go<T, DP, 1, true>(a, stream) : go<T, DP, 1, false>(a, stream);
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_prompt_kernel(AttendArgs a) {
+  __shared__ __align__(16) unsigned char lds[Thick<T, DP>::kLds];
+  __shared__ int odd;
+  Unit u;
+  u.b = 0;
+  if (!find_prompt_unit(a, (int32_t) (blockIdx.x / (uint32_t) a.heads_kv), u)) return;
+  u.head = (int32_t) (blockIdx.x % (uint32_t) a.heads_kv);
+  const int32_t tiles = unit_tiles<kThickRows, Thick<T, DP>::TK>(a, u);
+  thick_piece<T, DP, 0>(a, scalar(u), 0, scalar(tiles), lds, &odd, nullptr);
+}
+
+// ---- 32 or 64 rows a workgroup -----------------------------------------------------------------------------------------
+
+template <typename T, int DP, int RB>
+struct Thin {
+  using S = Shape<T, DP>;
+  static constexpr int R = 32 * RB;
+  static constexpr int kTile = 32 * S::RB;
+  static constexpr int kQueries = RB > 1 ? R * S::RB : 0;       // two blocks' queries do not fit the registers
+  static constexpr int kLds = kAttendWaves * 2 * kTile + kQueries;
+  static_assert(2 * R * (DP + 2) * 4 <= kLds, "two waves' rows on their way to the others");
+  static constexpr int kRuns = 2 * kLds <= 160 * 1024 ? 512 : 256;       // what fits the chip at a time
+};
+
+template <typename T, int DP, int RB, int PAGES>
+__device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
+                                           Part<DP, 32 * RB> *part) {
+  using S = Shape<T, DP>;
+  using W = Thin<T, DP, RB>;
+  int tid = threadIdx.x;
+  asm("" : "+v"(tid));                  // what follows from it is formed here, not kept in registers from piece to piece
+  const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, half = lane >> 5;
+  const Loader<T, DP, 32, 1, PAGES> loader(a, u, lane, 0);
+  constexpr int NI = decltype(loader)::NI;
+  unsigned char *lk = lds + wave * 2 * W::kTile, *lv = lk + W::kTile, *lq = lds + kAttendWaves * 2 * W::kTile;
+  int32_t k0 = u.k_lo + tile * kThinKeys + wave * 32;
+  const int32_t end = min(u.k_hi, u.k_lo + (tile + tiles) * kThinKeys);
+  __syncthreads();                      // nobody uses the piece before any more
+  if (k0 < end) {
+    loader.template load<false>(k0, lk);
+    loader.template load<true>(k0, lv);
   }
-  if (rows <= 64) return a.table ? go<T, DP, 2, true>(a, stream) : go<T, DP, 2, false>(a, stream);
-  return a.table ? go<T, DP, 4, true>(a, stream) : go<T, DP, 4, false>(a, stream);
+  u32x4 qf[S::NQ];
+  int32_t pos[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) pos[rb] = row_at(a, u, u.r0 + rb * 32 + l32).pos;
+  if constexpr (RB == 1) {
+    load_query<T, DP>(a, row_at(a, u, u.r0 + l32), half, qf);
+  } else {
+    if (wave < RB) {
+      load_query<T, DP>(a, row_at(a, u, u.r0 + wave * 32 + l32), half, qf);
+#pragma unroll
+      for (int i = 0; i < S::NQ; ++i)
+        *reinterpret_cast<u32x4 *>(lq + key_at<S::RB>(wave * 32 + l32, 2 * i + half)) = qf[i];
+    }
+    bare_barrier();
+  }
+  floatx16 o[RB][S::NO];
+  float ref[RB], sum[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+    for (int n = 0; n < S::NO; ++n) o[rb][n] = floatx16{};
+    ref[rb] = -INFINITY;
+    sum[rb] = 0.f;
+  }
+  const int32_t begin = k0;
+  auto at_edge = [&](int32_t k) { return k + 32 > u.min_hi || k < u.max_lo; };
+  bool odd = false;
+  for (; k0 < end; k0 += kThinKeys) {
+    const bool more = k0 + kThinKeys < end;
+    wait_vm<NI>();                      // keys are in, values may be on their way
+    floatx16 s[RB];
+    if constexpr (RB == 1) {
+      if (a.D == DP) scores<T, DP, false>(lk, lane, qf, DP, s);
+      else scores<T, DP, true>(lk, lane, qf, a.D, s);
+    } else {
+      int away = (int) (lq - lk);
+      asm volatile("" : "+s"(away));    // an addition a read, instead of as many addresses in registers
+      if (a.D == DP) scores<T, DP, false>(lk, lk + away, lane, DP, s);
+      else scores<T, DP, true>(lk, lk + away, lane, a.D, s);
+    }
+    wait_lds();
+    if (more) loader.template load<false>(k0 + kThinKeys, lk);
+    const bool edge = at_edge(k0);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      if (edge) hide(s[rb], k0, half, pos[rb], a.window > 0 ? pos[rb] - a.window : -1);
+      weigh<1, S::NO>(reinterpret_cast<floatx16(&)[1]>(s[rb]), a.c, ref[rb], sum[rb], o[rb]);
+    }
+    if (more) wait_vm<NI>();
+    else wait_vm<0>();
+    if (edge) {
+      odd = __builtin_amdgcn_ballot_w64(clear_odd_values<S::kBf16>(lv, W::kTile, lane, kWave)) != 0 || odd;
+      wait_lds();
+    }
+    add_values<T, DP, RB>(lv, 0, lane, s, o);
+    wait_lds();
+    if (more) loader.template load<true>(k0 + kThinKeys, lv);
+  }
+
+  if (odd) {
+    for (k0 = begin; k0 < end; k0 += kThinKeys) {
+      if (!at_edge(k0)) continue;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+        add_odd_values<T, DP, PAGES != 0>(a, u, k0, min(k0 + 32, u.k_hi), half, pos[rb], a.window > 0 ? pos[rb] - a.window : -1, o[rb]);
+    }
+  }
+
+  // The waves' sums: 2 to 0 and 3 to 1, then 1 to 0 (with two blocks of rows 0 also gives its second to 1).
+  float *room = reinterpret_cast<float *>(lds);
+  constexpr int kBlock = 32 * (DP + 2);
+  auto give = [&](float *to, int rb) {
+#pragma unroll
+    for (int n = 0; n < S::NO; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) to[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] = o[rb][n][i];
+    const float all = pair_sum(sum[rb]);
+    if (half == 0) {
+      to[DP * 32 + l32] = ref[rb];
+      to[(DP + 1) * 32 + l32] = all;
+    }
+  };
+  auto take = [&](const float *from, int rb) {
+    const float theirs = from[DP * 32 + l32], now = fmaxf(ref[rb], theirs);
+    const float f0 = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[rb] - now);
+    const float f1 = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(theirs - now);
+    ref[rb] = now;
+    sum[rb] = sum[rb] * f0 + (half == 0 ? from[(DP + 1) * 32 + l32] * f1 : 0.f);
+#pragma unroll
+    for (int n = 0; n < S::NO; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        o[rb][n][i] = o[rb][n][i] * f0 + from[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] * f1;
+  };
+  __syncthreads();
+  if (wave >= 2) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) give(room + ((wave - 2) * RB + rb) * kBlock, rb);
+  }
+  __syncthreads();
+  if (wave < 2) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) take(room + (wave * RB + rb) * kBlock, rb);
+  }
+  __syncthreads();
+  if (wave == 1) give(room, 0);
+  if (RB > 1 && wave == 0) give(room + kBlock, RB - 1);
+  __syncthreads();
+  auto finish = [&](int rb) {
+    const float all = pair_sum(sum[rb]);
+    int32_t r = rb * 32 + l32;
+    asm("" : "+v"(r));                  // formed here, not kept in registers since the beginning
+    const Row w = row_at(a, u, u.r0 + r);
+    if (part) store_part<DP, 32 * RB>(part, r, half, w.there, o[rb], ref[rb], all);
+    else store_row<T, DP>(a, w, half, o[rb], all);
+  };
+  if (wave == 0) {
+    take(room, 0);
+    finish(0);
+  }
+  if (RB > 1 && wave == 1) {
+    take(room + kBlock, RB - 1);
+    finish(RB - 1);
+  }
+}
+
+template <typename T, int DP, int RB, int PAGES>
+__global__ __launch_bounds__(kAttendThreads, (Thin<T, DP, RB>::kRuns / 256)) void attend_thin_kernel(AttendArgs a, int32_t least,
+                                                                                                  Join *join,
+                                                                                                  Part<DP, 32 * RB> *parts) {
+  __shared__ __align__(16) unsigned char lds[Thin<T, DP, RB>::kLds];
+  work_on_run<DP, 32 * RB, kThinKeys>(a, least, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32 * RB> *part) {
+    thin_piece<T, DP, RB, PAGES>(a, u, tile, tiles, lds, part);
+  });
+}
+
+// ---- units in parts ----------------------------------------------------------------------------------------------------------
+
+// Workgroup i joins the parts of the unit that run i began and did not finish, a wave a row.
+template <typename T, int DP, int R>
+__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a, const Join *join, const Part<DP, R> *parts) {
+  const Join j = join[blockIdx.x];
+  if (j.parts < 2) return;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Unit u;
+  u.b = j.b;
+  u.head = j.head;
+  u.rows = request_tokens(a, j.b, u.first) * a.G;
+  u.ctx = request_ctx(a, j.b);
+  const Part<DP, R> *first = parts + 2 * (int64_t) blockIdx.x;
+  auto part_at = [&](int32_t p) -> const Part<DP, R> & { return first[p ? 2 * p : 1]; };
+  constexpr int kEach = DP / kWave;
+  for (int row = wave; row < R && j.r0 + row < u.rows; row += kJoinThreads / kWave) {
+    const Row w = row_at(a, u, j.r0 + row);
+    float top = -INFINITY;
+    for (int32_t p = lane; p < j.parts; p += kWave) top = fmaxf(top, part_at(p).ref[row]);
+    top = wave_max(top);
+    float o[kEach] = {}, sum = 0.f;
+    for (int32_t p0 = 0; p0 < j.parts; p0 += kWave) {
+      const int32_t p = p0 + lane;
+      float f = 0.f;
+      if (p < j.parts) {
+        f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part_at(p).ref[row] - top);
+        sum += f * part_at(p).sum[row];
+      }
+      const int32_t n = min(j.parts - p0, kWave);
+      for (int32_t i = 0; i < n; i += 4) {
+        float x[4][kEach];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float *from = &part_at(p0 + min(i + k, n - 1)).o[row][lane * kEach];
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) x[k][e] = from[e];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (i + k >= n) break;
+          const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i + k));
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) o[e] = fmaf(fi, x[k][e], o[e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T *out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int d = lane * kEach + e;
+      if (d >= a.D) continue;
+      if constexpr (sizeof(T) == 2) {
+        const floatx2 x = {o[e] * inv, 0.f};
+        out[d] = (T) __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+      } else {
+        out[d] = o[e] * inv;
+      }
+    }
+  }
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------------------
+
+constexpr int32_t kThickRuns = 512;
+
+constexpr size_t join_bytes(int32_t runs) { return ((size_t) runs * sizeof(Join) + 255) / 256 * 256; }
+
+template <typename T, int DP, int R>
+size_t parts_bytes(int32_t runs) { return join_bytes(runs) + 2 * (size_t) runs * sizeof(Part<DP, R>); }
+
+template <typename T, int DP, int R, typename Kernel>
+hipError_t split_launch(Kernel kernel, int32_t runs, int32_t least, const AttendArgs &a, void *workspace, hipStream_t stream) {
+  Join *join = reinterpret_cast<Join *>(workspace);
+  Part<DP, R> *parts = reinterpret_cast<Part<DP, R> *>(reinterpret_cast<char *>(workspace) + join_bytes(runs));
+  kernel<<<runs, kAttendThreads, 0, stream>>>(a, least, join, parts);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  attend_join_kernel<T, DP, R><<<runs, kJoinThreads, 0, stream>>>(a, join, parts);
+  return hipGetLastError();
+}
+
+// Rows of a request up to which the thin kernel takes a block of them at a time.
+template <typename T, int DP, int RB>
+hipError_t go_thin(const AttendArgs &a, bool shared_pages, void *workspace, hipStream_t stream) {
+  constexpr int32_t runs = Thin<T, DP, RB>::kRuns;
+  if (shared_pages) return split_launch<T, DP, 32 * RB>(attend_thin_kernel<T, DP, RB, 1>, runs, 1, a, workspace, stream);
+  return split_launch<T, DP, 32 * RB>(attend_thin_kernel<T, DP, RB, 2>, runs, 1, a, workspace, stream);
+}
+
+template <typename T, int DP>
+hipError_t go_cache(const AttendArgs &a, int64_t longest, void *workspace, hipStream_t stream) {
+  using S = Shape<T, DP>;
+  // 16 keys share a page, and those of a load lie within 32 bits of each other
+  const bool shared_pages = a.page_size % 16 == 0 && a.k_tok * S::RPI * (int64_t) sizeof(T) < (int64_t) 1 << 31;
+  const int64_t rows = longest * a.G;
+  if (rows <= 32) return go_thin<T, DP, 1>(a, shared_pages, workspace, stream);
+  if (rows <= 64) return go_thin<T, DP, 2>(a, shared_pages, workspace, stream);
+  if (shared_pages) return split_launch<T, DP, kThickRows>(attend_thick_kernel<T, DP, 1>, kThickRuns, 4, a, workspace, stream);
+  return split_launch<T, DP, kThickRows>(attend_thick_kernel<T, DP, 2>, kThickRuns, 4, a, workspace, stream);
+}
+
+template <typename T, int DP>
+size_t cache_bytes(int64_t rows) {
+  if (rows <= 32) return parts_bytes<T, DP, 32>(Thin<T, DP, 1>::kRuns);
+  if (rows <= 64) return parts_bytes<T, DP, 64>(Thin<T, DP, 2>::kRuns);
+  return parts_bytes<T, DP, kThickRows>(kThickRuns);
 }
 
 }  // namespace
 
-size_t attend_workspace_bytes(int32_t, int32_t, int64_t) { return 256; }
+size_t attend_workspace_bytes(int32_t G, int32_t D, int64_t longest) {
+  const int64_t rows = longest * G;
+  if (D <= 64) return max(cache_bytes<uint16_t, 64>(rows), cache_bytes<float, 64>(rows));
+  return max(cache_bytes<uint16_t, 128>(rows), cache_bytes<float, 128>(rows));
+}
 
-hipError_t launch_attend(const AttendArgs &a, bool bf16, int64_t longest, hipStream_t stream) {
-  if (bf16) return a.D <= 64 ? go_rows<uint16_t, 64>(a, longest, stream) : go_rows<uint16_t, 128>(a, longest, stream);
-  return a.D <= 64 ? go_rows<float, 64>(a, longest, stream) : go_rows<float, 128>(a, longest, stream);
+hipError_t launch_cache_attend(const AttendArgs &a, bool bf16, int64_t longest, void *workspace, hipStream_t stream) {
+  if (bf16) return a.D <= 64 ? go_cache<uint16_t, 64>(a, longest, workspace, stream) : go_cache<uint16_t, 128>(a, longest, workspace, stream);
+  return a.D <= 64 ? go_cache<float, 64>(a, longest, workspace, stream) : go_cache<float, 128>(a, longest, workspace, stream);
+}
+
+hipError_t launch_prompt_attend(const AttendArgs &a, bool bf16, hipStream_t stream) {
+  const int64_t units = (int64_t) a.T * a.G / kThickRows + a.B;
+  const dim3 grid((uint32_t) (units * a.heads_kv));
+  if (bf16 && a.D <= 64) attend_prompt_kernel<uint16_t, 64><<<grid, kAttendThreads, 0, stream>>>(a);
+  else if (bf16) attend_prompt_kernel<uint16_t, 128><<<grid, kAttendThreads, 0, stream>>>(a);
+  else if (a.D <= 64) attend_prompt_kernel<float, 64><<<grid, kAttendThreads, 0, stream>>>(a);
+  else attend_prompt_kernel<float, 128><<<grid, kAttendThreads, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace pcg

@@ -200,7 +200,7 @@ int pcg_cache_attend(const pcg_kv_cache *cache, const void *q, int64_t q_tok_str
   a.page_size = c.page_size;
   a.num_pages = c.num_pages;
   a.magic_page = magic(c.page_size);
-  return finish(launch_attend(a, c.dt == PCG_BF16, longest, (hipStream_t) hip_stream));
+  return finish(launch_cache_attend(a, c.dt == PCG_BF16, longest, workspace, (hipStream_t) hip_stream));
 }
 
 int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt, int64_t T, int32_t heads, int32_t kv_heads,
@@ -225,7 +225,7 @@ int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt,
   a.k_head = k_head_stride;
   a.v_tok = v_tok_stride;
   a.v_head = v_head_stride;
-  return finish(launch_attend(a, dt == PCG_BF16, longest, (hipStream_t) hip_stream));
+  return finish(launch_prompt_attend(a, dt == PCG_BF16, (hipStream_t) hip_stream));
 }
 
 }  // extern "C"
