@@ -36,7 +36,8 @@ constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = kAttendWaves * kWave;
 constexpr int kThickRows = 32 * kAttendWaves;
 constexpr int kThinKeys = 32 * kAttendWaves;      // keys a turn of the four waves takes
-constexpr int kJoinThreads = 1024;
+constexpr int kThinLeast = 1, kThickLeast = 4;     // tiles of a workgroup, at least
+constexpr int kJoinThreads = 256;
 constexpr float kLag = 8.f;        // how far (in powers of two) a maximum may run ahead of the one in use
 
 // What is read where there is nothing to read: keys behind the last, columns behind D.
@@ -145,9 +146,11 @@ __device__ __forceinline__ Unit scalar(const Unit &u) {
 
 template <int R>
 __device__ __forceinline__ void unit_keys(const AttendArgs &a, Unit &u) {
-  const int32_t t_first = u.r0 / a.G, t_last = (min(u.r0 + R, u.rows) - 1) / a.G;
-  u.k_hi = u.ctx + t_last + 1;
-  u.min_hi = u.ctx + t_first + 1;
+  uint32_t t_first, t_last, g;
+  split_by((uint32_t) u.r0, (uint32_t) a.G, a.magic_G, t_first, g);
+  split_by((uint32_t) (min(u.r0 + R, u.rows) - 1), (uint32_t) a.G, a.magic_G, t_last, g);
+  u.k_hi = u.ctx + (int32_t) t_last + 1;
+  u.min_hi = u.ctx + (int32_t) t_first + 1;
   u.k_lo = a.window > 0 ? max(0, u.min_hi - a.window) & ~31 : 0;
   u.max_lo = a.window > 0 ? u.k_hi - a.window : 0;
 }
@@ -202,20 +205,23 @@ struct Loader {
   __device__ __forceinline__ void load(int32_t k0, unsigned char *tile) const {
     const char *base = VALUES ? vb : kb;
     const int64_t tok = VALUES ? a.v_tok : a.k_tok, page_stride = VALUES ? a.v_page : a.k_page;
-    bool whole = PAGES < 2 && k0 + ROWS <= u.k_hi;
-    if (whole) {
+    if constexpr (PAGES < 2) {
       constexpr int kShared = kStep < 16 ? 16 / kStep : 1;      // loads of this wave from the same 16 keys
       const char *from[NI / kShared];
+      bool valid[NI / kShared], whole = k0 + ROWS <= u.k_hi;
 #pragma unroll
       for (int j = 0; j < NI / kShared; ++j) {
         const int32_t key = k0 + j * kShared * kStep + wave * S::RPI;
         if constexpr (PAGES) {
           uint32_t block, slot;
           split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
-          const int32_t page = fixed_at(table, min(block, (uint32_t) a.max_blocks - 1));
-          whole = whole && (uint32_t) page < (uint32_t) a.num_pages && block < (uint32_t) a.max_blocks;
+          valid[j] = block < (uint32_t) a.max_blocks && key < u.k_hi;
+          const int32_t page = valid[j] ? fixed_at(table, block) : 0;
+          valid[j] = valid[j] && (uint32_t) page < (uint32_t) a.num_pages;
+          whole = whole && valid[j];
           from[j] = base + ((int64_t) page * page_stride + (int64_t) slot * tok) * (int) sizeof(T);
         } else {
+          valid[j] = true;
           from[j] = base + (int64_t) (u.first + key) * tok * (int) sizeof(T);
         }
       }
@@ -224,35 +230,35 @@ struct Loader {
         for (int j = 0; j < NI; ++j)
           put(from[j / kShared] + (j % kShared) * kStep * tok * (int) sizeof(T) + (VALUES ? voff[j % NV] : koff[j % NK]),
               tile + (j * NW + wave) * 1024);
-        return;
-      }
-    }
-    // the last tile, pages of odd sizes, pages outside the cache
-    constexpr int kAtOnce = NI < 4 ? NI : 4;
-#pragma unroll 1
-    for (int j0 = 0; j0 < NI; j0 += kAtOnce) {
-      int64_t from[kAtOnce];
-      bool there[kAtOnce];
+      } else {
+        // a unit's last tile, or a page outside the cache: zeros where there is no key
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int32_t key = k0 + (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
-        there[i] = key < u.k_hi;
-        if constexpr (PAGES) {
-          uint32_t block, slot;
-          split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
-          there[i] = there[i] && block < (uint32_t) a.max_blocks;
-          const int32_t page = there[i] ? fixed_at(table, block) : -1;
-          there[i] = (uint32_t) page < (uint32_t) a.num_pages;
-          from[i] = (int64_t) page * page_stride + (int64_t) slot * tok;
-        } else {
-          from[i] = (int64_t) (u.first + key) * tok;
+        for (int j = 0; j < NI; ++j) {
+          const bool there = valid[j / kShared] && k0 + j * kStep + wave * S::RPI + lane / S::CH < u.k_hi;
+          const char *at = from[j / kShared] + (j % kShared) * kStep * tok * (int) sizeof(T) + (VALUES ? voff[j % NV] : koff[j % NK]);
+          put(there ? at : reinterpret_cast<const char *>(&kZeros), tile + (j * NW + wave) * 1024);
         }
       }
+    } else {
+      constexpr int kAtOnce = NI < 8 ? NI : 8;
+#pragma unroll 1
+      for (int j0 = 0; j0 < NI; j0 += kAtOnce) {
+        int32_t page[kAtOnce], slot[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int row = (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
-        put(there[i] ? base + (from[i] + chunk<VALUES>(row) * S::E) * (int) sizeof(T) : reinterpret_cast<const char *>(&kZeros),
-            tile + ((j0 + i) * NW + wave) * 1024);
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int32_t key = k0 + (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
+          uint32_t block, at;
+          split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, at);
+          const bool there = key < u.k_hi && block < (uint32_t) a.max_blocks;
+          page[i] = fixed_at(table, there ? block : 0);
+          slot[i] = there && (uint32_t) page[i] < (uint32_t) a.num_pages ? (int32_t) at : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int row = (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
+          const char *at = base + ((int64_t) page[i] * page_stride + (int64_t) slot[i] * tok + chunk<VALUES>(row) * S::E) * (int) sizeof(T);
+          put(slot[i] >= 0 ? at : reinterpret_cast<const char *>(&kZeros), tile + ((j0 + i) * NW + wave) * 1024);
+        }
       }
     }
   }
@@ -535,7 +541,7 @@ struct Part {
 // What attend_join_kernel finds at the workgroup that began a split unit: its parts are this workgroup's slot 1 and slot 0 of
 // the parts - 1 that follow.
 struct Join {
-  int32_t parts, b, head, r0;
+  int32_t parts, head, r0, rows, first;
 };
 
 template <int DP, int R>
@@ -562,15 +568,27 @@ __device__ __forceinline__ int32_t unit_tiles(const AttendArgs &a, Unit &u) {
 }
 
 // The tiles of all units (requests, their shared heads, their row blocks, in this order) are cut into `runs` equal runs, one a
-// workgroup: run i is tiles [total i / runs, total (i + 1) / runs).
+// workgroup, the first `longer` of them a tile longer than `each`.
 struct Run {
-  int64_t total, runs, end, left;
+  int32_t runs, longer;
+  int64_t each, left, end;
+  __device__ __forceinline__ int64_t begin(int32_t i) const { return each * i + min(i, longer); }
+  // the runs that begin ahead of tile x (which lies in one of them, or behind all)
+  __device__ __forceinline__ int32_t ahead_of(int64_t x) const {
+    int32_t lo = 0, hi = runs;
+    while (lo < hi) {                   // first run that begins at x or behind it
+      const int32_t mid = (lo + hi) >> 1;
+      if (begin(mid) < x) lo = mid + 1;
+      else hi = mid;
+    }
+    return lo;
+  }
 };
 
-// Finds run `index` of at most `count` runs of at least `least` tiles: its first unit and the tile in it.
+// Finds run `index` of at most `count` runs of at least LEAST tiles (but for the last): its first unit and the tile in it.
 // Every workgroup adds the requests up by itself: for 64 of them that takes a microsecond, less than a launch ahead would.
-template <int R, int TK>
-__device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t index, int32_t count, int32_t least, unsigned char *lds, Unit &u,
+template <int R, int TK, int LEAST>
+__device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t index, int32_t count, unsigned char *lds, Unit &u,
                                         int32_t &tile) {
   int64_t *wave_sum = reinterpret_cast<int64_t *>(lds);
   int32_t *found = reinterpret_cast<int32_t *>(wave_sum + kAttendWaves);
@@ -600,19 +618,24 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t index, int3
   if (lane == kWave - 1) wave_sum[wave] = upto;
   __syncthreads();
   Run run;
-  run.total = 0;
+  int64_t total = 0;
 #pragma unroll
   for (int w = 0; w < kAttendWaves; ++w) {
     const int64_t x = wave_sum[w];
     if (w < wave) upto += x;
-    run.total += x;
+    total += x;
   }
-  run.total = scalar(run.total);
-  run.runs = min((int64_t) count, (run.total + least - 1) / least);
+  total = scalar(total);
+  run.runs = (int32_t) min((int64_t) count, (total + LEAST - 1) / LEAST);
   run.left = 0;
   if (index >= run.runs) return run;
-  const int64_t begin = scalar(run.total * index / run.runs);
-  run.end = scalar(run.total * (index + 1) / run.runs);
+  // a quotient of numbers below 2^53, off by one at most in double
+  run.each = scalar((int64_t) ((double) total / (double) run.runs));
+  if (run.each * run.runs > total) --run.each;
+  if (total - run.each * run.runs >= run.runs) ++run.each;
+  run.longer = (int32_t) (total - run.each * run.runs);
+  const int64_t begin = run.begin(index);
+  run.end = run.begin(index + 1);
   run.left = run.end - begin;
   if (upto - mine <= begin && begin < upto) {
     int64_t ahead = begin - (upto - mine);
@@ -624,7 +647,9 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t index, int3
       }
       Unit v;
       request(b, v);
-      const int32_t head = (int32_t) (ahead / one);
+      int32_t head = (int32_t) ((double) ahead / (double) one);      // below 2^53: off by one at most
+      if (head * one > ahead) --head;
+      if (ahead - head * one >= one) ++head;
       ahead -= head * one;
       for (v.r0 = 0; v.r0 < v.rows; v.r0 += R) {
         const int32_t t = unit_tiles<R, TK>(a, v);
@@ -635,6 +660,9 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t index, int3
       found[1] = head;
       found[2] = v.r0;
       found[3] = (int32_t) ahead;
+      found[4] = v.rows;
+      found[5] = v.first;
+      found[6] = v.ctx;
       break;
     }
   }
@@ -643,8 +671,10 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t index, int3
   u.head = __builtin_amdgcn_readfirstlane(found[1]);
   u.r0 = __builtin_amdgcn_readfirstlane(found[2]);
   tile = __builtin_amdgcn_readfirstlane(found[3]);
+  u.rows = found[4];
+  u.first = found[5];
+  u.ctx = found[6];
   __syncthreads();                      // the tiles of the first piece come here
-  request(u.b, u);
   return run;
 }
 
@@ -665,28 +695,25 @@ __device__ __forceinline__ void next_unit(const AttendArgs &a, Unit &u) {
 
 // Calls work(unit, first tile, tiles, part) for every unit or piece of one in this workgroup's run; part: NULL where the unit is
 // whole.  A workgroup has two places for parts: 1 for the unit that it begins and does not finish, 0 for one that another began.
-template <int DP, int R, int TK, typename Work>
-__device__ __forceinline__ void work_on_run(const AttendArgs &a, int32_t least, unsigned char *lds, Join *join, Part<DP, R> *parts,
+template <int DP, int R, int TK, int LEAST, typename Work>
+__device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *lds, Join *join, Part<DP, R> *parts,
                                             Work work) {
   const int32_t index = (int32_t) blockIdx.x, count = (int32_t) gridDim.x;
   Unit u;
   int32_t tile = 0;
-  Run run = find_run<R, TK>(a, index, count, least, lds, u, tile);
-  run.left = scalar(run.left);
-  run.runs = scalar(run.runs);
-  Join j{0, 0, 0, 0};
+  Run run = find_run<R, TK, LEAST>(a, index, count, lds, u, tile);
+  Join j{0, 0, 0, 0, 0};
   while (run.left > 0) {
     u = scalar(u);
     const int32_t all = scalar(unit_tiles<R, TK>(a, u));
     const int32_t tiles = (int32_t) min((int64_t) (all - tile), run.left);
     Part<DP, R> *part = tiles == all ? nullptr : parts + 2 * (int64_t) index + (tile == 0);
     if (part && tile == 0) {
-      // run i begins ahead of this unit's end, tile `end`, if total i < end runs
-      const int64_t end = run.end + all - tiles;
-      j.parts = (int32_t) ((end * run.runs + run.total - 1) / run.total) - index;
-      j.b = u.b;
+      j.parts = run.ahead_of(run.end + all - tiles) - index;       // this one and those that begin ahead of the unit's end
       j.head = u.head;
       j.r0 = u.r0;
+      j.rows = u.rows;
+      j.first = u.first;
     }
     work(u, tile, tiles, part);
     run.left -= tiles;
@@ -781,11 +808,11 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
 }
 
 template <typename T, int DP, int PAGES>
-__global__ __launch_bounds__(kAttendThreads, 2) void attend_thick_kernel(AttendArgs a, int32_t least, Join *join,
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_thick_kernel(AttendArgs a, Join *join,
                                                                          Part<DP, kThickRows> *parts) {
   __shared__ __align__(16) unsigned char lds[Thick<T, DP>::kLds];
   __shared__ int odd;
-  work_on_run<DP, kThickRows, Thick<T, DP>::TK>(a, least, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
+  work_on_run<DP, kThickRows, Thick<T, DP>::TK, kThickLeast>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
     thick_piece<T, DP, PAGES>(a, u, tile, tiles, lds, &odd, part);
   });
 }
@@ -876,11 +903,7 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   unsigned char *lk = lds + wave * 2 * W::kTile, *lv = lk + W::kTile, *lq = lds + kAttendWaves * 2 * W::kTile;
   int32_t k0 = u.k_lo + tile * kThinKeys + wave * 32;
   const int32_t end = min(u.k_hi, u.k_lo + (tile + tiles) * kThinKeys);
-  __syncthreads();                      // nobody uses the piece before any more
-  if (k0 < end) {
-    loader.template load<false>(k0, lk);
-    loader.template load<true>(k0, lv);
-  }
+  bare_barrier();                      // nobody uses the piece before any more
   u32x4 qf[S::NQ];
   int32_t pos[RB];
 #pragma unroll
@@ -908,38 +931,45 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   const int32_t begin = k0;
   auto at_edge = [&](int32_t k) { return k + 32 > u.min_hi || k < u.max_lo; };
   bool odd = false;
-  for (; k0 < end; k0 += kThinKeys) {
-    const bool more = k0 + kThinKeys < end;
-    wait_vm<NI>();                      // keys are in, values may be on their way
+  // A turn works on keys k0 - kThinKeys and brings keys k0 behind it: one place in the code for each load.
+  for (bool now = false;; k0 += kThinKeys, now = true) {
+    const bool more = k0 < end;
+    if (!now && !more) break;
+    const int32_t k = k0 - kThinKeys;
     floatx16 s[RB];
-    if constexpr (RB == 1) {
-      if (a.D == DP) scores<T, DP, false>(lk, lane, qf, DP, s);
-      else scores<T, DP, true>(lk, lane, qf, a.D, s);
-    } else {
-      int away = (int) (lq - lk);
-      asm volatile("" : "+s"(away));    // an addition a read, instead of as many addresses in registers
-      if (a.D == DP) scores<T, DP, false>(lk, lk + away, lane, DP, s);
-      else scores<T, DP, true>(lk, lk + away, lane, a.D, s);
-    }
-    wait_lds();
-    if (more) loader.template load<false>(k0 + kThinKeys, lk);
-    const bool edge = at_edge(k0);
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      if (edge) hide(s[rb], k0, half, pos[rb], a.window > 0 ? pos[rb] - a.window : -1);
-      weigh<1, S::NO>(reinterpret_cast<floatx16(&)[1]>(s[rb]), a.c, ref[rb], sum[rb], o[rb]);
-    }
-    if (more) wait_vm<NI>();
-    else wait_vm<0>();
-    if (edge) {
-      odd = __builtin_amdgcn_ballot_w64(clear_odd_values<S::kBf16>(lv, W::kTile, lane, kWave)) != 0 || odd;
+    if (now) {
+      wait_vm<NI>();                    // keys are in, values may be on their way
+      if constexpr (RB == 1) {
+        if (a.D == DP) scores<T, DP, false>(lk, lane, qf, DP, s);
+        else scores<T, DP, true>(lk, lane, qf, a.D, s);
+      } else {
+        int away = (int) (lq - lk);
+        asm volatile("" : "+s"(away));  // an addition a read, instead of as many addresses in registers
+        if (a.D == DP) scores<T, DP, false>(lk, lk + away, lane, DP, s);
+        else scores<T, DP, true>(lk, lk + away, lane, a.D, s);
+      }
       wait_lds();
     }
-    add_values<T, DP, RB>(lv, 0, lane, s, o);
-    wait_lds();
-    if (more) loader.template load<true>(k0 + kThinKeys, lv);
+    if (more) loader.template load<false>(k0, lk);
+    if (now) {
+      const bool edge = at_edge(k);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        if (edge) hide(s[rb], k, half, pos[rb], a.window > 0 ? pos[rb] - a.window : -1);
+        weigh<1, S::NO>(reinterpret_cast<floatx16(&)[1]>(s[rb]), a.c, ref[rb], sum[rb], o[rb]);
+      }
+      if (more) wait_vm<NI>();
+      else wait_vm<0>();
+      if (edge) {
+        odd = __builtin_amdgcn_ballot_w64(clear_odd_values<S::kBf16>(lv, W::kTile, lane, kWave)) != 0 || odd;
+        wait_lds();
+      }
+      add_values<T, DP, RB>(lv, 0, lane, s, o);
+      wait_lds();
+    }
+    if (!more) break;
+    loader.template load<true>(k0, lv);
   }
-
   if (odd) {
     for (k0 = begin; k0 < end; k0 += kThinKeys) {
       if (!at_edge(k0)) continue;
@@ -975,20 +1005,20 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
       for (int i = 0; i < 16; ++i)
         o[rb][n][i] = o[rb][n][i] * f0 + from[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] * f1;
   };
-  __syncthreads();
+  bare_barrier();
   if (wave >= 2) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) give(room + ((wave - 2) * RB + rb) * kBlock, rb);
   }
-  __syncthreads();
+  bare_barrier();
   if (wave < 2) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) take(room + (wave * RB + rb) * kBlock, rb);
   }
-  __syncthreads();
+  bare_barrier();
   if (wave == 1) give(room, 0);
   if (RB > 1 && wave == 0) give(room + kBlock, RB - 1);
-  __syncthreads();
+  bare_barrier();
   auto finish = [&](int rb) {
     const float all = pair_sum(sum[rb]);
     int32_t r = rb * 32 + l32;
@@ -1008,59 +1038,61 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
 }
 
 template <typename T, int DP, int RB, int PAGES>
-__global__ __launch_bounds__(kAttendThreads, (Thin<T, DP, RB>::kRuns / 256)) void attend_thin_kernel(AttendArgs a, int32_t least,
+__global__ __launch_bounds__(kAttendThreads, (Thin<T, DP, RB>::kRuns / 256)) void attend_thin_kernel(AttendArgs a,
                                                                                                   Join *join,
                                                                                                   Part<DP, 32 * RB> *parts) {
   __shared__ __align__(16) unsigned char lds[Thin<T, DP, RB>::kLds];
-  work_on_run<DP, 32 * RB, kThinKeys>(a, least, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32 * RB> *part) {
+  work_on_run<DP, 32 * RB, kThinKeys, kThinLeast>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32 * RB> *part) {
     thin_piece<T, DP, RB, PAGES>(a, u, tile, tiles, lds, part);
   });
 }
 
 // ---- units in parts ----------------------------------------------------------------------------------------------------------
 
-// Workgroup i joins the parts of the unit that run i began and did not finish, a wave a row.
+// Workgroups (i, y) join the parts of the unit that run i began and did not finish, a wave a row, every second part to each half
+// of it.  A trip to memory takes a microsecond: 16 parts are asked for at a time.
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a, const Join *join, const Part<DP, R> *parts) {
   const Join j = join[blockIdx.x];
   if (j.parts < 2) return;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, half = lane >> 5;
   Unit u;
-  u.b = j.b;
   u.head = j.head;
-  u.rows = request_tokens(a, j.b, u.first) * a.G;
-  u.ctx = request_ctx(a, j.b);
+  u.rows = j.rows;
+  u.first = j.first;
+  u.ctx = 0;
   const Part<DP, R> *first = parts + 2 * (int64_t) blockIdx.x;
   auto part_at = [&](int32_t p) -> const Part<DP, R> & { return first[p ? 2 * p : 1]; };
-  constexpr int kEach = DP / kWave;
-  for (int row = wave; row < R && j.r0 + row < u.rows; row += kJoinThreads / kWave) {
+  constexpr int kEach = DP / 32, kAtOnce = 8;
+  typedef float vec __attribute__((ext_vector_type(kEach)));
+  const int32_t rows = min(R, u.rows - j.r0);
+  for (int row = blockIdx.y * (kJoinThreads / kWave) + wave; row < rows; row += gridDim.y * (kJoinThreads / kWave)) {
     const Row w = row_at(a, u, j.r0 + row);
-    float top = -INFINITY;
-    for (int32_t p = lane; p < j.parts; p += kWave) top = fmaxf(top, part_at(p).ref[row]);
-    top = wave_max(top);
-    float o[kEach] = {}, sum = 0.f;
+    vec o = {};
+    float sum = 0.f, top = -INFINITY;
     for (int32_t p0 = 0; p0 < j.parts; p0 += kWave) {
-      const int32_t p = p0 + lane;
-      float f = 0.f;
-      if (p < j.parts) {
-        f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part_at(p).ref[row] - top);
-        sum += f * part_at(p).sum[row];
-      }
+      // references and sums of 64 parts, one a lane
       const int32_t n = min(j.parts - p0, kWave);
-      for (int32_t i = 0; i < n; i += 4) {
-        float x[4][kEach];
+      const Part<DP, R> &mine = part_at(p0 + min(lane, n - 1));
+      const float ref = lane < n ? mine.ref[row] : -INFINITY;
+      const float now = fmaxf(top, wave_max(ref));
+      const float before = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
+      const float f = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
+      top = now;
+      sum = sum * before + (lane < n ? f * mine.sum[row] : 0.f);
+      o *= before;
+      for (int32_t i = 0; i < n; i += 2 * kAtOnce) {
+        vec x[kAtOnce];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float *from = &part_at(p0 + min(i + k, n - 1)).o[row][lane * kEach];
+        for (int k = 0; k < kAtOnce; ++k)
+          x[k] = *reinterpret_cast<const vec *>(&part_at(p0 + min(i + 2 * k + half, n - 1)).o[row][l32 * kEach]);
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) x[k][e] = from[e];
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (i + k >= n) break;
-          const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i + k));
-#pragma unroll
-          for (int e = 0; e < kEach; ++e) o[e] = fmaf(fi, x[k][e], o[e]);
+        for (int k = 0; k < kAtOnce; ++k) {
+          const int32_t p = i + 2 * k + half;
+          const float fp = __shfl(f, min(p, n - 1));
+    #pragma unroll
+          for (int e = 0; e < kEach; ++e) o[e] = p < n ? fmaf(fp, x[k][e], o[e]) : o[e];
         }
       }
     }
@@ -1069,15 +1101,19 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T *out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int d = lane * kEach + e;
-      if (d >= a.D) continue;
-      if constexpr (sizeof(T) == 2) {
-        const floatx2 x = {o[e] * inv, 0.f};
-        out[d] = (T) __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-      } else {
-        out[d] = o[e] * inv;
-      }
+    for (int e = 0; e < kEach; ++e) o[e] = pair_sum(o[e]) * inv;
+    const int d = l32 * kEach;
+    if (half || d >= a.D) continue;
+    if constexpr (sizeof(T) == 2) {
+      uint32_t two[kEach / 2];
+#pragma unroll
+      for (int e = 0; e < kEach / 2; ++e)
+        two[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{o[2 * e], o[2 * e + 1]}), bf16x2));
+#pragma unroll
+      for (int e = 0; e < kEach / 2; ++e) reinterpret_cast<uint32_t *>(out + d)[e] = two[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) out[d + e] = o[e];
     }
   }
 }
@@ -1092,13 +1128,13 @@ template <typename T, int DP, int R>
 size_t parts_bytes(int32_t runs) { return join_bytes(runs) + 2 * (size_t) runs * sizeof(Part<DP, R>); }
 
 template <typename T, int DP, int R, typename Kernel>
-hipError_t split_launch(Kernel kernel, int32_t runs, int32_t least, const AttendArgs &a, void *workspace, hipStream_t stream) {
+hipError_t split_launch(Kernel kernel, int32_t runs, const AttendArgs &a, void *workspace, hipStream_t stream) {
   Join *join = reinterpret_cast<Join *>(workspace);
   Part<DP, R> *parts = reinterpret_cast<Part<DP, R> *>(reinterpret_cast<char *>(workspace) + join_bytes(runs));
-  kernel<<<runs, kAttendThreads, 0, stream>>>(a, least, join, parts);
+  kernel<<<runs, kAttendThreads, 0, stream>>>(a, join, parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  attend_join_kernel<T, DP, R><<<runs, kJoinThreads, 0, stream>>>(a, join, parts);
+  attend_join_kernel<T, DP, R><<<dim3(runs, R / 4), kJoinThreads, 0, stream>>>(a, join, parts);
   return hipGetLastError();
 }
 
@@ -1106,8 +1142,8 @@ hipError_t split_launch(Kernel kernel, int32_t runs, int32_t least, const Attend
 template <typename T, int DP, int RB>
 hipError_t go_thin(const AttendArgs &a, bool shared_pages, void *workspace, hipStream_t stream) {
   constexpr int32_t runs = Thin<T, DP, RB>::kRuns;
-  if (shared_pages) return split_launch<T, DP, 32 * RB>(attend_thin_kernel<T, DP, RB, 1>, runs, 1, a, workspace, stream);
-  return split_launch<T, DP, 32 * RB>(attend_thin_kernel<T, DP, RB, 2>, runs, 1, a, workspace, stream);
+  if (shared_pages) return split_launch<T, DP, 32 * RB>(attend_thin_kernel<T, DP, RB, 1>, runs, a, workspace, stream);
+  return split_launch<T, DP, 32 * RB>(attend_thin_kernel<T, DP, RB, 2>, runs, a, workspace, stream);
 }
 
 template <typename T, int DP>
@@ -1118,8 +1154,8 @@ hipError_t go_cache(const AttendArgs &a, int64_t longest, void *workspace, hipSt
   const int64_t rows = longest * a.G;
   if (rows <= 32) return go_thin<T, DP, 1>(a, shared_pages, workspace, stream);
   if (rows <= 64) return go_thin<T, DP, 2>(a, shared_pages, workspace, stream);
-  if (shared_pages) return split_launch<T, DP, kThickRows>(attend_thick_kernel<T, DP, 1>, kThickRuns, 4, a, workspace, stream);
-  return split_launch<T, DP, kThickRows>(attend_thick_kernel<T, DP, 2>, kThickRuns, 4, a, workspace, stream);
+  if (shared_pages) return split_launch<T, DP, kThickRows>(attend_thick_kernel<T, DP, 1>, kThickRuns, a, workspace, stream);
+  return split_launch<T, DP, kThickRows>(attend_thick_kernel<T, DP, 2>, kThickRuns, a, workspace, stream);
 }
 
 template <typename T, int DP>

@@ -10,8 +10,8 @@ constexpr int kPagesThreads = 1024;
 constexpr int kPagesWaves = kPagesThreads / kWave;
 constexpr int kWriteThreads = 256;
 
-// Inclusive running sum over the workgroup, and the sum of all.  `part` holds a value per wave.
-template <typename T>
+// Inclusive running sum over the workgroup of WAVES waves, and the sum of all.  `part` holds a value per wave.
+template <int WAVES, typename T>
 __device__ __forceinline__ T block_scan(T v, T *part, T &total) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
 #pragma unroll
@@ -25,7 +25,7 @@ __device__ __forceinline__ T block_scan(T v, T *part, T &total) {
   T before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kPagesWaves; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     const T x = part[w];
     before += w < wave ? x : T(0);
     total += x;
@@ -63,8 +63,9 @@ __device__ __forceinline__ Request request_at(const PagesArgs &p, int32_t b) {
 
 // A run of pages that a request gives back or takes: upto[t] is the sum of the first t + 1 threads' counts.  Thread and place
 // of page `i` of them all.
+template <int THREADS>
 __device__ __forceinline__ int run_of(const int32_t *upto, int32_t i) {
-  int lo = 0, n = kPagesThreads;
+  int lo = 0, n = THREADS;
   while (n > 1) {                       // first t with upto[t] > i
     const int half = n >> 1;
     if (upto[lo + half - 1] <= i) lo += half;
@@ -92,7 +93,75 @@ __device__ __forceinline__ void place_token(const PagesArgs &p, const int32_t *s
   if (p.positions) p.positions[row] = position;
 }
 
-__global__ __launch_bounds__(kPagesThreads) void pages_step_kernel(PagesArgs p, int32_t fill_rows) {
+// As many threads as requests, or more: every request is read once and stays in registers.  Bound by trips to memory one after the
+// other (state, pages that come back, pages taken, the table for the slots); the running sums are two where nobody is refused.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void pages_step_kernel(PagesArgs p, int32_t fill_rows) {
+  constexpr int W = THREADS / kWave;
+  __shared__ int64_t part64[W];
+  __shared__ int32_t part[W];
+  __shared__ int32_t upto_back[THREADS], upto_taken[THREADS], need[THREADS], held[THREADS], starts[THREADS + 1], lens[THREADS];
+  const int tid = threadIdx.x, b = tid;
+  const int32_t free_in = min(max(p.state_in[3 * (int64_t) p.B], 0), p.num_pages);
+  Request r{0, 0, 0, 0, false};
+  if (b < p.B) r = request_at(p, b);
+  bool refuse = r.need > p.max_blocks;
+  const int64_t want = refuse ? 0 : r.want;
+  int64_t total;
+  const int64_t sum = block_scan<W>(want, part64, total);
+  refuse = refuse || (want > 0 && sum > p.max_tokens);
+  const int32_t gives = !refuse && r.held > r.need ? r.held - (int32_t) r.need : 0;
+  int32_t takes = !refuse && r.need > r.held ? (int32_t) r.need - r.held : 0;
+  int64_t both;
+  const int64_t moved = block_scan<W>((int64_t) gives << 32 | takes, part64, both);       // each sum is below 2^31
+  const int32_t back = (int32_t) (both >> 32), top = min(free_in + back, p.num_pages);
+  if (takes > 0 && (int32_t) moved > top) {
+    refuse = true;
+    takes = 0;
+  }
+  int32_t got = (int32_t) want, end = (int32_t) sum, given = (int32_t) both, all = (int32_t) total, refused = 0;
+  if (__syncthreads_or(refuse)) {
+    got = refuse ? 0 : got;
+    end = block_scan<W>(got, part, all);
+    (void) block_scan<W>(takes, part, given);
+    (void) block_scan<W>(refuse && r.asks ? 1 : 0, part, refused);
+  }
+  upto_back[tid] = (int32_t) (moved >> 32);
+  upto_taken[tid] = (int32_t) moved;
+  need[tid] = (int32_t) r.need;
+  held[tid] = r.held;
+  starts[tid] = end - got;
+  lens[tid] = r.len;
+  if (tid == THREADS - 1) starts[THREADS] = all;
+  __syncthreads();
+  for (int32_t i = tid; i < back; i += THREADS) {
+    const int t = run_of<THREADS>(upto_back, i);
+    const int32_t at = free_in + i, block = need[t] + i - (t ? upto_back[t - 1] : 0);
+    if (at < p.num_pages) p.free_pages[at] = p.table[(int64_t) t * p.table_stride + block];
+  }
+  if (back > 0) __syncthreads();         // what came back can be taken
+  for (int32_t i = tid; i < given; i += THREADS) {
+    const int t = run_of<THREADS>(upto_taken, i);
+    p.table[(int64_t) t * p.table_stride + held[t] + i - (t ? upto_taken[t - 1] : 0)] = p.free_pages[top - 1 - i];
+  }
+  if (b < p.B) {
+    p.state_out[b] = r.len;
+    p.state_out[p.B + b] = refuse ? r.held : (int32_t) r.need;
+    p.state_out[2 * (int64_t) p.B + b] = got;
+    p.q_start[b] = end - got;
+  }
+  if (tid == 0) {
+    p.state_out[3 * (int64_t) p.B] = top - given;
+    p.q_start[p.B] = all;
+    if (p.refused) *p.refused = refused;
+  }
+  if (!fill_rows) return;
+  if (given > 0) __syncthreads();        // the table is whole
+  for (int64_t row = tid; row < p.max_tokens; row += THREADS) place_token(p, starts, lens, all, row);
+}
+
+// More requests than threads: two passes over them.
+__global__ __launch_bounds__(kPagesThreads) void pages_step_large_kernel(PagesArgs p, int32_t fill_rows) {
   __shared__ int64_t part64[kPagesWaves];
   __shared__ int32_t part[kPagesWaves];
   __shared__ int32_t upto[kPagesThreads], first[kPagesThreads];
@@ -112,17 +181,17 @@ __global__ __launch_bounds__(kPagesThreads) void pages_step_kernel(PagesArgs p, 
     bool refuse = r.need > p.max_blocks;
     const int64_t want = refuse ? 0 : r.want;
     int64_t total;
-    const int64_t sum = tokens + block_scan(want, part64, total);
+    const int64_t sum = tokens + block_scan<kPagesWaves>(want, part64, total);
     tokens += total;
     refuse = refuse || (want > 0 && sum > p.max_tokens);
     if (refuse) atomicOr(&no[b >> 5], 1u << (b & 31));
     const int32_t gives = !refuse && r.held > r.need ? r.held - (int32_t) r.need : 0;
     int32_t back;
-    upto[tid] = block_scan(gives, part, back);
+    upto[tid] = block_scan<kPagesWaves>(gives, part, back);
     first[tid] = (int32_t) r.need;
     __syncthreads();
     for (int32_t i = tid; i < back; i += kPagesThreads) {
-      const int t = run_of(upto, i);
+      const int t = run_of<kPagesThreads>(upto, i);
       const int32_t at = top + i, block = first[t] + i - (t ? upto[t - 1] : 0);
       if (at < p.num_pages) p.free_pages[at] = p.table[(int64_t) (b0 + t) * p.table_stride + block];
     }
@@ -138,7 +207,7 @@ __global__ __launch_bounds__(kPagesThreads) void pages_step_kernel(PagesArgs p, 
     if (b < p.B) r = request_at(p, b);
     bool refuse = b < p.B && ((no[b >> 5] >> (b & 31)) & 1);
     int32_t takes = !refuse && r.need > r.held ? (int32_t) r.need - r.held : 0, total;
-    const int32_t sum = asked + block_scan(takes, part, total);
+    const int32_t sum = asked + block_scan<kPagesWaves>(takes, part, total);
     const int32_t before = asked;        // nobody ahead of one who gets pages was refused for want of them
     asked += total;
     if (takes > 0 && sum > top) {
@@ -146,15 +215,15 @@ __global__ __launch_bounds__(kPagesThreads) void pages_step_kernel(PagesArgs p, 
       takes = 0;
     }
     int32_t given;
-    upto[tid] = block_scan(takes, part, given);
+    upto[tid] = block_scan<kPagesWaves>(takes, part, given);
     first[tid] = r.held;
     const int32_t got = refuse ? 0 : (int32_t) r.want;
-    const int32_t end = starts + block_scan(got, part, total);
+    const int32_t end = starts + block_scan<kPagesWaves>(got, part, total);
     starts += total;
-    (void) block_scan(refuse && r.asks ? 1 : 0, part, total);
+    (void) block_scan<kPagesWaves>(refuse && r.asks ? 1 : 0, part, total);
     refused += total;
     for (int32_t i = tid; i < given; i += kPagesThreads) {
-      const int t = run_of(upto, i);
+      const int t = run_of<kPagesThreads>(upto, i);
       p.table[(int64_t) (b0 + t) * p.table_stride + first[t] + i - (t ? upto[t - 1] : 0)] = p.free_pages[top - 1 - before - i];
     }
     taken += given;
@@ -207,7 +276,10 @@ __global__ __launch_bounds__(kWriteThreads) void cache_write_kernel(WriteArgs w)
 
 hipError_t launch_pages_step(const PagesArgs &p, hipStream_t stream) {
   const bool fill = p.max_tokens <= kPagesFillRows;
-  pages_step_kernel<<<1, kPagesThreads, 0, stream>>>(p, fill);
+  // fewer waves meet sooner
+  if (p.B <= 256) pages_step_kernel<256><<<1, 256, 0, stream>>>(p, fill);
+  else if (p.B <= kPagesThreads) pages_step_kernel<kPagesThreads><<<1, kPagesThreads, 0, stream>>>(p, fill);
+  else pages_step_large_kernel<<<1, kPagesThreads, 0, stream>>>(p, fill);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || fill) return e;
   pages_slots_kernel<<<(uint32_t) ((p.max_tokens + 255) / 256), 256, 0, stream>>>(p);
