@@ -164,6 +164,21 @@ __device__ __forceinline__ int32_t request_ctx(const AttendArgs &a, int32_t b) {
   return a.lens ? min(max(fixed_at(a.lens, b), 0), a.max_ctx) : 0;
 }
 
+// 16 bytes a lane from memory to 1024 bytes of LDS in a row.  Written as instructions because the compiler waits for all such
+// loads in flight ahead of a transposing read of LDS (ds_read_b64_tr_b16), whatever buffer they fill; the kernels wait themselves
+// (wait_vm).  They bring nothing into registers, and what the compiler counts of its own loads stays right: it only waits longer.
+__device__ __forceinline__ uint32_t lds_address(const unsigned char *p) {
+  return (uint32_t) (uintptr_t) (const __attribute__((address_space(3))) unsigned char *) p;
+}
+__device__ __forceinline__ void bring(const char *base, uint32_t offset, const unsigned char *to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(offset), "s"(base), "s"(lds_address(to)) : "memory");
+}
+__device__ __forceinline__ void bring(const char *from, const unsigned char *to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :: "v"(from), "s"(lds_address(to)) : "memory");
+}
+
 // Brings ROWS keys or values of a unit, beginning at key k0, into LDS: loads of 16 bytes a lane, 1024 bytes of LDS in a row each,
 // dealt to NW waves.  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
 // multiple of 32) share a page, which the scalar unit looks up; 2: pages of any size.  Columns behind D get the row's first ones: keys are cleared there
@@ -228,15 +243,15 @@ struct Loader {
       if (whole) {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
-          put(from[j / kShared] + (j % kShared) * kStep * tok * (int) sizeof(T) + (VALUES ? voff[j % NV] : koff[j % NK]),
-              tile + (j * NW + wave) * 1024);
+          bring(from[j / kShared] + (j % kShared) * kStep * tok * (int) sizeof(T), VALUES ? voff[j % NV] : koff[j % NK],
+                tile + (j * NW + wave) * 1024);
       } else {
         // a unit's last tile, or a page outside the cache: zeros where there is no key
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
           const bool there = valid[j / kShared] && k0 + j * kStep + wave * S::RPI + lane / S::CH < u.k_hi;
           const char *at = from[j / kShared] + (j % kShared) * kStep * tok * (int) sizeof(T) + (VALUES ? voff[j % NV] : koff[j % NK]);
-          put(there ? at : reinterpret_cast<const char *>(&kZeros), tile + (j * NW + wave) * 1024);
+          bring(there ? at : reinterpret_cast<const char *>(&kZeros), tile + (j * NW + wave) * 1024);
         }
       }
     } else {
@@ -257,14 +272,10 @@ struct Loader {
         for (int i = 0; i < kAtOnce; ++i) {
           const int row = (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
           const char *at = base + ((int64_t) page[i] * page_stride + (int64_t) slot[i] * tok + chunk<VALUES>(row) * S::E) * (int) sizeof(T);
-          put(slot[i] >= 0 ? at : reinterpret_cast<const char *>(&kZeros), tile + ((j0 + i) * NW + wave) * 1024);
+          bring(slot[i] >= 0 ? at : reinterpret_cast<const char *>(&kZeros), tile + ((j0 + i) * NW + wave) * 1024);
         }
       }
     }
-  }
-  static __device__ __forceinline__ void put(const char *from, unsigned char *to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *) from,
-                                     (__attribute__((address_space(3))) void *) to, 16, 0, 0);
   }
 };
 
