@@ -182,7 +182,7 @@ __device__ __forceinline__ void bring(const char *from, const unsigned char *to)
 // Brings ROWS keys or values of a unit, beginning at key k0, into LDS: loads of 16 bytes a lane, 1024 bytes of LDS in a row each,
 // dealt to NW waves.  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
 // multiple of 32) share a page, which the scalar unit looks up; 2: pages of any size.  Columns behind D get the row's first ones: keys are cleared there
-// where they are used (scores), values make columns that nobody stores.
+// once they are in, values make columns that nobody stores.
 template <typename T, int DP, int ROWS, int NW, int PAGES>
 struct Loader {
   using S = Shape<T, DP>;
@@ -202,6 +202,14 @@ struct Loader {
     const int pos = lane % S::CH;
     const int ch = VALUES ? value_swap<S::RB, S::kBf16>(row, pos) : key_swap<S::RB>(row, pos);
     return ch * S::E < a.D ? ch : 0;
+  }
+  // Zeros in the columns behind D of the keys that this lane brought, once they are in.
+  __device__ __forceinline__ void clear_keys(unsigned char *tile) const {
+    if (a.D == DP) return;
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+      if (key_swap<S::RB>(j * kStep + wave * S::RPI + lane / S::CH, lane % S::CH) * S::E >= a.D)
+        *reinterpret_cast<u32x4 *>(tile + (j * NW + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
   }
   __device__ __forceinline__ Loader(const AttendArgs &a_, const Unit &u_, int lane_, int wave_)
       : a(a_), u(u_), lane(lane_), wave(wave_), table(PAGES ? a_.table + (int64_t) u_.b * a_.table_stride : nullptr) {
@@ -290,41 +298,34 @@ __device__ __forceinline__ void multiply(floatx16 &s, u32x4 x, u32x4 y) {
   }
 }
 
-// The 16-byte chunk of a key that a lane multiplies in step i.  CUT: there is nothing behind D.
-template <typename T, int DP, bool CUT>
-__device__ __forceinline__ u32x4 key_chunk(const unsigned char *lk, int base, int lane, int i, int32_t D) {
-  using S = Shape<T, DP>;
-  const int ch = 2 * i + (lane >> 5);
-  const u32x4 x = *reinterpret_cast<const u32x4 *>(lk + key_at<S::RB>(base + (lane & 31), ch));
-  if constexpr (CUT) return ch * S::E < D ? x : u32x4{0, 0, 0, 0};
-  return x;
+// The 16-byte chunk of a key that a lane multiplies in step i: key `base` + lane % 32 of the tile.
+template <int RB>
+__device__ __forceinline__ u32x4 key_chunk(const unsigned char *lk, int base, int lane, int i) {
+  return *reinterpret_cast<const u32x4 *>(lk + key_at<RB>(base + (lane & 31), 2 * i + (lane >> 5)));
 }
 
-// Scores of 32 keys, the first at row `base` of the tile: register 4 j + i is key base + 8 j + 4 half + i.  Queries in
+// Scores of KB blocks of 32 keys of a tile: register 4 j + i of a block is its key 8 j + 4 half + i.  Queries in
 // registers, or of RB blocks of rows in LDS, laid out as keys are.
-template <typename T, int DP, bool CUT, int KB>
-__device__ __forceinline__ void scores(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], int32_t D,
-                                       floatx16 (&s)[KB]) {
+template <typename T, int DP, int KB>
+__device__ __forceinline__ void scores(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[KB]) {
   using S = Shape<T, DP>;
 #pragma unroll
   for (int k = 0; k < KB; ++k) {
     s[k] = floatx16{};
 #pragma unroll
-    for (int i = 0; i < S::NQ; ++i) multiply<S::kBf16>(s[k], key_chunk<T, DP, CUT>(lk, 32 * k, lane, i, D), qf[i]);
+    for (int i = 0; i < S::NQ; ++i) multiply<S::kBf16>(s[k], key_chunk<S::RB>(lk, 32 * k, lane, i), qf[i]);
   }
 }
-template <typename T, int DP, bool CUT, int RB>
-__device__ __forceinline__ void scores(const unsigned char *lk, const unsigned char *lq, int lane, int32_t D, floatx16 (&s)[RB]) {
+template <typename T, int DP, int RB>
+__device__ __forceinline__ void scores(const unsigned char *lk, const unsigned char *lq, int lane, floatx16 (&s)[RB]) {
   using S = Shape<T, DP>;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) s[rb] = floatx16{};
 #pragma unroll
   for (int i = 0; i < S::NQ; ++i) {
-    const u32x4 kf = key_chunk<T, DP, CUT>(lk, 0, lane, i, D);
+    const u32x4 kf = key_chunk<S::RB>(lk, 0, lane, i);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-      multiply<S::kBf16>(s[rb], kf,
-                         *reinterpret_cast<const u32x4 *>(lq + key_at<S::RB>(rb * 32 + (lane & 31), 2 * i + (lane >> 5))));
+    for (int rb = 0; rb < RB; ++rb) multiply<S::kBf16>(s[rb], kf, key_chunk<S::RB>(lq, rb * 32, lane, i));
     if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);         // not all operands in registers at a time
   }
 }
@@ -338,27 +339,36 @@ __device__ __forceinline__ void hide(floatx16 &s, int32_t key0, int half, int32_
   }
 }
 
-// Scores of KB blocks of keys to weights 2^(c s - ref), their sum added; ref follows the rows' maxima where one runs more than
-// kLag ahead of it (the weights then stay below 2^kLag, and sums and outputs are rarely rescaled).
-template <int KB, int NO>
-__device__ __forceinline__ void weigh(floatx16 (&s)[KB], float c, float &ref, float &sum, floatx16 (&o)[NO]) {
-  float m[2] = {-INFINITY, -INFINITY};
+// The largest of a row's scores of KB blocks of keys, in log2 units.
+template <int KB>
+__device__ __forceinline__ float row_max(const floatx16 (&s)[KB], float c) {
+  float m[2] = {s[0][0], s[0][1]};
 #pragma unroll
   for (int k = 0; k < KB; ++k)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) m[r & 1] = fmaxf(m[r & 1], s[k][r]);
-  const float mx = pair_max(fmaxf(m[0], m[1])) * c;
-  if (__builtin_amdgcn_ballot_w64(mx > ref + kLag) != 0) {
-    const float now = fmaxf(ref, mx);
-    const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
-    ref = now;
-    sum *= f;
+    for (int r = k ? 0 : 2; r < 16; ++r) m[r & 1] = fmaxf(m[r & 1], s[k][r]);
+  return pair_max(fmaxf(m[0], m[1])) * c;
+}
+
+// The rows' reference maxima follow the maxima where one runs more than kLag ahead (weights stay below 2^kLag, and sums
+// and outputs are rarely rescaled).
+template <int NO>
+__device__ __forceinline__ void follow(float mx, float &ref, float &sum, floatx16 (&o)[NO]) {
+  if (__builtin_amdgcn_ballot_w64(mx > ref + kLag) == 0) return;
+  const float now = fmaxf(ref, mx);
+  const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
+  ref = now;
+  sum *= f;
 #pragma unroll
-    for (int n = 0; n < NO; ++n)
+  for (int n = 0; n < NO; ++n)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[n][r] *= f;
-  }
-  const float minus = ref == -INFINITY ? 0.f : -ref;
+    for (int r = 0; r < 16; ++r) o[n][r] *= f;
+}
+
+// Scores to weights 2^(c s - ref), and their sum.
+__device__ __forceinline__ float minus_ref(float ref) { return ref == -INFINITY ? 0.f : -ref; }
+template <int KB>
+__device__ __forceinline__ void to_weights(floatx16 (&s)[KB], float c, float minus, float &sum) {
   float z[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < KB; ++k)
@@ -368,6 +378,29 @@ __device__ __forceinline__ void weigh(floatx16 (&s)[KB], float c, float &ref, fl
       z[r & 3] += s[k][r];
     }
   sum += (z[0] + z[1]) + (z[2] + z[3]);
+}
+
+// Nothing moves across: the order of instructions around it is the one written.
+__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
+
+// scores in steps of one operand of keys, read kAhead steps ahead.
+template <typename T, int DP, int KB>
+__device__ __forceinline__ void scores_in_steps(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[KB]) {
+  using S = Shape<T, DP>;
+  constexpr int kAhead = 3, kSteps = KB * S::NQ;
+  u32x4 kf[kAhead + 1];
+  auto read = [&](int i) { kf[i % (kAhead + 1)] = key_chunk<S::RB>(lk, 32 * (i / S::NQ), lane, i % S::NQ); };
+#pragma unroll
+  for (int i = 0; i < kAhead && i < kSteps; ++i) read(i);
+#pragma unroll
+  for (int k = 0; k < KB; ++k) s[k] = floatx16{};
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    pin();
+    if (i + kAhead < kSteps) read(i + kAhead);
+    multiply<S::kBf16>(s[i / S::NQ], kf[i % (kAhead + 1)], qf[i % S::NQ]);
+  }
+  pin();
 }
 
 // Operand of the product of weights and values: the weights of one 16 keys (bf16) or of two (float32) in a lane.
@@ -427,6 +460,47 @@ __device__ __forceinline__ void add_values(const unsigned char *lv, int base, in
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) o[rb][m] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[rb][r], o[rb][m], 0, 0, 0);
       }
+  }
+}
+
+// The same for KB blocks of 32 keys and one block of rows, in steps with the operands read ahead.
+template <typename T, int DP, int KB>
+__device__ __forceinline__ void add_values_in_steps(const unsigned char *lv, int lane, const floatx16 (&p)[KB],
+                                                    floatx16 (&o)[Shape<T, DP>::NO]) {
+  using S = Shape<T, DP>;
+  if constexpr (S::kBf16) {
+    constexpr int kAhead = 3, kSteps = KB * 2 * S::NO;
+    shortx8 vf[kAhead + 1];
+    bf16x8 pf[2];
+    auto read = [&](int i) { vf[i % (kAhead + 1)] = values_of<S::RB>(lv, i / S::NO * 16, lane, i % S::NO); };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) read(i);
+    pf[0] = weights_of(p[0], 0);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int c = i / S::NO, m = i % S::NO;
+      pin();
+      if (i + kAhead < kSteps) read(i + kAhead);
+      if (m == 0 && c + 1 < 2 * KB) pf[(c + 1) & 1] = weights_of(p[(c + 1) / 2], (c + 1) & 1);
+      o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[i % (kAhead + 1)]), pf[c & 1], o[m], 0, 0, 0);
+    }
+    pin();
+  } else {
+    constexpr int kSteps = KB * 16;
+    float x[2][S::NO];
+    auto read = [&](int i) {
+#pragma unroll
+      for (int m = 0; m < S::NO; ++m) x[i & 1][m] = value_of<S::RB>(lv, i / 16 * 32, lane, i % 16, m);
+    };
+    read(0);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      pin();
+      if (i + 1 < kSteps) read(i + 1);
+#pragma unroll
+      for (int m = 0; m < S::NO; ++m) o[m] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i & 1][m], p[i / 16][i % 16], o[m], 0, 0, 0);
+    }
+    pin();
   }
 }
 
@@ -782,27 +856,24 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
   const int32_t begin = k0;
   auto at_edge = [&](int32_t k) { return k + W::TK > u.min_hi || k < u.max_lo; };
   for (; k0 < end; k0 += W::TK) {
-    wait_vm<0>();                       // this wave's part of the tile is in; past the barrier everyone's is
-    bare_barrier();
+    wait_vm<0>();                       // this wave's part of the tile is in;
+    loader.clear_keys(cur);
+    bare_barrier();                     // now everyone's is, and nobody reads the tile before any more
     if (k0 + W::TK < end) load(k0 + W::TK, nxt);
     if (at_edge(k0)) {
       if (clear_odd_values<S::kBf16>(cur + W::kTile, W::kTile, tid, kAttendThreads)) *odd = 1;
       bare_barrier();
     }
-    if (k0 <= pos_last) {
-      const unsigned char *lk = cur, *lv = cur + W::kTile;
+    if (k0 <= pos_last) {               // else no row of this wave sees anything of it
       floatx16 s[W::KB];
-      if (a.D == DP) scores<T, DP, false>(lk, lane, qf, DP, s);
-      else scores<T, DP, true>(lk, lane, qf, a.D, s);
+      scores_in_steps<T, DP, W::KB>(cur, lane, qf, s);
       if (k0 + W::TK - 1 > pos_first || k0 < u.max_lo) {
 #pragma unroll
         for (int k = 0; k < W::KB; ++k) hide(s[k], k0 + 32 * k, half, w.pos, lo);
       }
-      weigh<W::KB, S::NO>(s, a.c, ref, sum, o);
-#pragma unroll
-      for (int k = 0; k < W::KB; ++k)
-        add_values<T, DP, 1>(lv, 32 * k, lane, reinterpret_cast<const floatx16(&)[1]>(s[k]),
-                             reinterpret_cast<floatx16(&)[1][S::NO]>(o));
+      follow<S::NO>(row_max<W::KB>(s, a.c), ref, sum, o);
+      to_weights<W::KB>(s, a.c, minus_ref(ref), sum);
+      add_values_in_steps<T, DP, W::KB>(cur + W::kTile, lane, s, o);
     }
     unsigned char *x = cur;
     cur = nxt;
@@ -950,14 +1021,13 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
     floatx16 s[RB];
     if (now) {
       wait_vm<NI>();                    // keys are in, values may be on their way
+      loader.clear_keys(lk);
       if constexpr (RB == 1) {
-        if (a.D == DP) scores<T, DP, false>(lk, lane, qf, DP, s);
-        else scores<T, DP, true>(lk, lane, qf, a.D, s);
+        scores<T, DP, 1>(lk, lane, qf, reinterpret_cast<floatx16(&)[1]>(s[0]));
       } else {
         int away = (int) (lq - lk);
         asm volatile("" : "+s"(away));  // an addition a read, instead of as many addresses in registers
-        if (a.D == DP) scores<T, DP, false>(lk, lk + away, lane, DP, s);
-        else scores<T, DP, true>(lk, lk + away, lane, a.D, s);
+        scores<T, DP, RB>(lk, lk + away, lane, s);
       }
       wait_lds();
     }
@@ -967,7 +1037,9 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         if (edge) hide(s[rb], k, half, pos[rb], a.window > 0 ? pos[rb] - a.window : -1);
-        weigh<1, S::NO>(reinterpret_cast<floatx16(&)[1]>(s[rb]), a.c, ref[rb], sum[rb], o[rb]);
+        floatx16(&one)[1] = reinterpret_cast<floatx16(&)[1]>(s[rb]);
+        follow<S::NO>(row_max<1>(one, a.c), ref[rb], sum[rb], o[rb]);
+        to_weights<1>(one, a.c, minus_ref(ref[rb]), sum[rb]);
       }
       if (more) wait_vm<NI>();
       else wait_vm<0>();
