@@ -36,7 +36,8 @@ constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = kAttendWaves * kWave;
 constexpr int kThickRows = 32 * kAttendWaves;
 constexpr int kThinKeys = 32 * kAttendWaves;      // keys a turn of the four waves takes
-constexpr int kThinLeast = 1, kThickLeast = 4;     // tiles of a workgroup, at least
+constexpr int kThinLeast = 1, kThickLeast = 5;     // length of a workgroup's run, at least (see Run)
+constexpr int kThinCost = 1, kThickCost = 1;
 constexpr int kJoinThreads = 256;
 constexpr float kLag = 8.f;        // how far (in powers of two) a maximum may run ahead of the one in use
 
@@ -224,64 +225,67 @@ struct Loader {
       voff[j] = (uint32_t) (row_in * (int32_t) a.v_tok + chunk<true>(j * kStep + wave * S::RPI + row_in) * S::E) * (uint32_t) sizeof(T);
   }
 
+  // Pages of the keys from k0 on, asked for ahead of their use: of 16 keys each (PAGES 1), of each load of this lane (PAGES 2).
+  static constexpr int kShared = kStep < 16 ? 16 / kStep : 1;          // loads of a wave from the same 16 keys
+  static constexpr int NP = PAGES == 2 ? NI : NI / kShared;
+  struct Pages {
+    int32_t page[NP];
+  };
+  __device__ __forceinline__ int32_t key_of(int32_t k0, int i) const {
+    return PAGES == 2 ? k0 + i * kStep + wave * S::RPI + lane / S::CH : k0 + i * kShared * kStep + wave * S::RPI;
+  }
+  __device__ __forceinline__ Pages look_up(int32_t k0) const {
+    Pages p;
+#pragma unroll
+    for (int i = 0; i < NP && PAGES; ++i) {
+      uint32_t block, slot;
+      split_by((uint32_t) key_of(k0, i), (uint32_t) a.page_size, a.magic_page, block, slot);
+      p.page[i] = fixed_at(table, min(block, (uint32_t) a.max_blocks - 1));
+    }
+    return p;
+  }
+
   template <bool VALUES>
-  __device__ __forceinline__ void load(int32_t k0, unsigned char *tile) const {
+  __device__ __forceinline__ void load(int32_t k0, const Pages &p, unsigned char *tile) const {
     const char *base = VALUES ? vb : kb;
-    const int64_t tok = VALUES ? a.v_tok : a.k_tok, page_stride = VALUES ? a.v_page : a.k_page;
-    if constexpr (PAGES < 2) {
-      constexpr int kShared = kStep < 16 ? 16 / kStep : 1;      // loads of this wave from the same 16 keys
-      const char *from[NI / kShared];
-      bool valid[NI / kShared], whole = k0 + ROWS <= u.k_hi;
+    // of a cache keys and values have the same strides
+    const int64_t tok = VALUES && !PAGES ? a.v_tok : a.k_tok;
+    int64_t at[NP];
+    bool valid[NP], whole = PAGES < 2 && k0 + ROWS <= u.k_hi;
 #pragma unroll
-      for (int j = 0; j < NI / kShared; ++j) {
-        const int32_t key = k0 + j * kShared * kStep + wave * S::RPI;
-        if constexpr (PAGES) {
-          uint32_t block, slot;
-          split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
-          valid[j] = block < (uint32_t) a.max_blocks && key < u.k_hi;
-          const int32_t page = valid[j] ? fixed_at(table, block) : 0;
-          valid[j] = valid[j] && (uint32_t) page < (uint32_t) a.num_pages;
-          whole = whole && valid[j];
-          from[j] = base + ((int64_t) page * page_stride + (int64_t) slot * tok) * (int) sizeof(T);
-        } else {
-          valid[j] = true;
-          from[j] = base + (int64_t) (u.first + key) * tok * (int) sizeof(T);
-        }
-      }
-      if (whole) {
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-          bring(from[j / kShared] + (j % kShared) * kStep * tok * (int) sizeof(T), VALUES ? voff[j % NV] : koff[j % NK],
-                tile + (j * NW + wave) * 1024);
+    for (int i = 0; i < NP; ++i) {
+      const int32_t key = key_of(k0, i);
+      if constexpr (PAGES) {
+        uint32_t block, slot;
+        split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
+        valid[i] = key < u.k_hi && block < (uint32_t) a.max_blocks && (uint32_t) p.page[i] < (uint32_t) a.num_pages;
+        whole = whole && valid[i];
+        at[i] = (int64_t) p.page[i] * a.k_page + (int64_t) slot * tok;
       } else {
-        // a unit's last tile, or a page outside the cache: zeros where there is no key
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          const bool there = valid[j / kShared] && k0 + j * kStep + wave * S::RPI + lane / S::CH < u.k_hi;
-          const char *at = from[j / kShared] + (j % kShared) * kStep * tok * (int) sizeof(T) + (VALUES ? voff[j % NV] : koff[j % NK]);
-          bring(there ? at : reinterpret_cast<const char *>(&kZeros), tile + (j * NW + wave) * 1024);
-        }
+        valid[i] = key < u.k_hi;
+        at[i] = (int64_t) (u.first + key) * tok;
       }
+    }
+    if (whole) {
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+        bring(base + (at[j / kShared % NP] + (j % kShared) * kStep * tok) * (int) sizeof(T), VALUES ? voff[j % NV] : koff[j % NK],
+              tile + (j * NW + wave) * 1024);
     } else {
-      constexpr int kAtOnce = NI < 8 ? NI : 8;
-#pragma unroll 1
-      for (int j0 = 0; j0 < NI; j0 += kAtOnce) {
-        int32_t page[kAtOnce], slot[kAtOnce];
+      // a unit's last tile, pages of odd sizes or outside the cache: zeros where there is no key
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          const int32_t key = k0 + (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
-          uint32_t block, at;
-          split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, at);
-          const bool there = key < u.k_hi && block < (uint32_t) a.max_blocks;
-          page[i] = fixed_at(table, there ? block : 0);
-          slot[i] = there && (uint32_t) page[i] < (uint32_t) a.num_pages ? (int32_t) at : -1;
+      for (int j = 0; j < NI; ++j) {
+        const int row = j * kStep + wave * S::RPI + lane / S::CH;
+        const char *from;
+        bool there;
+        if constexpr (PAGES == 2) {
+          there = valid[j];
+          from = base + (at[j] + chunk<VALUES>(row) * S::E) * (int) sizeof(T);
+        } else {
+          there = valid[j / kShared] && k0 + row < u.k_hi;
+          from = base + (at[j / kShared] + (j % kShared) * kStep * tok) * (int) sizeof(T) + (VALUES ? voff[j % NV] : koff[j % NK]);
         }
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          const int row = (j0 + i) * kStep + wave * S::RPI + lane / S::CH;
-          const char *at = base + ((int64_t) page[i] * page_stride + (int64_t) slot[i] * tok + chunk<VALUES>(row) * S::E) * (int) sizeof(T);
-          bring(slot[i] >= 0 ? at : reinterpret_cast<const char *>(&kZeros), tile + ((j0 + i) * NW + wave) * 1024);
-        }
+        bring(there ? from : reinterpret_cast<const char *>(&kZeros), tile + (j * NW + wave) * 1024);
       }
     }
   }
@@ -652,13 +656,13 @@ __device__ __forceinline__ int32_t unit_tiles(const AttendArgs &a, Unit &u) {
   return (u.k_hi - u.k_lo + TK - 1) / TK;
 }
 
-// The tiles of all units (requests, their shared heads, their row blocks, in this order) are cut into `runs` equal runs, one a
-// workgroup, the first `longer` of them a tile longer than `each`.
+// All units (requests, their shared heads, their row blocks, in this order) in a row, COST for what a unit costs beside its tiles
+// and then 1 for each of them, are cut into `runs` runs of a length, one a workgroup; the first `longer` are one longer than `each`.
 struct Run {
-  int32_t runs, longer;
-  int64_t each, left, end;
+  int32_t runs, longer, index;
+  int64_t each, left;
   __device__ __forceinline__ int64_t begin(int32_t i) const { return each * i + min(i, longer); }
-  // the runs that begin ahead of tile x (which lies in one of them, or behind all)
+  // the runs that begin ahead of x (which lies in one of them, or behind all)
   __device__ __forceinline__ int32_t ahead_of(int64_t x) const {
     int32_t lo = 0, hi = runs;
     while (lo < hi) {                   // first run that begins at x or behind it
@@ -670,96 +674,127 @@ struct Run {
   }
 };
 
-// Finds run `index` of at most `count` runs of at least LEAST tiles (but for the last): its first unit and the tile in it.
-// Every workgroup adds the requests up by itself: for 64 of them that takes a microsecond, less than a launch ahead would.
-template <int R, int TK, int LEAST>
-__device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t index, int32_t count, unsigned char *lds, Unit &u,
-                                        int32_t &tile) {
-  int64_t *wave_sum = reinterpret_cast<int64_t *>(lds);
-  int32_t *found = reinterpret_cast<int32_t *>(wave_sum + kAttendWaves);
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  const int32_t each = (a.B + kAttendThreads - 1) / kAttendThreads, b0 = min(tid * each, a.B), b1 = min(b0 + each, a.B);
-  auto request = [&](int32_t b, Unit &v) {
-    v.b = b;
-    v.rows = request_tokens(a, b, v.first) * a.G;
-    v.ctx = request_ctx(a, b);
+// Finds this workgroup's run, of `count` at most, LEAST long at least (but for the last): its first unit and how far into it.
+// Every workgroup adds the requests up by itself, a quarter of them a wave, a request a lane or (with many row blocks) a row block
+// a lane: for 64 requests that takes two microseconds, less than a launch ahead would.  Lengths are whole numbers below 2^53 in
+// double, whose running sums go through DPP.
+template <int R, int TK, int LEAST, int COST>
+__device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsigned char *lds, Unit &u, int64_t &into) {
+  double *sums = reinterpret_cast<double *>(lds);
+  int32_t *found = reinterpret_cast<int32_t *>(sums + kAttendWaves);
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int32_t quarter = (a.B + kAttendWaves - 1) / kAttendWaves, b_lo = min(wave * quarter, a.B), b_hi = min(b_lo + quarter, a.B);
+  // running sum of the lengths of requests b0 .. b0 + lane, all shared heads
+  auto lengths = [&](int32_t b0, Unit &v, double &one) -> double {
+    v.b = b0 + lane;
+    v.rows = v.ctx = 0;
+    if (v.b < b_hi) {
+      v.rows = request_tokens(a, v.b, v.first) * a.G;
+      v.ctx = request_ctx(a, v.b);
+    }
+    v.r0 = 0;
+    one = v.rows > 0 && v.rows <= R ? unit_tiles<R, TK>(a, v) + COST : 0;
+    for (uint64_t many = __builtin_amdgcn_ballot_w64(v.rows > R); many; many &= many - 1) {
+      const int l = __ffsll((long long) many) - 1;
+      Unit x;
+      x.rows = read_lane(v.rows, l);
+      x.ctx = read_lane(v.ctx, l);
+      double all = 0;
+      for (int64_t r0 = (int64_t) lane * R; r0 < x.rows; r0 += kWave * R) {
+        x.r0 = (int32_t) r0;
+        all += unit_tiles<R, TK>(a, x) + COST;
+      }
+      all = wave_sum(all);
+      if (lane == l) one = all;
+    }
+    return wave_scan(one * a.heads_kv);
   };
-  auto tiles_of = [&](int32_t b) -> int64_t {        // of one shared head
-    Unit v;
-    request(b, v);
-    int64_t sum = 0;
-    for (v.r0 = 0; v.r0 < v.rows; v.r0 += R) sum += unit_tiles<R, TK>(a, v);
-    return sum;
-  };
-  int64_t mine = 0;
-  for (int32_t b = b0; b < b1; ++b) mine += tiles_of(b);
-  mine *= a.heads_kv;
-  int64_t upto = mine;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int64_t x = __shfl_up(upto, d);
-    if (lane >= d) upto += x;
+  Unit v;
+  double one, upto = 0, mine = 0;
+  for (int32_t b0 = b_lo; b0 < b_hi; b0 += kWave) {
+    upto = lengths(b0, v, one);
+    mine += read_lane(upto, kWave - 1);
   }
-  if (lane == kWave - 1) wave_sum[wave] = upto;
-  __syncthreads();
+  if (lane == 0) sums[wave] = mine;
+  bare_barrier();
   Run run;
-  int64_t total = 0;
+  double sum = 0, before = 0;
 #pragma unroll
   for (int w = 0; w < kAttendWaves; ++w) {
-    const int64_t x = wave_sum[w];
-    if (w < wave) upto += x;
-    total += x;
+    const double x = sums[w];
+    if (w < wave) before += x;
+    sum += x;
   }
-  total = scalar(total);
+  const int64_t total = scalar((int64_t) sum);
   run.runs = (int32_t) min((int64_t) count, (total + LEAST - 1) / LEAST);
+  // An XCD (every eighth workgroup) takes runs that follow each other: those of a shared head find its keys in its L2.
+  const int32_t eighth = (run.runs + 7) / 8;
+  run.index = (int32_t) blockIdx.x / 8 < eighth ? (int32_t) (blockIdx.x % 8) * eighth + (int32_t) blockIdx.x / 8 : run.runs;
   run.left = 0;
-  if (index >= run.runs) return run;
+  if (run.index >= run.runs) return run;
   // a quotient of numbers below 2^53, off by one at most in double
   run.each = scalar((int64_t) ((double) total / (double) run.runs));
   if (run.each * run.runs > total) --run.each;
   if (total - run.each * run.runs >= run.runs) ++run.each;
   run.longer = (int32_t) (total - run.each * run.runs);
-  const int64_t begin = run.begin(index);
-  run.end = run.begin(index + 1);
-  run.left = run.end - begin;
-  if (upto - mine <= begin && begin < upto) {
-    int64_t ahead = begin - (upto - mine);
-    for (int32_t b = b0; b < b1; ++b) {
-      const int64_t one = tiles_of(b);
-      if (ahead >= one * a.heads_kv) {
-        ahead -= one * a.heads_kv;
+  const int64_t begin = run.begin(run.index);
+  run.left = run.begin(run.index + 1) - begin;
+  double ahead = (double) begin - before;
+  if (0 <= ahead && ahead < mine) {
+    for (int32_t b0 = b_lo; b0 < b_hi; b0 += kWave) {
+      if (quarter > kWave) upto = lengths(b0, v, one);
+      const uint64_t past = __builtin_amdgcn_ballot_w64(upto > ahead);
+      if (!past) {
+        ahead -= read_lane(upto, kWave - 1);
         continue;
       }
-      Unit v;
-      request(b, v);
-      int32_t head = (int32_t) ((double) ahead / (double) one);      // below 2^53: off by one at most
-      if (head * one > ahead) --head;
-      if (ahead - head * one >= one) ++head;
-      ahead -= head * one;
-      for (v.r0 = 0; v.r0 < v.rows; v.r0 += R) {
-        const int32_t t = unit_tiles<R, TK>(a, v);
-        if (ahead < t) break;
-        ahead -= t;
+      const int l = __ffsll((long long) past) - 1;
+      const double length = read_lane(one, l);
+      ahead -= read_lane(upto, l) - length * a.heads_kv;
+      int32_t head = (int32_t) (ahead / length);      // off by one at most
+      if (head * length > ahead) --head;
+      if (ahead - head * length >= length) ++head;
+      ahead -= head * length;
+      Unit x;
+      x.b = b0 + l;
+      x.rows = read_lane(v.rows, l);
+      x.ctx = read_lane(v.ctx, l);
+      x.first = read_lane(v.first, l);
+      int32_t r0 = 0;
+      for (int64_t c0 = 0; c0 < x.rows && x.rows > R; c0 += kWave * R) {
+        const int64_t mine_r0 = c0 + (int64_t) lane * R;
+        x.r0 = (int32_t) mine_r0;
+        const double t = mine_r0 < x.rows ? unit_tiles<R, TK>(a, x) + COST : 0, blocks = wave_scan(t);
+        const uint64_t in = __builtin_amdgcn_ballot_w64(blocks > ahead);
+        if (in) {
+          const int k = __ffsll((long long) in) - 1;
+          ahead -= read_lane(blocks - t, k);
+          r0 = (int32_t) c0 + k * R;
+          break;
+        }
+        ahead -= read_lane(blocks, kWave - 1);
       }
-      found[0] = b;
-      found[1] = head;
-      found[2] = v.r0;
-      found[3] = (int32_t) ahead;
-      found[4] = v.rows;
-      found[5] = v.first;
-      found[6] = v.ctx;
+      if (lane == 0) {
+        found[0] = x.b;
+        found[1] = head;
+        found[2] = r0;
+        found[3] = (int32_t) ahead;
+        found[4] = x.rows;
+        found[5] = x.first;
+        found[6] = x.ctx;
+      }
       break;
     }
   }
-  __syncthreads();
-  u.b = __builtin_amdgcn_readfirstlane(found[0]);
-  u.head = __builtin_amdgcn_readfirstlane(found[1]);
-  u.r0 = __builtin_amdgcn_readfirstlane(found[2]);
-  tile = __builtin_amdgcn_readfirstlane(found[3]);
+  bare_barrier();
+  u.b = found[0];
+  u.head = found[1];
+  u.r0 = found[2];
+  into = scalar(found[3]);
   u.rows = found[4];
   u.first = found[5];
   u.ctx = found[6];
-  __syncthreads();                      // the tiles of the first piece come here
+  bare_barrier();                       // the tiles of the first piece come here
   return run;
 }
 
@@ -780,32 +815,36 @@ __device__ __forceinline__ void next_unit(const AttendArgs &a, Unit &u) {
 
 // Calls work(unit, first tile, tiles, part) for every unit or piece of one in this workgroup's run; part: NULL where the unit is
 // whole.  A workgroup has two places for parts: 1 for the unit that it begins and does not finish, 0 for one that another began.
-template <int DP, int R, int TK, int LEAST, typename Work>
-__device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *lds, Join *join, Part<DP, R> *parts,
-                                            Work work) {
-  const int32_t index = (int32_t) blockIdx.x, count = (int32_t) gridDim.x;
+template <int DP, int R, int TK, int LEAST, int COST, typename Work>
+__device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *lds, Join *join, Part<DP, R> *parts, Work work) {
   Unit u;
-  int32_t tile = 0;
-  Run run = find_run<R, TK, LEAST>(a, index, count, lds, u, tile);
+  int64_t into = 0;
+  Run run = find_run<R, TK, LEAST, COST>(a, (int32_t) gridDim.x, lds, u, into);
   Join j{0, 0, 0, 0, 0};
   while (run.left > 0) {
     u = scalar(u);
     const int32_t all = scalar(unit_tiles<R, TK>(a, u));
-    const int32_t tiles = (int32_t) min((int64_t) (all - tile), run.left);
-    Part<DP, R> *part = tiles == all ? nullptr : parts + 2 * (int64_t) index + (tile == 0);
-    if (part && tile == 0) {
-      j.parts = run.ahead_of(run.end + all - tiles) - index;       // this one and those that begin ahead of the unit's end
-      j.head = u.head;
-      j.r0 = u.r0;
-      j.rows = u.rows;
-      j.first = u.first;
+    const int64_t until = min((int64_t) all + COST, into + run.left);       // in the unit's length
+    const int32_t tile = into > COST ? (int32_t) into - COST : 0, tiles = until > COST ? (int32_t) until - COST - tile : 0;
+    run.left -= until - into;
+    if (tiles > 0) {
+      Part<DP, R> *part = tiles == all ? nullptr : parts + 2 * (int64_t) run.index + (tile == 0);
+      if (part && tile == 0) {
+        // this run and those that begin ahead of the unit's end
+        j.parts = run.ahead_of(run.begin(run.index + 1) - run.left + all + COST - until) - run.index;
+        j.head = u.head;
+        j.r0 = u.r0;
+        j.rows = u.rows;
+        j.first = u.first;
+      }
+      work(u, tile, tiles, part);
     }
-    work(u, tile, tiles, part);
-    run.left -= tiles;
-    tile = 0;
+    into = 0;
     if (run.left > 0) next_unit<R>(a, u);
   }
-  if (threadIdx.x == 0) join[index] = j;
+  if (threadIdx.x != 0) return;
+  if (run.index < run.runs) join[run.index] = j;
+  if ((int32_t) blockIdx.x >= run.runs) join[blockIdx.x] = Join{0, 0, 0, 0, 0};
 }
 
 // ---- 128 rows a workgroup ----------------------------------------------------------------------------------------------
@@ -832,9 +871,11 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
   int32_t k0 = u.k_lo + tile * W::TK;
   const int32_t end = min(u.k_hi, k0 + tiles * W::TK);
   unsigned char *cur = lds, *nxt = lds + 2 * W::kTile;
+  auto pages = loader.look_up(k0);      // of the tile that is brought next
   auto load = [&](int32_t k, unsigned char *to) {
-    loader.template load<false>(k, to);
-    loader.template load<true>(k, to + W::kTile);
+    loader.template load<false>(k, pages, to);
+    loader.template load<true>(k, pages, to + W::kTile);
+    pages = loader.look_up(k + W::TK);
   };
   bare_barrier();                       // nobody reads the piece before any more
   load(k0, cur);
@@ -894,7 +935,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_thick_kernel(AttendA
                                                                          Part<DP, kThickRows> *parts) {
   __shared__ __align__(16) unsigned char lds[Thick<T, DP>::kLds];
   __shared__ int odd;
-  work_on_run<DP, kThickRows, Thick<T, DP>::TK, kThickLeast>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
+  work_on_run<DP, kThickRows, Thick<T, DP>::TK, kThickLeast, kThickCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
     thick_piece<T, DP, PAGES>(a, u, tile, tiles, lds, &odd, part);
   });
 }
@@ -1013,6 +1054,7 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   const int32_t begin = k0;
   auto at_edge = [&](int32_t k) { return k + 32 > u.min_hi || k < u.max_lo; };
   bool odd = false;
+  auto pages = loader.look_up(k0);      // of the keys that are brought next
   // A turn works on keys k0 - kThinKeys and brings keys k0 behind it: one place in the code for each load.
   for (bool now = false;; k0 += kThinKeys, now = true) {
     const bool more = k0 < end;
@@ -1031,7 +1073,7 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
       }
       wait_lds();
     }
-    if (more) loader.template load<false>(k0, lk);
+    if (more) loader.template load<false>(k0, pages, lk);
     if (now) {
       const bool edge = at_edge(k);
 #pragma unroll
@@ -1051,7 +1093,8 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
       wait_lds();
     }
     if (!more) break;
-    loader.template load<true>(k0, lv);
+    loader.template load<true>(k0, pages, lv);
+    pages = loader.look_up(k0 + kThinKeys);
   }
   if (odd) {
     for (k0 = begin; k0 < end; k0 += kThinKeys) {
@@ -1125,7 +1168,7 @@ __global__ __launch_bounds__(kAttendThreads, (Thin<T, DP, RB>::kRuns / 256)) voi
                                                                                                   Join *join,
                                                                                                   Part<DP, 32 * RB> *parts) {
   __shared__ __align__(16) unsigned char lds[Thin<T, DP, RB>::kLds];
-  work_on_run<DP, 32 * RB, kThinKeys, kThinLeast>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32 * RB> *part) {
+  work_on_run<DP, 32 * RB, kThinKeys, kThinLeast, kThinCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32 * RB> *part) {
     thin_piece<T, DP, RB, PAGES>(a, u, tile, tiles, lds, part);
   });
 }
@@ -1217,7 +1260,7 @@ hipError_t split_launch(Kernel kernel, int32_t runs, const AttendArgs &a, void *
   kernel<<<runs, kAttendThreads, 0, stream>>>(a, join, parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  attend_join_kernel<T, DP, R><<<dim3(runs, R / 4), kJoinThreads, 0, stream>>>(a, join, parts);
+  attend_join_kernel<T, DP, R><<<dim3(runs, R == 128 ? 8 : R / 4), kJoinThreads, 0, stream>>>(a, join, parts);
   return hipGetLastError();
 }
 
