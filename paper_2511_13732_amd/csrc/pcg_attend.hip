@@ -36,6 +36,7 @@ constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = kAttendWaves * kWave;
 constexpr int kThickRows = 32 * kAttendWaves;
 constexpr int kThinKeys = 32 * kAttendWaves;      // keys a turn of the four waves takes
+constexpr int kCUs = 256;
 constexpr int kThinLeast = 1, kThickLeast = 5;     // length of a workgroup's run, at least (see Run)
 constexpr int kThinCost = 1, kThickCost = 1;
 constexpr int kJoinThreads = 256;
@@ -302,6 +303,11 @@ __device__ __forceinline__ void multiply(floatx16 &s, u32x4 x, u32x4 y) {
   }
 }
 
+// Whether there is nothing to multiply from column d on.  Asked with float32 only, whose products take 64 cycles each and four a
+// step; with bf16 the question would cost about what it saves.
+template <typename T>
+__device__ __forceinline__ bool beyond(int d, int32_t D) { return sizeof(T) == 4 && d > 0 && d >= D; }
+
 // The 16-byte chunk of a key that a lane multiplies in step i: key `base` + lane % 32 of the tile.
 template <int RB>
 __device__ __forceinline__ u32x4 key_chunk(const unsigned char *lk, int base, int lane, int i) {
@@ -311,22 +317,27 @@ __device__ __forceinline__ u32x4 key_chunk(const unsigned char *lk, int base, in
 // Scores of KB blocks of 32 keys of a tile: register 4 j + i of a block is its key 8 j + 4 half + i.  Queries in
 // registers, or of RB blocks of rows in LDS, laid out as keys are.
 template <typename T, int DP, int KB>
-__device__ __forceinline__ void scores(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[KB]) {
+__device__ __forceinline__ void scores(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[KB],
+                                       int32_t D) {
   using S = Shape<T, DP>;
 #pragma unroll
   for (int k = 0; k < KB; ++k) {
     s[k] = floatx16{};
 #pragma unroll
-    for (int i = 0; i < S::NQ; ++i) multiply<S::kBf16>(s[k], key_chunk<S::RB>(lk, 32 * k, lane, i), qf[i]);
+    for (int i = 0; i < S::NQ; ++i) {
+      if (beyond<T>(i * 2 * S::E, D)) break;
+      multiply<S::kBf16>(s[k], key_chunk<S::RB>(lk, 32 * k, lane, i), qf[i]);
+    }
   }
 }
 template <typename T, int DP, int RB>
-__device__ __forceinline__ void scores(const unsigned char *lk, const unsigned char *lq, int lane, floatx16 (&s)[RB]) {
+__device__ __forceinline__ void scores(const unsigned char *lk, const unsigned char *lq, int lane, floatx16 (&s)[RB], int32_t D) {
   using S = Shape<T, DP>;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) s[rb] = floatx16{};
 #pragma unroll
   for (int i = 0; i < S::NQ; ++i) {
+    if (beyond<T>(i * 2 * S::E, D)) break;
     const u32x4 kf = key_chunk<S::RB>(lk, 0, lane, i);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) multiply<S::kBf16>(s[rb], kf, key_chunk<S::RB>(lq, rb * 32, lane, i));
@@ -389,7 +400,8 @@ __device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
 // scores in steps of one operand of keys, read kAhead steps ahead.
 template <typename T, int DP, int KB>
-__device__ __forceinline__ void scores_in_steps(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[KB]) {
+__device__ __forceinline__ void scores_in_steps(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[KB],
+                                                int32_t D) {
   using S = Shape<T, DP>;
   constexpr int kAhead = 3, kSteps = KB * S::NQ;
   u32x4 kf[kAhead + 1];
@@ -402,7 +414,7 @@ __device__ __forceinline__ void scores_in_steps(const unsigned char *lk, int lan
   for (int i = 0; i < kSteps; ++i) {
     pin();
     if (i + kAhead < kSteps) read(i + kAhead);
-    multiply<S::kBf16>(s[i / S::NQ], kf[i % (kAhead + 1)], qf[i % S::NQ]);
+    if (!beyond<T>(i % S::NQ * 2 * S::E, D)) multiply<S::kBf16>(s[i / S::NQ], kf[i % (kAhead + 1)], qf[i % S::NQ]);
   }
   pin();
 }
@@ -440,7 +452,7 @@ __device__ __forceinline__ float value_of(const unsigned char *lv, int base, int
 // Adds weights times values of 32 keys, the first at row `base` of the tile, for RB blocks of rows.
 template <typename T, int DP, int RB>
 __device__ __forceinline__ void add_values(const unsigned char *lv, int base, int lane, const floatx16 (&p)[RB],
-                                           floatx16 (&o)[RB][Shape<T, DP>::NO]) {
+                                           floatx16 (&o)[RB][Shape<T, DP>::NO], int32_t D) {
   using S = Shape<T, DP>;
   if constexpr (S::kBf16) {
 #pragma unroll
@@ -460,6 +472,7 @@ __device__ __forceinline__ void add_values(const unsigned char *lv, int base, in
     for (int r = 0; r < 16; ++r)
 #pragma unroll
       for (int m = 0; m < S::NO; ++m) {
+        if (beyond<T>(32 * m, D)) break;
         const float x = value_of<S::RB>(lv, base, lane, r, m);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) o[rb][m] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[rb][r], o[rb][m], 0, 0, 0);
@@ -470,7 +483,7 @@ __device__ __forceinline__ void add_values(const unsigned char *lv, int base, in
 // The same for KB blocks of 32 keys and one block of rows, in steps with the operands read ahead.
 template <typename T, int DP, int KB>
 __device__ __forceinline__ void add_values_in_steps(const unsigned char *lv, int lane, const floatx16 (&p)[KB],
-                                                    floatx16 (&o)[Shape<T, DP>::NO]) {
+                                                    floatx16 (&o)[Shape<T, DP>::NO], int32_t D) {
   using S = Shape<T, DP>;
   if constexpr (S::kBf16) {
     constexpr int kAhead = 3, kSteps = KB * 2 * S::NO;
@@ -502,7 +515,8 @@ __device__ __forceinline__ void add_values_in_steps(const unsigned char *lv, int
       pin();
       if (i + 1 < kSteps) read(i + 1);
 #pragma unroll
-      for (int m = 0; m < S::NO; ++m) o[m] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i & 1][m], p[i / 16][i % 16], o[m], 0, 0, 0);
+      for (int m = 0; m < S::NO; ++m)
+        if (!beyond<T>(32 * m, D)) o[m] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i & 1][m], p[i / 16][i % 16], o[m], 0, 0, 0);
     }
     pin();
   }
@@ -860,7 +874,7 @@ struct Thick {
 
 template <typename T, int DP, int PAGES>
 __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
-                                            int *odd, Part<DP, kThickRows> *part) {
+                                            int *odd, int turn, Part<DP, kThickRows> *part) {
   using S = Shape<T, DP>;
   using W = Thick<T, DP>;
   int tid = threadIdx.x;
@@ -881,13 +895,14 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
   load(k0, cur);
   if (tid == 0) *odd = 0;               // read behind a barrier of the loop: a piece has a tile
 
-  const int32_t row = wave * 32 + l32;
+  // A wave's number is its SIMD's, and the block's last rows see the most keys: they are turned round from workgroup to workgroup.
+  const int32_t block = (wave + turn) % kAttendWaves * 32, row = block + l32;
   const Row w = row_at(a, u, u.r0 + row);
   u32x4 qf[S::NQ];
   load_query<T, DP>(a, w, half, qf);
   // rows of this wave, and the positions of its first and last
-  const int32_t last = min(u.r0 + wave * 32 + 32, u.rows) - 1;
-  const int32_t pos_first = u.ctx + (u.r0 + wave * 32) / a.G, pos_last = last >= u.r0 + wave * 32 ? u.ctx + last / a.G : -1;
+  const int32_t last = min(u.r0 + block + 32, u.rows) - 1;
+  const int32_t pos_first = u.ctx + (u.r0 + block) / a.G, pos_last = last >= u.r0 + block ? u.ctx + last / a.G : -1;
   const int32_t lo = a.window > 0 ? w.pos - a.window : -1;
 
   floatx16 o[S::NO];
@@ -907,14 +922,20 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
     }
     if (k0 <= pos_last) {               // else no row of this wave sees anything of it
       floatx16 s[W::KB];
-      scores_in_steps<T, DP, W::KB>(cur, lane, qf, s);
+      // The waves of a SIMD are then more often at different ends of their tiles, one in products while another forms weights
+      // (bf16: 27 000 tokens of prompts 1312 -> 1271 us, prompts by pieces 372 -> 359).
+      if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(1);
+      scores_in_steps<T, DP, W::KB>(cur, lane, qf, s, a.D);
+      if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(0);
       if (k0 + W::TK - 1 > pos_first || k0 < u.max_lo) {
 #pragma unroll
         for (int k = 0; k < W::KB; ++k) hide(s[k], k0 + 32 * k, half, w.pos, lo);
       }
       follow<S::NO>(row_max<W::KB>(s, a.c), ref, sum, o);
       to_weights<W::KB>(s, a.c, minus_ref(ref), sum);
-      add_values_in_steps<T, DP, W::KB>(cur + W::kTile, lane, s, o);
+      if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(1);
+      add_values_in_steps<T, DP, W::KB>(cur + W::kTile, lane, s, o, a.D);
+      if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(0);
     }
     unsigned char *x = cur;
     cur = nxt;
@@ -936,7 +957,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_thick_kernel(AttendA
   __shared__ __align__(16) unsigned char lds[Thick<T, DP>::kLds];
   __shared__ int odd;
   work_on_run<DP, kThickRows, Thick<T, DP>::TK, kThickLeast, kThickCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
-    thick_piece<T, DP, PAGES>(a, u, tile, tiles, lds, &odd, part);
+    thick_piece<T, DP, PAGES>(a, u, tile, tiles, lds, &odd, (int) blockIdx.x / kCUs, part);
   });
 }
 
@@ -993,10 +1014,14 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_prompt_kernel(Attend
   __shared__ int odd;
   Unit u;
   u.b = 0;
-  if (!find_prompt_unit(a, (int32_t) (blockIdx.x / (uint32_t) a.heads_kv), u)) return;
-  u.head = (int32_t) (blockIdx.x % (uint32_t) a.heads_kv);
+  // Workgroups come in rounds of one a CU.  Every second round the other way round: where they all run at a time, the CU that began
+  // with the longest unit then gets the shortest of the next round.
+  const uint32_t round = blockIdx.x / kCUs, at = blockIdx.x % kCUs;
+  const uint32_t rank = round % 2 && gridDim.x <= 4 * kCUs ? round * kCUs + kCUs - 1 - at : blockIdx.x;
+  if (!find_prompt_unit(a, (int32_t) (rank / (uint32_t) a.heads_kv), u)) return;
+  u.head = (int32_t) (rank % (uint32_t) a.heads_kv);
   const int32_t tiles = unit_tiles<kThickRows, Thick<T, DP>::TK>(a, u);
-  thick_piece<T, DP, 0>(a, scalar(u), 0, scalar(tiles), lds, &odd, nullptr);
+  thick_piece<T, DP, 0>(a, scalar(u), 0, scalar(tiles), lds, &odd, (int) round, nullptr);
 }
 
 // ---- 32 or 64 rows a workgroup -----------------------------------------------------------------------------------------
@@ -1065,11 +1090,11 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
       wait_vm<NI>();                    // keys are in, values may be on their way
       loader.clear_keys(lk);
       if constexpr (RB == 1) {
-        scores<T, DP, 1>(lk, lane, qf, reinterpret_cast<floatx16(&)[1]>(s[0]));
+        scores<T, DP, 1>(lk, lane, qf, reinterpret_cast<floatx16(&)[1]>(s[0]), a.D);
       } else {
         int away = (int) (lq - lk);
         asm volatile("" : "+s"(away));  // an addition a read, instead of as many addresses in registers
-        scores<T, DP, RB>(lk, lk + away, lane, s);
+        scores<T, DP, RB>(lk, lk + away, lane, s, a.D);
       }
       wait_lds();
     }
@@ -1089,7 +1114,7 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
         odd = __builtin_amdgcn_ballot_w64(clear_odd_values<S::kBf16>(lv, W::kTile, lane, kWave)) != 0 || odd;
         wait_lds();
       }
-      add_values<T, DP, RB>(lv, 0, lane, s, o);
+      add_values<T, DP, RB>(lv, 0, lane, s, o, a.D);
       wait_lds();
     }
     if (!more) break;
@@ -1306,7 +1331,7 @@ hipError_t launch_cache_attend(const AttendArgs &a, bool bf16, int64_t longest, 
 
 hipError_t launch_prompt_attend(const AttendArgs &a, bool bf16, hipStream_t stream) {
   const int64_t units = (int64_t) a.T * a.G / kThickRows + a.B;
-  const dim3 grid((uint32_t) (units * a.heads_kv));
+  const dim3 grid((uint32_t) ((units * a.heads_kv + kCUs - 1) / kCUs * kCUs));
   if (bf16 && a.D <= 64) attend_prompt_kernel<uint16_t, 64><<<grid, kAttendThreads, 0, stream>>>(a);
   else if (bf16) attend_prompt_kernel<uint16_t, 128><<<grid, kAttendThreads, 0, stream>>>(a);
   else if (a.D <= 64) attend_prompt_kernel<float, 64><<<grid, kAttendThreads, 0, stream>>>(a);
