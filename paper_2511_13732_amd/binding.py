@@ -594,10 +594,11 @@ def propose(groups: Groups, draft_logits: torch.Tensor, *, temperature: float = 
 
 # ------------------------------------------------- the forward pass between proposals and verification
 
-def _int32(t: torch.Tensor, shape, dev, what: str):
-    """Checks an int32 tensor of that shape on that device, contiguous."""
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or t.device != dev or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {tuple(shape)} on {dev}")
+def _int32(t: torch.Tensor, n: int, dev, what: str):
+    """Checks an int32 tensor [n] on that device, contiguous.  (These checks are part of every call: they read as few
+    properties as they can.)"""
+    if t.dtype is not torch.int32 or t.numel() != n or t.dim() != 1 or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{what} must be a contiguous int32 tensor [{n}] on {dev}")
 
 
 @dataclass
@@ -617,10 +618,11 @@ class Pages:
             raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
         self.B, self.max_blocks = t.shape
         self.num_pages = self.free_pages.numel()
-        _int32(self.free_pages, (self.num_pages,), t.device, "free_pages")
-        _int32(self.state, (3 * self.B + 1,), t.device, "state")
-        self._struct = _PagesStruct(self.B, self.num_pages, self.page_size, self.max_blocks, t.data_ptr(),
-                                    t.stride(0) if self.B > 1 else self.max_blocks, self.free_pages.data_ptr())
+        _int32(self.free_pages, self.num_pages, t.device, "free_pages")
+        _int32(self.state, 3 * self.B + 1, t.device, "state")
+        self.device = t.device
+        self._ref = C.pointer(_PagesStruct(self.B, self.num_pages, self.page_size, self.max_blocks, t.data_ptr(),
+                                    t.stride(0) if self.B > 1 else self.max_blocks, self.free_pages.data_ptr()))
 
     @classmethod
     def empty(cls, B: int, num_pages: int, page_size: int, max_blocks: int, device) -> "Pages":
@@ -667,20 +669,21 @@ def pages_step(pages: Pages, add, *, max_tokens: int, commit: Optional[torch.Ten
     ``commit``; after ``verify``: ``commit=out.accept_len, commit_extra=1``), adjusts the pages that it holds to ``add``
     new tokens (an int for all, or int32 [B]; negative: the request has ended) and says where each of them goes.
     The state is updated in place, or written to ``state_out``."""
-    dev, B = pages.state.device, pages.B
+    dev, B = pages.device, pages.B
     if out is None:
         out = pages_step_outputs(B, max_tokens, dev)
     if out.slots.numel() < max_tokens or out.positions.numel() < max_tokens or out.q_start.numel() != B + 1:
         raise ValueError("the outputs have room for another number of rows or requests")
     each = isinstance(add, torch.Tensor)
-    for t, what in ((commit, "commit"), (add if each else None, "add")):
-        if t is not None:
-            _int32(t, (B,), dev, what)
+    if each:
+        _int32(add, B, dev, "add")
+    if commit is not None:
+        _int32(commit, B, dev, "commit")
     if state_out is None:
         state_out = pages.state
     else:
-        _int32(state_out, (3 * B + 1,), dev, "state_out")
-    _call(dev, "pcg_pages_step", lib().pcg_pages_step, C.byref(pages._struct), pages.state.data_ptr(), state_out.data_ptr(),
+        _int32(state_out, 3 * B + 1, dev, "state_out")
+    _call(dev, "pcg_pages_step", lib().pcg_pages_step, pages._ref, pages.state.data_ptr(), state_out.data_ptr(),
           None if commit is None else commit.data_ptr(), commit_extra, add.data_ptr() if each else None,
           0 if each else add, max_tokens, out.q_start.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(),
           out.refused.data_ptr())
@@ -701,30 +704,28 @@ class KvCache:
         if k.stride(3) != 1:
             raise ValueError("the last axis of the cache must be contiguous")
         self.num_pages, self.page_size, self.kv_heads, self.head_dim = k.shape
-        self._struct = _KvCacheStruct(k.data_ptr(), v.data_ptr(), _dtype_code(k), *k.shape, *k.stride()[:3])
+        self.device, self.dtype = k.device, k.dtype
+        self._ref = C.pointer(_KvCacheStruct(k.data_ptr(), v.data_ptr(), _dtype_code(k), *k.shape, *k.stride()[:3]))
 
 
-def _rows(t: torch.Tensor, like: torch.Tensor, heads: int, head_dim: int, what: str):
-    """Checks rows [T, heads, head_dim] of the dtype and device of `like`; (token stride, head stride)."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{what} must be [T, {heads}, {head_dim}], {like.dtype}, on {like.device}")
-    st = t.stride()
-    if st[2] != 1:
+def _rows(t: torch.Tensor, rows: int, heads: int, head_dim: int, dtype, dev, what: str):
+    """Checks rows [rows, heads, head_dim] of a dtype and device; (token stride, head stride)."""
+    if t.shape != (rows, heads, head_dim) or t.dtype is not dtype or t.device != dev:
+        raise ValueError(f"{what} must be [{rows}, {heads}, {head_dim}], {dtype}, on {dev}")
+    tok, head, one = t.stride()
+    if one != 1:
         raise ValueError(f"the last axis of {what} must be contiguous")
-    return st[0], st[1]
+    return tok, head
 
 
 def cache_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Keys and values [T, kv_heads, head_dim] of new tokens to their ``slots`` (int32 [T], as pages_step gives them;
     negative: left out)."""
-    ks = _rows(k, cache.k, cache.kv_heads, cache.head_dim, "k")
-    vs = _rows(v, cache.k, cache.kv_heads, cache.head_dim, "v")
-    if k.shape[0] != v.shape[0]:
-        raise ValueError("k and v must have the same rows")
-    dev = cache.k.device
-    _int32(slots, (k.shape[0],), dev, "slots")
-    _call(dev, "pcg_cache_write", lib().pcg_cache_write, C.byref(cache._struct), k.data_ptr(), v.data_ptr(), k.shape[0], *ks, *vs,
-          slots.data_ptr())
+    T, dev = slots.numel(), cache.device
+    ks = _rows(k, T, cache.kv_heads, cache.head_dim, cache.dtype, dev, "k")
+    vs = _rows(v, T, cache.kv_heads, cache.head_dim, cache.dtype, dev, "v")
+    _int32(slots, T, dev, "slots")
+    _call(dev, "pcg_cache_write", lib().pcg_cache_write, cache._ref, k.data_ptr(), v.data_ptr(), T, *ks, *vs, slots.data_ptr())
 
 
 def cache_attend_workspace_bytes(B: int, rows: int, heads: int, kv_heads: int, head_dim: int, longest: int) -> int:
@@ -739,27 +740,24 @@ def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, len
     seeing the keys up to itself, with ``window`` the last that many of them.  ``longest`` bounds the new tokens of a request
     (it decides how the work is cut; without it: the mean).  ``scale`` is 1 / sqrt(head_dim) unless given.  Rows of ``out`` behind
     the last request's stay as they were (zeros where ``out`` is not given)."""
-    T, heads = q.shape[0], q.shape[1]
-    qs = _rows(q, cache.k, heads, cache.head_dim, "q")
-    dev, B = q.device, lens.numel()
+    T, heads, head_dim = q.shape
+    dev, B = cache.device, lens.numel()
+    qs = _rows(q, T, heads, cache.head_dim, cache.dtype, dev, "q")
     if out is None:
-        out = torch.zeros((T, heads, cache.head_dim), dtype=q.dtype, device=dev)
-    os_ = _rows(out, cache.k, heads, cache.head_dim, "out")
-    if out.shape[0] != T:
-        raise ValueError("out must have q's rows")
-    if block_table.dim() != 2 or block_table.dtype != torch.int32 or block_table.shape[0] != B or block_table.device != dev or \
+        out = torch.zeros((T, heads, head_dim), dtype=q.dtype, device=dev)
+    os_ = _rows(out, T, heads, head_dim, cache.dtype, dev, "out")
+    if block_table.dim() != 2 or block_table.dtype is not torch.int32 or block_table.shape[0] != B or block_table.device != dev or \
             (block_table.shape[1] > 1 and block_table.stride(1) != 1):
         raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
-    _int32(lens, (B,), dev, "lens")
-    _int32(q_start, (B + 1,), dev, "q_start")
+    _int32(lens, B, dev, "lens")
+    _int32(q_start, B + 1, dev, "q_start")
     if longest is None:
         longest = -(-T // max(B, 1))
     if workspace is None:
-        workspace = _workspace(dev, cache_attend_workspace_bytes(B, T, heads, cache.kv_heads, cache.head_dim, longest))
-    _call(dev, "pcg_cache_attend", lib().pcg_cache_attend, C.byref(cache._struct), q.data_ptr(), *qs, heads, T,
-          block_table.data_ptr(), block_table.stride(0), block_table.shape[1], lens.data_ptr(), q_start.data_ptr(), B, longest,
-          cache.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), *os_, workspace.data_ptr(),
-          workspace.numel())
+        workspace = _workspace(dev, cache_attend_workspace_bytes(B, T, heads, cache.kv_heads, head_dim, longest))
+    _call(dev, "pcg_cache_attend", lib().pcg_cache_attend, cache._ref, q.data_ptr(), *qs, heads, T, block_table.data_ptr(),
+          block_table.stride(0), block_table.shape[1], lens.data_ptr(), q_start.data_ptr(), B, longest,
+          head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), *os_, workspace.data_ptr(), workspace.numel())
     return out
 
 
@@ -768,17 +766,14 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: to
     """Causal attention of packed prompts: rows q_start[b] .. q_start[b + 1] of ``q`` [T, heads, head_dim], ``k`` and ``v``
     [T, kv_heads, head_dim] are request b's tokens.  Arguments as for ``cache_attend``."""
     T, heads, head_dim = q.shape
-    kv_heads = k.shape[1]
-    qs, ks, vs = (_rows(t, q, h, head_dim, w) for t, h, w in ((q, heads, "q"), (k, kv_heads, "k"), (v, kv_heads, "v")))
-    if k.shape[0] != T or v.shape[0] != T:
-        raise ValueError("k and v must have q's rows")
-    dev, B = q.device, q_start.numel() - 1
+    kv_heads, dtype, dev, B = k.shape[1], q.dtype, q.device, q_start.numel() - 1
+    qs = _rows(q, T, heads, head_dim, dtype, dev, "q")
+    ks = _rows(k, T, kv_heads, head_dim, dtype, dev, "k")
+    vs = _rows(v, T, kv_heads, head_dim, dtype, dev, "v")
     if out is None:
-        out = torch.zeros((T, heads, head_dim), dtype=q.dtype, device=dev)
-    os_ = _rows(out, q, heads, head_dim, "out")
-    if out.shape[0] != T:
-        raise ValueError("out must have q's rows")
-    _int32(q_start, (B + 1,), dev, "q_start")
+        out = torch.zeros((T, heads, head_dim), dtype=dtype, device=dev)
+    os_ = _rows(out, T, heads, head_dim, dtype, dev, "out")
+    _int32(q_start, B + 1, dev, "q_start")
     if longest is None:
         longest = -(-T // max(B, 1))
     _call(dev, "pcg_prompt_attend", lib().pcg_prompt_attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q), T, heads,

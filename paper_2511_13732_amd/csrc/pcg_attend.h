@@ -24,6 +24,6 @@ struct AttendArgs {
 
 size_t attend_workspace_bytes(int32_t G, int32_t D, int64_t longest);
 hipError_t launch_cache_attend(const AttendArgs &a, bool bf16, int64_t longest, void *workspace, hipStream_t stream);
-hipError_t launch_prompt_attend(const AttendArgs &a, bool bf16, hipStream_t stream);
+hipError_t launch_prompt_attend(const AttendArgs &a, bool bf16, int64_t longest, hipStream_t stream);
 
 }  // namespace pcg

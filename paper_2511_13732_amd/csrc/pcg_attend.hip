@@ -863,20 +863,54 @@ __device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *
 
 // ---- 128 rows a workgroup ----------------------------------------------------------------------------------------------
 
-template <typename T, int DP>
+// Rows of a wave on their way to another through LDS: 32 rows' outputs (not divided), references and sums.
+template <int DP>
+constexpr int kRowsFloats = 32 * (DP + 2);
+
+template <int DP>
+__device__ __forceinline__ void give_rows(float *to, int lane, const floatx16 (&o)[DP / 32], float ref, float sum) {
+  const int l32 = lane & 31, half = lane >> 5;
+#pragma unroll
+  for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) to[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] = o[n][i];
+  const float all = pair_sum(sum);
+  if (half == 0) {
+    to[DP * 32 + l32] = ref;
+    to[(DP + 1) * 32 + l32] = all;
+  }
+}
+template <int DP>
+__device__ __forceinline__ void take_rows(const float *from, int lane, floatx16 (&o)[DP / 32], float &ref, float &sum) {
+  const int l32 = lane & 31, half = lane >> 5;
+  const float theirs = from[DP * 32 + l32], now = fmaxf(ref, theirs);
+  const float f0 = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
+  const float f1 = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(theirs - now);
+  ref = now;
+  sum = sum * f0 + (half == 0 ? from[(DP + 1) * 32 + l32] * f1 : 0.f);
+#pragma unroll
+  for (int n = 0; n < DP / 32; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[n][i] = o[n][i] * f0 + from[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] * f1;
+}
+
+// WK waves share 32 rows and take the keys of a tile in turn, KB blocks of 32 each.
+template <typename T, int DP, int WK>
 struct Thick {
   using S = Shape<T, DP>;
-  static constexpr int KB = S::kBf16 ? 2 : 1;
-  static constexpr int TK = 32 * KB;
+  static constexpr int R = kThickRows / WK;
+  static constexpr int KB = S::kBf16 && WK == 1 ? 2 : 1;
+  static constexpr int TK = 32 * KB * WK;
   static constexpr int kTile = TK * S::RB;
   static constexpr int kLds = 4 * kTile;            // keys and values, two of each
 };
 
-template <typename T, int DP, int PAGES>
+template <typename T, int DP, int WK, int PAGES>
 __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
-                                            int *odd, int turn, Part<DP, kThickRows> *part) {
+                                            int *odd, int turn, Part<DP, Thick<T, DP, WK>::R> *part) {
   using S = Shape<T, DP>;
-  using W = Thick<T, DP>;
+  using W = Thick<T, DP, WK>;
+  constexpr int WR = kAttendWaves / WK;
   int tid = threadIdx.x;
   asm("" : "+v"(tid));                  // what follows from it is formed here, not kept in registers from piece to piece
   const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -896,7 +930,8 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
   if (tid == 0) *odd = 0;               // read behind a barrier of the loop: a piece has a tile
 
   // A wave's number is its SIMD's, and the block's last rows see the most keys: they are turned round from workgroup to workgroup.
-  const int32_t block = (wave + turn) % kAttendWaves * 32, row = block + l32;
+  const int32_t block = (wave + turn) % WR * 32, row = block + l32;
+  const int32_t first_key = wave / WR * 32 * W::KB;       // this wave's in a tile
   const Row w = row_at(a, u, u.r0 + row);
   u32x4 qf[S::NQ];
   load_query<T, DP>(a, w, half, qf);
@@ -920,21 +955,23 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
       if (clear_odd_values<S::kBf16>(cur + W::kTile, W::kTile, tid, kAttendThreads)) *odd = 1;
       bare_barrier();
     }
-    if (k0 <= pos_last) {               // else no row of this wave sees anything of it
+    const int32_t k = k0 + first_key;
+    if (k <= pos_last && k < end) {     // else no row of this wave sees anything of it
+      const unsigned char *lk = cur + first_key * S::RB, *lv = lk + W::kTile;
       floatx16 s[W::KB];
       // The waves of a SIMD are then more often at different ends of their tiles, one in products while another forms weights
       // (bf16: 27 000 tokens of prompts 1312 -> 1271 us, prompts by pieces 372 -> 359).
       if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(1);
-      scores_in_steps<T, DP, W::KB>(cur, lane, qf, s, a.D);
+      scores_in_steps<T, DP, W::KB>(lk, lane, qf, s, a.D);
       if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(0);
-      if (k0 + W::TK - 1 > pos_first || k0 < u.max_lo) {
+      if (k + 32 * W::KB - 1 > pos_first || k < u.max_lo) {
 #pragma unroll
-        for (int k = 0; k < W::KB; ++k) hide(s[k], k0 + 32 * k, half, w.pos, lo);
+        for (int i = 0; i < W::KB; ++i) hide(s[i], k + 32 * i, half, w.pos, lo);
       }
       follow<S::NO>(row_max<W::KB>(s, a.c), ref, sum, o);
       to_weights<W::KB>(s, a.c, minus_ref(ref), sum);
       if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(1);
-      add_values_in_steps<T, DP, W::KB>(cur + W::kTile, lane, s, o, a.D);
+      add_values_in_steps<T, DP, W::KB>(lv, lane, s, o, a.D);
       if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(0);
     }
     unsigned char *x = cur;
@@ -944,46 +981,54 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
   bare_barrier();
   if (*odd) {
     for (k0 = begin; k0 < end; k0 += W::TK)
-      if (at_edge(k0)) add_odd_values<T, DP, PAGES != 0>(a, u, k0, min(k0 + W::TK, u.k_hi), half, w.pos, lo, o);
+      if (at_edge(k0))
+        add_odd_values<T, DP, PAGES != 0>(a, u, k0 + first_key, min(k0 + first_key + 32 * W::KB, u.k_hi), half, w.pos, lo, o);
+  }
+  if constexpr (WK > 1) {
+    static_assert(WK == 2 && WR * kRowsFloats<DP> * 4 <= W::kLds, "the rows of the second half of the keys");
+    float *room = reinterpret_cast<float *>(lds) + wave % WR * kRowsFloats<DP>;
+    bare_barrier();
+    if (wave >= WR) give_rows<DP>(room, lane, o, ref, sum);
+    bare_barrier();
+    if (wave >= WR) return;
+    take_rows<DP>(room, lane, o, ref, sum);
   }
   sum = pair_sum(sum);
-  if (part) store_part<DP, kThickRows>(part, row, half, w.there, o, ref, sum);
+  if (part) store_part<DP, W::R>(part, row, half, w.there, o, ref, sum);
   else store_row<T, DP>(a, w, half, o, sum);
 }
 
 template <typename T, int DP, int PAGES>
 __global__ __launch_bounds__(kAttendThreads, 2) void attend_thick_kernel(AttendArgs a, Join *join,
                                                                          Part<DP, kThickRows> *parts) {
-  __shared__ __align__(16) unsigned char lds[Thick<T, DP>::kLds];
+  __shared__ __align__(16) unsigned char lds[Thick<T, DP, 1>::kLds];
   __shared__ int odd;
-  work_on_run<DP, kThickRows, Thick<T, DP>::TK, kThickLeast, kThickCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
-    thick_piece<T, DP, PAGES>(a, u, tile, tiles, lds, &odd, (int) blockIdx.x / kCUs, part);
+  work_on_run<DP, kThickRows, Thick<T, DP, 1>::TK, kThickLeast, kThickCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
+    thick_piece<T, DP, 1, PAGES>(a, u, tile, tiles, lds, &odd, (int) blockIdx.x / kCUs, part);
   });
 }
 
 // Unit `rank` of all requests' row blocks, the ones furthest down their prompt first: they have the most keys, and what is
 // begun last should be short.
+template <int R>
 __device__ __forceinline__ bool find_prompt_unit(const AttendArgs &a, int32_t rank, Unit &u) {
   const int lane = threadIdx.x & (kWave - 1);
   auto blocks_of = [&](int32_t b) -> int32_t {
     int32_t first;
-    return b < a.B ? (request_tokens(a, b, first) * a.G + kThickRows - 1) / kThickRows : 0;
+    return b < a.B ? (request_tokens(a, b, first) * a.G + R - 1) / R : 0;
   };
   const int32_t here = blocks_of(lane);
   // units at block `level` (from 1) or further down
   auto at_least = [&](int32_t level) -> int32_t {
     int32_t n = max(0, here - level + 1);
     for (int32_t b = lane + kWave; b < a.B; b += kWave) n += max(0, blocks_of(b) - level + 1);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
-    return n;
+    return (int32_t) wave_sum((double) n);              // exact, through DPP
   };
   if (rank >= at_least(1)) return false;
   int32_t most = here;
   for (int32_t b = lane + kWave; b < a.B; b += kWave) most = max(most, blocks_of(b));
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) most = max(most, __shfl_xor(most, d));
-  int32_t lo = 1, hi = most + 1;       // at_least(lo) > rank >= at_least(hi)
+  // at_least(lo) > rank >= at_least(hi); a maximum in float32 may be rounded, up if need be
+  int32_t lo = 1, hi = (int32_t) (wave_max((float) most) * 1.0000002f) + 2;
   while (hi - lo > 1) {
     const int32_t mid = (lo + hi) >> 1;
     if (at_least(mid) > rank) lo = mid;
@@ -1004,13 +1049,14 @@ __device__ __forceinline__ bool find_prompt_unit(const AttendArgs &a, int32_t ra
   u.b = __builtin_amdgcn_readfirstlane(u.b);
   u.rows = request_tokens(a, u.b, u.first) * a.G;
   u.ctx = 0;
-  u.r0 = (lo - 1) * kThickRows;
+  u.r0 = (lo - 1) * R;
   return true;
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(kAttendThreads, 2) void attend_prompt_kernel(AttendArgs a) {
-  __shared__ __align__(16) unsigned char lds[Thick<T, DP>::kLds];
+template <typename T, int DP, int WK>
+__global__ __launch_bounds__(kAttendThreads, (2 * Thick<T, DP, WK>::kLds < 160 * 1024 ? 2 : 1)) void attend_prompt_kernel(AttendArgs a) {
+  using W = Thick<T, DP, WK>;
+  __shared__ __align__(16) unsigned char lds[W::kLds];
   __shared__ int odd;
   Unit u;
   u.b = 0;
@@ -1018,10 +1064,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_prompt_kernel(Attend
   // with the longest unit then gets the shortest of the next round.
   const uint32_t round = blockIdx.x / kCUs, at = blockIdx.x % kCUs;
   const uint32_t rank = round % 2 && gridDim.x <= 4 * kCUs ? round * kCUs + kCUs - 1 - at : blockIdx.x;
-  if (!find_prompt_unit(a, (int32_t) (rank / (uint32_t) a.heads_kv), u)) return;
+  if (!find_prompt_unit<W::R>(a, (int32_t) (rank / (uint32_t) a.heads_kv), u)) return;
   u.head = (int32_t) (rank % (uint32_t) a.heads_kv);
-  const int32_t tiles = unit_tiles<kThickRows, Thick<T, DP>::TK>(a, u);
-  thick_piece<T, DP, 0>(a, scalar(u), 0, scalar(tiles), lds, &odd, (int) round, nullptr);
+  const int32_t tiles = unit_tiles<W::R, W::TK>(a, u);
+  thick_piece<T, DP, WK, 0>(a, scalar(u), 0, scalar(tiles), lds, &odd, (int) round, nullptr);
 }
 
 // ---- 32 or 64 rows a workgroup -----------------------------------------------------------------------------------------
@@ -1132,30 +1178,9 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
 
   // The waves' sums: 2 to 0 and 3 to 1, then 1 to 0 (with two blocks of rows 0 also gives its second to 1).
   float *room = reinterpret_cast<float *>(lds);
-  constexpr int kBlock = 32 * (DP + 2);
-  auto give = [&](float *to, int rb) {
-#pragma unroll
-    for (int n = 0; n < S::NO; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) to[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] = o[rb][n][i];
-    const float all = pair_sum(sum[rb]);
-    if (half == 0) {
-      to[DP * 32 + l32] = ref[rb];
-      to[(DP + 1) * 32 + l32] = all;
-    }
-  };
-  auto take = [&](const float *from, int rb) {
-    const float theirs = from[DP * 32 + l32], now = fmaxf(ref[rb], theirs);
-    const float f0 = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[rb] - now);
-    const float f1 = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(theirs - now);
-    ref[rb] = now;
-    sum[rb] = sum[rb] * f0 + (half == 0 ? from[(DP + 1) * 32 + l32] * f1 : 0.f);
-#pragma unroll
-    for (int n = 0; n < S::NO; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        o[rb][n][i] = o[rb][n][i] * f0 + from[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] * f1;
-  };
+  constexpr int kBlock = kRowsFloats<DP>;
+  auto give = [&](float *to, int rb) { give_rows<DP>(to, lane, o[rb], ref[rb], sum[rb]); };
+  auto take = [&](const float *from, int rb) { take_rows<DP>(from, lane, o[rb], ref[rb], sum[rb]); };
   bare_barrier();
   if (wave >= 2) {
 #pragma unroll
@@ -1329,14 +1354,32 @@ hipError_t launch_cache_attend(const AttendArgs &a, bool bf16, int64_t longest, 
   return a.D <= 64 ? go_cache<float, 64>(a, longest, workspace, stream) : go_cache<float, 128>(a, longest, workspace, stream);
 }
 
-hipError_t launch_prompt_attend(const AttendArgs &a, bool bf16, hipStream_t stream) {
-  const int64_t units = (int64_t) a.T * a.G / kThickRows + a.B;
-  const dim3 grid((uint32_t) ((units * a.heads_kv + kCUs - 1) / kCUs * kCUs));
-  if (bf16 && a.D <= 64) attend_prompt_kernel<uint16_t, 64><<<grid, kAttendThreads, 0, stream>>>(a);
-  else if (bf16) attend_prompt_kernel<uint16_t, 128><<<grid, kAttendThreads, 0, stream>>>(a);
-  else if (a.D <= 64) attend_prompt_kernel<float, 64><<<grid, kAttendThreads, 0, stream>>>(a);
-  else attend_prompt_kernel<float, 128><<<grid, kAttendThreads, 0, stream>>>(a);
+namespace {
+template <typename T, int DP, int WK>
+hipError_t go_prompt(const AttendArgs &a, hipStream_t stream) {
+  const int64_t units = ((int64_t) a.T * a.G / Thick<T, DP, WK>::R + a.B) * a.heads_kv;
+  attend_prompt_kernel<T, DP, WK><<<(uint32_t) ((units + kCUs - 1) / kCUs * kCUs), kAttendThreads, 0, stream>>>(a);
   return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t go_prompts(const AttendArgs &a, int64_t longest, hipStream_t stream) {
+  // Keys that a workgroup place of the chip works through if all units fill it evenly, against those of the longest unit, which
+  // nothing can overtake.  Two waves on the keys of the same rows halve the way, but every unit has its joining and half the rows for
+  // the keys that it brings.  us with one wave and with two, at longest / even:
+  //   bf16, d = 64:   0.57 64 and 82;  1.9 27 and 32;  2.1 40 and 35;  3.7 19 and 17;  8 14.5 and 13.3
+  //   bf16, d = 128:  0.57 113 and 169;  2.1 57 and 66;  3.8 21 and 25;  7.6 15.4 and 13.6;  16 29 and 23
+  //   fp32, d = 64:   0.57 297 and 369;  1.9 117 and 114;  2.8 124 and 98;  8 49 and 30
+  //   fp32, d = 128:  0.57 601 and 914;  2.1 309 and 407;  3.7 123 and 124;  7.6 55 and 46;  16 158 and 93
+  const double units = (double) a.T * a.G / kThickRows * a.heads_kv, even = units * (0.5 * a.T / a.B) / 512;
+  if (longest > (DP == 64 ? 2 : 5) * even) return go_prompt<T, DP, 2>(a, stream);
+  return go_prompt<T, DP, 1>(a, stream);
+}
+}  // namespace
+
+hipError_t launch_prompt_attend(const AttendArgs &a, bool bf16, int64_t longest, hipStream_t stream) {
+  if (bf16) return a.D <= 64 ? go_prompts<uint16_t, 64>(a, longest, stream) : go_prompts<uint16_t, 128>(a, longest, stream);
+  return a.D <= 64 ? go_prompts<float, 64>(a, longest, stream) : go_prompts<float, 128>(a, longest, stream);
 }
 
 }  // namespace pcg

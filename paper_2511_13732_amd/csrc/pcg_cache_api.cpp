@@ -225,7 +225,7 @@ int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt,
   a.k_head = k_head_stride;
   a.v_tok = v_tok_stride;
   a.v_head = v_head_stride;
-  return finish(launch_prompt_attend(a, dt == PCG_BF16, (hipStream_t) hip_stream));
+  return finish(launch_prompt_attend(a, dt == PCG_BF16, longest, (hipStream_t) hip_stream));
 }
 
 }  // extern "C"
