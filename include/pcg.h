@@ -574,7 +574,9 @@ size_t pcg_cache_attend_workspace_bytes(int32_t B, int64_t T, int32_t heads, int
 
 /*
  * The same for whole prompts, packed one behind the other: rows q_start[b] .. q_start[b + 1] of q, k and v are request b's
- * tokens, at positions 0, 1, ..  Types, strides, scale, window and empty rows as above; needs no workspace.
+ * tokens, at positions 0, 1, ..  Types, strides, scale, window and empty rows as above (k and v: eight tokens within 2 GiB of each
+ * other); needs no workspace.  `longest` is the longest prompt's tokens, as near as the caller knows: where one is long beside the
+ * load of the whole chip, the work is cut finer.
  */
 int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt, int64_t T, int32_t heads, int32_t kv_heads,
                       int32_t head_dim, int64_t q_tok_stride, int64_t q_head_stride, int64_t k_tok_stride,

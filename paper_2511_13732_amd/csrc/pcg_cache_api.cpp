@@ -1,6 +1,7 @@
 // C ABI of the operators around a step's forward pass (see include/pcg.h): argument checks, then one launcher each.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -53,7 +54,7 @@ int check_queries(AttendArgs &a, const void *q, int64_t q_tok, int64_t q_head, p
                   int32_t head_dim, int64_t T, const int32_t *q_start, int32_t B, int64_t longest, float scale,
                   int32_t window, void *out, int64_t o_tok, int64_t o_head) {
   if (int rc = check_heads(heads, kv_heads, head_dim)) return rc;
-  if (B < 0 || T < 0 || longest < 0 || window < 0) return PCG_ERR_BAD_SHAPE;
+  if (B < 0 || T < 0 || longest < 0 || longest >= kInt31 || window < 0) return PCG_ERR_BAD_SHAPE;
   // rows of a shared head and workgroups are counted in 32 bits
   if (T * (heads / kv_heads) >= kInt31 || (T * (heads / kv_heads) / 32 + B) * kv_heads >= kInt31) return PCG_ERR_BAD_SHAPE;
   if (!(std::isfinite(scale) && scale > 0.0f)) return PCG_ERR_BAD_SCALE;
@@ -164,7 +165,7 @@ int pcg_cache_write(const pcg_kv_cache *cache, const void *k_new, const void *v_
 
 size_t pcg_cache_attend_workspace_bytes(int32_t B, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                         int64_t longest) {
-  if (B < 0 || T < 0 || longest < 0 || check_heads(heads, kv_heads, head_dim)) return 0;
+  if (B < 0 || T < 0 || longest < 0 || longest >= kInt31 || check_heads(heads, kv_heads, head_dim)) return 0;
   return attend_workspace_bytes(heads / kv_heads, head_dim, longest);
 }
 
@@ -179,8 +180,8 @@ int pcg_cache_attend(const pcg_kv_cache *cache, const void *q, int64_t q_tok_str
   if (int rc = check_queries(a, q, q_tok_stride, q_head_stride, c.dt, heads, c.kv_heads, c.head_dim, T, q_start, B, longest,
                              scale, window, out, out_tok_stride, out_head_stride))
     return rc;
-  // positions are counted in 32 bits
-  if (max_blocks < 1 || (int64_t) max_blocks * c.page_size + T >= kInt31) return PCG_ERR_BAD_SHAPE;
+  // positions are counted in 32 bits, up to a tile behind the last
+  if (max_blocks < 1 || (int64_t) max_blocks * c.page_size + T >= kInt31 - 256) return PCG_ERR_BAD_SHAPE;
   if (B > 1 && (table_stride < max_blocks || table_stride >= kFar)) return PCG_ERR_BAD_STRIDE;
   if (B == 0 || T == 0) return PCG_OK;
   if (!block_table || !lens || !workspace) return PCG_ERR_NULL_ARG;
@@ -218,12 +219,14 @@ int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt,
   if (!stride16(k_tok_stride, dt, T == 1) || !stride16(v_tok_stride, dt, T == 1) ||
       !stride16(k_head_stride, dt, kv_heads == 1) || !stride16(v_head_stride, dt, kv_heads == 1))
     return PCG_ERR_BAD_STRIDE;
+  // a load brings up to eight tokens' keys, whose offsets from the first are counted in 32 bits
+  if (T > 1 && std::max(k_tok_stride, v_tok_stride) * 8 * elem_bytes(dt) >= kInt31) return PCG_ERR_BAD_STRIDE;
   if (!aligned(k, 16) || !aligned(v, 16)) return PCG_ERR_MISALIGNED;
   a.k = k;
   a.v = v;
-  a.k_tok = k_tok_stride;
+  a.k_tok = T > 1 ? k_tok_stride : 0;      // of a single token any stride will do
   a.k_head = k_head_stride;
-  a.v_tok = v_tok_stride;
+  a.v_tok = T > 1 ? v_tok_stride : 0;
   a.v_head = v_head_stride;
   return finish(launch_prompt_attend(a, dt == PCG_BF16, longest, (hipStream_t) hip_stream));
 }

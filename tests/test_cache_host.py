@@ -64,7 +64,7 @@ def test_rows_that_are_refused(bad, status):
 
 
 QUERIES = [(dict(heads=3), BAD_SHAPE), (dict(heads=0), BAD_SHAPE), (dict(B=-1), BAD_SHAPE), (dict(T=-1), BAD_SHAPE),
-           (dict(longest=-1), BAD_SHAPE), (dict(window=-1), BAD_SHAPE), (dict(T=1 << 31), BAD_SHAPE), (dict(scale=0.0), BAD_SCALE),
+           (dict(longest=-1), BAD_SHAPE), (dict(longest=1 << 31), BAD_SHAPE), (dict(window=-1), BAD_SHAPE), (dict(T=1 << 31), BAD_SHAPE), (dict(scale=0.0), BAD_SCALE),
            (dict(scale=math.nan), BAD_SCALE), (dict(scale=math.inf), BAD_SCALE), (dict(scale=-1.0), BAD_SCALE),
            (dict(q=None), NULL_ARG), (dict(out=None), NULL_ARG), (dict(starts=None), NULL_ARG), (dict(qt=0), BAD_STRIDE),
            (dict(qh=4), BAD_STRIDE), (dict(ot=-256), BAD_STRIDE), (dict(oh=65), BAD_STRIDE), (dict(q=P + 2), MISALIGNED),
@@ -77,7 +77,7 @@ def test_queries_that_are_refused(bad, status):
     assert prompt(**bad) == status
 
 
-@pytest.mark.parametrize("bad,status", [(dict(blocks=0), BAD_SHAPE), (dict(blocks=1 << 28), BAD_SHAPE), (dict(ts=7), BAD_STRIDE),
+@pytest.mark.parametrize("bad,status", [(dict(blocks=0), BAD_SHAPE), (dict(blocks=1 << 28), BAD_SHAPE), (dict(blocks=(1 << 27) - 1, ts=1 << 27), BAD_SHAPE), (dict(ts=7), BAD_STRIDE),
                                         (dict(table=None), NULL_ARG), (dict(lens=None), NULL_ARG), (dict(ws=None), NULL_ARG),
                                         (dict(table=P + 2), MISALIGNED), (dict(lens=P + 2), MISALIGNED), (dict(ws=P + 16), MISALIGNED),
                                         (dict(wsb=0), WS_SMALL)])
@@ -88,13 +88,14 @@ def test_tables_that_are_refused(bad, status):
 def test_the_workspace_is_what_the_helper_says():
     need = pcg.cache_attend_workspace_bytes(2, 4, 4, 2, 64, 2)
     assert need > 0 and attend(wsb=need - 1) == WS_SMALL
-    for bad in ((-1, 4, 4, 2, 64, 2), (2, -4, 4, 2, 64, 2), (2, 4, 3, 2, 64, 2), (2, 4, 4, 2, 60, 2), (2, 4, 4, 2, 64, -2)):
+    for bad in ((-1, 4, 4, 2, 64, 2), (2, -4, 4, 2, 64, 2), (2, 4, 3, 2, 64, 2), (2, 4, 4, 2, 60, 2), (2, 4, 4, 2, 64, -2), (2, 4, 4, 2, 64, 1 << 31)):
         assert pcg.cache_attend_workspace_bytes(*bad) == 0
 
 
 @pytest.mark.parametrize("bad,status", [(dict(dt=7), BAD_DTYPE), (dict(kv=0), BAD_SHAPE), (dict(D=4), BAD_SHAPE), (dict(D=192), BAD_SHAPE),
                                         (dict(k=None), NULL_ARG), (dict(v=None), NULL_ARG), (dict(kt=0), BAD_STRIDE),
-                                        (dict(vh=12), BAD_STRIDE), (dict(k=P + 8), MISALIGNED), (dict(v=P + 4), MISALIGNED)])
+                                        (dict(kt=1 << 27), BAD_STRIDE), (dict(vt=1 << 30), BAD_STRIDE), (dict(vh=12), BAD_STRIDE),
+                                        (dict(k=P + 8), MISALIGNED), (dict(v=P + 4), MISALIGNED)])
 def test_prompts_that_are_refused(bad, status):
     assert prompt(**bad) == status
 
