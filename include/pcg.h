@@ -574,8 +574,8 @@ size_t pcg_cache_attend_workspace_bytes(int32_t B, int64_t T, int32_t heads, int
 
 /*
  * The same for whole prompts, packed one behind the other: rows q_start[b] .. q_start[b + 1] of q, k and v are request b's
- * tokens, at positions 0, 1, ..  Types, strides, scale, window and empty rows as above (k and v: eight tokens within 2 GiB of each
- * other); needs no workspace.  `longest` is the longest prompt's tokens, as near as the caller knows: where one is long beside the
+ * tokens, at positions 0, 1, ..  Types, strides, scale, window and empty rows as above (k and v: sixteen tokens within 2 GiB of
+ * each other); needs no workspace.  `longest` is the longest prompt's tokens, as near as the caller knows: where one is long beside the
  * load of the whole chip, the work is cut finer.
  */
 int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt, int64_t T, int32_t heads, int32_t kv_heads,

@@ -172,33 +172,50 @@ __device__ __forceinline__ int32_t request_ctx(const AttendArgs &a, int32_t b) {
 __device__ __forceinline__ uint32_t lds_address(const unsigned char *p) {
   return (uint32_t) (uintptr_t) (const __attribute__((address_space(3))) unsigned char *) p;
 }
-__device__ __forceinline__ void bring(const char *base, uint32_t offset, const unsigned char *to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-               :: "v"(offset), "s"(base), "s"(lds_address(to)) : "memory");
-}
 __device__ __forceinline__ void bring(const char *from, const unsigned char *to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :: "v"(from), "s"(lds_address(to)) : "memory");
 }
+// N of them to N KB in a row, load i from base + offset[i] - kBias + 1024 i: what an instruction's own offset adds to the place in
+// LDS it adds to the address as well.
+constexpr uint32_t kBias = 3072;
+template <int N>
+__device__ __forceinline__ void bring_some(const char *base, const uint32_t *offset, const unsigned char *to) {
+  static_assert(N == 1 || N == 2 || N == 4, "");
+  const uint32_t m = lds_address(to);
+  base -= kBias;
+  if constexpr (N == 4) {
+    asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
+                 :: "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base), "s"(m) : "memory");
+  } else if constexpr (N == 2) {
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
+                 :: "v"(offset[0]), "v"(offset[1]), "s"(base), "s"(m) : "memory");
+  } else {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset[0]), "s"(base), "s"(m) : "memory");
+  }
+}
 
-// Brings ROWS keys or values of a unit, beginning at key k0, into LDS: loads of 16 bytes a lane, 1024 bytes of LDS in a row each,
-// dealt to NW waves.  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
-// multiple of 32) share a page, which the scalar unit looks up; 2: pages of any size.  Columns behind D get the row's first ones: keys are cleared there
-// once they are in, values make columns that nobody stores.
+// Brings ROWS keys or values of a unit, beginning at key k0, into LDS, dealt to NW waves: keys in a row to each, loads of
+// 16 bytes a lane.  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
+// multiple of 32) share a page, which the scalar unit looks up; 2: pages of any size.  Columns behind D get the row's first ones: keys are
+// cleared there once they are in, values make columns that nobody stores.
 template <typename T, int DP, int ROWS, int NW, int PAGES>
 struct Loader {
   using S = Shape<T, DP>;
-  static constexpr int NI = ROWS / S::RPI / NW;                       // loads of a wave
-  static constexpr int kStep = S::RPI * NW;                           // keys from one of its loads to the next
-  static constexpr int NK = kStep < 16 ? 16 / kStep : 1;              // after so many the order of chunks repeats
-  static constexpr int NV = kStep < (S::kBf16 ? 4 : 8) ? (S::kBf16 ? 4 : 8) / kStep : 1;
+  static constexpr int kRows = ROWS / NW;                             // keys of a wave
+  static constexpr int NI = kRows / S::RPI;                           // its loads
+  static constexpr int NG = kRows > 16 ? kRows / 16 : 1;              // its groups of 16 keys, or what there are
+  static constexpr int NL = NI / NG;                                  // loads of a group
+  static constexpr int kAtOnce = NL < 4 ? NL : 4;
   const AttendArgs &a;
   const Unit &u;
   const int lane, wave;
   const int32_t *table;
   const char *kb, *vb;
-  uint32_t koff[NK], voff[NV];       // of this lane from the first of a load's keys
+  uint32_t koff[NL], voff[NL];       // of this lane from the first key of a group, see bring_some
 
+  __device__ __forceinline__ int row_of(int i) const { return wave * kRows + i * S::RPI + lane / S::CH; }
   template <bool VALUES>
   __device__ __forceinline__ int chunk(int row) const {
     const int pos = lane % S::CH;
@@ -209,32 +226,28 @@ struct Loader {
   __device__ __forceinline__ void clear_keys(unsigned char *tile) const {
     if (a.D == DP) return;
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
-      if (key_swap<S::RB>(j * kStep + wave * S::RPI + lane / S::CH, lane % S::CH) * S::E >= a.D)
-        *reinterpret_cast<u32x4 *>(tile + (j * NW + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+    for (int i = 0; i < NI; ++i)
+      if (key_swap<S::RB>(row_of(i), lane % S::CH) * S::E >= a.D)
+        *reinterpret_cast<u32x4 *>(tile + (wave * NI + i) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
   }
   __device__ __forceinline__ Loader(const AttendArgs &a_, const Unit &u_, int lane_, int wave_)
       : a(a_), u(u_), lane(lane_), wave(wave_), table(PAGES ? a_.table + (int64_t) u_.b * a_.table_stride : nullptr) {
     kb = reinterpret_cast<const char *>(a.k) + (int64_t) u.head * a.k_head * (int) sizeof(T);
     vb = reinterpret_cast<const char *>(a.v) + (int64_t) u.head * a.v_head * (int) sizeof(T);
-    const int row_in = lane / S::CH;
 #pragma unroll
-    for (int j = 0; j < NK; ++j)
-      koff[j] = (uint32_t) (row_in * (int32_t) a.k_tok + chunk<false>(j * kStep + wave * S::RPI + row_in) * S::E) * (uint32_t) sizeof(T);
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      voff[j] = (uint32_t) (row_in * (int32_t) a.v_tok + chunk<true>(j * kStep + wave * S::RPI + row_in) * S::E) * (uint32_t) sizeof(T);
+    for (int i = 0; i < NL; ++i) {
+      const uint32_t in = (uint32_t) (i * S::RPI + lane / S::CH), bias = kBias - (uint32_t) (i % kAtOnce) * 1024;
+      koff[i] = (in * (uint32_t) a.k_tok + (uint32_t) (chunk<false>(row_of(i)) * S::E)) * (uint32_t) sizeof(T) + bias;
+      voff[i] = (in * (uint32_t) a.v_tok + (uint32_t) (chunk<true>(row_of(i)) * S::E)) * (uint32_t) sizeof(T) + bias;
+    }
   }
 
-  // Pages of the keys from k0 on, asked for ahead of their use: of 16 keys each (PAGES 1), of each load of this lane (PAGES 2).
-  static constexpr int kShared = kStep < 16 ? 16 / kStep : 1;          // loads of a wave from the same 16 keys
-  static constexpr int NP = PAGES == 2 ? NI : NI / kShared;
+  // Pages of the keys from k0 on, asked for ahead of their use: of a group (PAGES 1), of each load of this lane (PAGES 2).
+  static constexpr int NP = PAGES == 2 ? NI : NG;
   struct Pages {
     int32_t page[NP];
   };
-  __device__ __forceinline__ int32_t key_of(int32_t k0, int i) const {
-    return PAGES == 2 ? k0 + i * kStep + wave * S::RPI + lane / S::CH : k0 + i * kShared * kStep + wave * S::RPI;
-  }
+  __device__ __forceinline__ int32_t key_of(int32_t k0, int i) const { return k0 + (PAGES == 2 ? row_of(i) : wave * kRows + 16 * i); }
   __device__ __forceinline__ Pages look_up(int32_t k0) const {
     Pages p;
 #pragma unroll
@@ -251,42 +264,40 @@ struct Loader {
     const char *base = VALUES ? vb : kb;
     // of a cache keys and values have the same strides
     const int64_t tok = VALUES && !PAGES ? a.v_tok : a.k_tok;
-    int64_t at[NP];
+    const char *from[NP];
     bool valid[NP], whole = PAGES < 2 && k0 + ROWS <= u.k_hi;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int32_t key = key_of(k0, i);
+      valid[i] = key < u.k_hi;
       if constexpr (PAGES) {
         uint32_t block, slot;
         split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
-        valid[i] = key < u.k_hi && block < (uint32_t) a.max_blocks && (uint32_t) p.page[i] < (uint32_t) a.num_pages;
+        valid[i] = valid[i] && block < (uint32_t) a.max_blocks && (uint32_t) p.page[i] < (uint32_t) a.num_pages;
         whole = whole && valid[i];
-        at[i] = (int64_t) p.page[i] * a.k_page + (int64_t) slot * tok;
+        from[i] = base + ((int64_t) p.page[i] * a.k_page + (int64_t) slot * tok) * (int) sizeof(T);
       } else {
-        valid[i] = key < u.k_hi;
-        at[i] = (int64_t) (u.first + key) * tok;
+        from[i] = base + (int64_t) (u.first + key) * tok * (int) sizeof(T);
       }
     }
+    unsigned char *to = tile + wave * NI * 1024;
     if (whole) {
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
-        bring(base + (at[j / kShared % NP] + (j % kShared) * kStep * tok) * (int) sizeof(T), VALUES ? voff[j % NV] : koff[j % NK],
-              tile + (j * NW + wave) * 1024);
+      for (int i = 0; i < NI; i += kAtOnce) bring_some<kAtOnce>(from[i / NL % NP], (VALUES ? voff : koff) + i % NL, to + i * 1024);
     } else {
       // a unit's last tile, pages of odd sizes or outside the cache: zeros where there is no key
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int row = j * kStep + wave * S::RPI + lane / S::CH;
-        const char *from;
+      for (int i = 0; i < NI; ++i) {
+        const char *at;
         bool there;
         if constexpr (PAGES == 2) {
-          there = valid[j];
-          from = base + (at[j] + chunk<VALUES>(row) * S::E) * (int) sizeof(T);
+          there = valid[i];
+          at = from[i] + chunk<VALUES>(row_of(i)) * 16;
         } else {
-          there = valid[j / kShared] && k0 + row < u.k_hi;
-          from = base + (at[j / kShared] + (j % kShared) * kStep * tok) * (int) sizeof(T) + (VALUES ? voff[j % NV] : koff[j % NK]);
+          there = valid[i / NL] && k0 + row_of(i) < u.k_hi;
+          at = from[i / NL] + (int64_t) (VALUES ? voff : koff)[i % NL] - kBias + i % NL % kAtOnce * 1024;
         }
-        bring(there ? from : reinterpret_cast<const char *>(&kZeros), tile + (j * NW + wave) * 1024);
+        bring(there ? at : reinterpret_cast<const char *>(&kZeros), to + i * 1024);
       }
     }
   }
@@ -1324,9 +1335,8 @@ hipError_t go_thin(const AttendArgs &a, bool shared_pages, void *workspace, hipS
 
 template <typename T, int DP>
 hipError_t go_cache(const AttendArgs &a, int64_t longest, void *workspace, hipStream_t stream) {
-  using S = Shape<T, DP>;
-  // 16 keys share a page, and those of a load lie within 32 bits of each other
-  const bool shared_pages = a.page_size % 16 == 0 && a.k_tok * S::RPI * (int64_t) sizeof(T) < (int64_t) 1 << 31;
+  // 16 keys share a page, and lie within 32 bits of each other
+  const bool shared_pages = a.page_size % 16 == 0 && a.k_tok * 16 * (int64_t) sizeof(T) < (int64_t) 1 << 31;
   const int64_t rows = longest * a.G;
   if (rows <= 32) return go_thin<T, DP, 1>(a, shared_pages, workspace, stream);
   if (rows <= 64) return go_thin<T, DP, 2>(a, shared_pages, workspace, stream);

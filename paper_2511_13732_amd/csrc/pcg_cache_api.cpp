@@ -219,8 +219,8 @@ int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt,
   if (!stride16(k_tok_stride, dt, T == 1) || !stride16(v_tok_stride, dt, T == 1) ||
       !stride16(k_head_stride, dt, kv_heads == 1) || !stride16(v_head_stride, dt, kv_heads == 1))
     return PCG_ERR_BAD_STRIDE;
-  // a load brings up to eight tokens' keys, whose offsets from the first are counted in 32 bits
-  if (T > 1 && std::max(k_tok_stride, v_tok_stride) * 8 * elem_bytes(dt) >= kInt31) return PCG_ERR_BAD_STRIDE;
+  // sixteen tokens' keys at a time, whose offsets from the first are counted in 32 bits
+  if (T > 1 && std::max(k_tok_stride, v_tok_stride) * 16 * elem_bytes(dt) >= kInt31) return PCG_ERR_BAD_STRIDE;
   if (!aligned(k, 16) || !aligned(v, 16)) return PCG_ERR_MISALIGNED;
   a.k = k;
   a.v = v;
