@@ -179,25 +179,34 @@ __device__ __forceinline__ void bring(const char *from, const unsigned char *to)
 // N of them to N KB in a row, load i from base + offset[i] - kBias + 1024 i: what an instruction's own offset adds to the place in
 // LDS it adds to the address as well.
 constexpr uint32_t kBias = 3072;
-template <int N>
+// ONCE: what is read is not read again by others, and need not stay in the caches.
+#define PCG_BRING(HINT) \
+  if constexpr (N == 4) { \
+    asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4" HINT "\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024" HINT \
+                 "\n\tglobal_load_lds_dwordx4 %2, %4 offset:2048" HINT "\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072" HINT \
+                 :: "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base), "s"(m) : "memory"); \
+  } else if constexpr (N == 2) { \
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" HINT "\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024" HINT \
+                 :: "v"(offset[0]), "v"(offset[1]), "s"(base), "s"(m) : "memory"); \
+  } else { \
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" HINT :: "v"(offset[0]), "s"(base), "s"(m) : "memory"); \
+  }
+template <int N, bool ONCE>
 __device__ __forceinline__ void bring_some(const char *base, const uint32_t *offset, const unsigned char *to) {
   static_assert(N == 1 || N == 2 || N == 4, "");
   const uint32_t m = lds_address(to);
   base -= kBias;
-  if constexpr (N == 4) {
-    asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
-                 "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
-                 :: "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base), "s"(m) : "memory");
-  } else if constexpr (N == 2) {
-    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
-                 :: "v"(offset[0]), "v"(offset[1]), "s"(base), "s"(m) : "memory");
+  if constexpr (ONCE) {
+    PCG_BRING(" nt")
   } else {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset[0]), "s"(base), "s"(m) : "memory");
+    PCG_BRING("")
   }
 }
+#undef PCG_BRING
 
 // Brings ROWS keys or values of a unit, beginning at key k0, into LDS, dealt to NW waves: keys in a row to each, loads of
-// 16 bytes a lane.  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
+// 16 bytes a lane.  (A wave that has keys of its own is the only one to read them: past the caches, 2 x 120 000 tokens took 171 us
+// instead of 196, 64 sequences of 9 new tokens 89 instead of 98; where others read them too, prompts by pieces, 379 instead of 324.)  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
 // multiple of 32) share a page, which the scalar unit looks up; 2: pages of any size.  Columns behind D get the row's first ones: keys are
 // cleared there once they are in, values make columns that nobody stores.
 template <typename T, int DP, int ROWS, int NW, int PAGES>
@@ -283,7 +292,7 @@ struct Loader {
     unsigned char *to = tile + wave * NI * 1024;
     if (whole) {
 #pragma unroll
-      for (int i = 0; i < NI; i += kAtOnce) bring_some<kAtOnce>(from[i / NL % NP], (VALUES ? voff : koff) + i % NL, to + i * 1024);
+      for (int i = 0; i < NI; i += kAtOnce) bring_some<kAtOnce, NW == 1>(from[i / NL % NP], (VALUES ? voff : koff) + i % NL, to + i * 1024);
     } else {
       // a unit's last tile, pages of odd sizes or outside the cache: zeros where there is no key
 #pragma unroll
