@@ -1267,27 +1267,32 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
     const Row w = row_at(a, u, j.r0 + row);
     vec o = {};
     float sum = 0.f, top = -INFINITY;
+    vec x[kAtOnce];
+    auto ask = [&](int32_t p0, int32_t i, int32_t n) {
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+        x[k] = *reinterpret_cast<const vec *>(&part_at(p0 + min(i + 2 * k + half, n - 1)).o[row][l32 * kEach]);
+    };
     for (int32_t p0 = 0; p0 < j.parts; p0 += kWave) {
-      // references and sums of 64 parts, one a lane
+      // references and sums of 64 parts, one a lane, and the first outputs beside them
       const int32_t n = min(j.parts - p0, kWave);
       const Part<DP, R> &mine = part_at(p0 + min(lane, n - 1));
-      const float ref = lane < n ? mine.ref[row] : -INFINITY;
+      const float mine_ref = mine.ref[row], mine_sum = mine.sum[row];
+      ask(p0, 0, n);
+      const float ref = lane < n ? mine_ref : -INFINITY;
       const float now = fmaxf(top, wave_max(ref));
       const float before = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
       const float f = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
       top = now;
-      sum = sum * before + (lane < n ? f * mine.sum[row] : 0.f);
+      sum = sum * before + (lane < n ? f * mine_sum : 0.f);
       o *= before;
       for (int32_t i = 0; i < n; i += 2 * kAtOnce) {
-        vec x[kAtOnce];
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k)
-          x[k] = *reinterpret_cast<const vec *>(&part_at(p0 + min(i + 2 * k + half, n - 1)).o[row][l32 * kEach]);
+        if (i) ask(p0, i, n);
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
           const int32_t p = i + 2 * k + half;
           const float fp = __shfl(f, min(p, n - 1));
-    #pragma unroll
+#pragma unroll
           for (int e = 0; e < kEach; ++e) o[e] = p < n ? fmaf(fp, x[k][e], o[e]) : o[e];
         }
       }
