@@ -9,9 +9,10 @@
 // the weights never pass through LDS.  One pass with the running maximum and sum of the softmax, in float32;
 // products accumulate in float32.
 //
-// Two kernels.  attend_thick_kernel: 128 rows a workgroup, 32 a wave, the four waves share tiles of keys and values in
-// LDS (prompts, long chunks: bound by the matrix and vector units).  attend_thin_kernel: 32 or 64 rows a workgroup, each wave
-// streams keys of its own (a step's chunks, single tokens: bound by memory).  Keys and values go from memory straight into LDS.
+// Keys and values go from memory straight into LDS.  attend_thick_kernel (a cache) and attend_prompt_kernel (prompts beside their
+// keys) let the four waves of a workgroup share tiles of keys: 128 rows, 32 a wave, or 64 rows, two waves on the two halves of a
+// tile.  attend_thin_kernel: 32 rows of float32, each wave with keys of its own.  A cache's keys are split over the whole chip in
+// runs of equal length (see Run), and attend_join_kernel joins the rows of what was split.
 #include <math.h>
 
 #include "pcg_attend.h"
@@ -37,8 +38,8 @@ constexpr int kAttendThreads = kAttendWaves * kWave;
 constexpr int kThickRows = 32 * kAttendWaves;
 constexpr int kThinKeys = 32 * kAttendWaves;      // keys a turn of the four waves takes
 constexpr int kCUs = 256;
-constexpr int kThinLeast = 1, kThickLeast = 5;     // length of a workgroup's run, at least (see Run)
-constexpr int kThinCost = 1, kThickCost = 1;
+// See Run.  kCost 0, 1, 2, 4: 64 sequences with 9 new tokens 102, 97, 100, 99 us.
+constexpr int kCost = 1, kThinLeast = 1;
 constexpr int kJoinThreads = 256;
 constexpr float kLag = 8.f;        // how far (in powers of two) a maximum may run ahead of the one in use
 
@@ -178,15 +179,17 @@ __device__ __forceinline__ void bring(const char *from, const unsigned char *to)
 }
 // N of them to N KB in a row, load i from base + offset[i] - kBias + 1024 i: what an instruction's own offset adds to the place in
 // LDS it adds to the address as well.
-constexpr uint32_t kBias = 3072;
-// ONCE: what is read is not read again by others, and need not stay in the caches.
+constexpr uint32_t kBias = 3 * 1024;
+// ONCE: what is read is not read again by others, and need not stay in the caches.  us with the hint and without: 32 sequences of
+// 4000 keys with 9 new tokens 103 and 117, with 17 111 and 128; 2 of 120 000 with 9 158 and 178; 8 of 2000, which the caches would
+// have kept from call to call, 30 and 29; prompts by pieces, whose keys others read too, 370 and 316.
 #define PCG_BRING(HINT) \
   if constexpr (N == 4) { \
-    asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4" HINT "\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024" HINT \
-                 "\n\tglobal_load_lds_dwordx4 %2, %4 offset:2048" HINT "\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072" HINT \
+    asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4" HINT "\n\tglobal_load_lds_dwordx4 %1, %4 offset:0x400" HINT \
+                 "\n\tglobal_load_lds_dwordx4 %2, %4 offset:0x800" HINT "\n\tglobal_load_lds_dwordx4 %3, %4 offset:0xc00" HINT \
                  :: "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base), "s"(m) : "memory"); \
   } else if constexpr (N == 2) { \
-    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" HINT "\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024" HINT \
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" HINT "\n\tglobal_load_lds_dwordx4 %1, %2 offset:0x400" HINT \
                  :: "v"(offset[0]), "v"(offset[1]), "s"(base), "s"(m) : "memory"); \
   } else { \
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" HINT :: "v"(offset[0]), "s"(base), "s"(m) : "memory"); \
@@ -205,11 +208,11 @@ __device__ __forceinline__ void bring_some(const char *base, const uint32_t *off
 #undef PCG_BRING
 
 // Brings ROWS keys or values of a unit, beginning at key k0, into LDS, dealt to NW waves: keys in a row to each, loads of
-// 16 bytes a lane.  (A wave that has keys of its own is the only one to read them: past the caches, 2 x 120 000 tokens took 171 us
-// instead of 196, 64 sequences of 9 new tokens 89 instead of 98; where others read them too, prompts by pieces, 379 instead of 324.)  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
-// multiple of 32) share a page, which the scalar unit looks up; 2: pages of any size.  Columns behind D get the row's first ones: keys are
-// cleared there once they are in, values make columns that nobody stores.
-template <typename T, int DP, int ROWS, int NW, int PAGES>
+// 16 bytes a lane.  PAGES 0: the batch's own rows; 1: pages of a multiple of 16 slots, so that 16 keys in a row (k0 is a
+// multiple of 32) share a page, which the scalar unit looks up; 2: pages of any size, looked up by each lane.  ONCE: no other
+// workgroup reads them, see bring_some.  Columns behind D get the row's first ones: keys are cleared there once they are in, values
+// make columns that nobody stores.
+template <typename T, int DP, int ROWS, int NW, int PAGES, bool ONCE>
 struct Loader {
   using S = Shape<T, DP>;
   static constexpr int kRows = ROWS / NW;                             // keys of a wave
@@ -292,7 +295,7 @@ struct Loader {
     unsigned char *to = tile + wave * NI * 1024;
     if (whole) {
 #pragma unroll
-      for (int i = 0; i < NI; i += kAtOnce) bring_some<kAtOnce, NW == 1>(from[i / NL % NP], (VALUES ? voff : koff) + i % NL, to + i * 1024);
+      for (int i = 0; i < NI; i += kAtOnce) bring_some<kAtOnce, ONCE>(from[i / NL % NP], (VALUES ? voff : koff) + i % NL, to + i * 1024);
     } else {
       // a unit's last tile, pages of odd sizes or outside the cache: zeros where there is no key
 #pragma unroll
@@ -334,34 +337,16 @@ __device__ __forceinline__ u32x4 key_chunk(const unsigned char *lk, int base, in
   return *reinterpret_cast<const u32x4 *>(lk + key_at<RB>(base + (lane & 31), 2 * i + (lane >> 5)));
 }
 
-// Scores of KB blocks of 32 keys of a tile: register 4 j + i of a block is its key 8 j + 4 half + i.  Queries in
-// registers, or of RB blocks of rows in LDS, laid out as keys are.
-template <typename T, int DP, int KB>
-__device__ __forceinline__ void scores(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[KB],
+// Scores of 32 keys: register 4 j + i is key 8 j + 4 half + i.
+template <typename T, int DP>
+__device__ __forceinline__ void scores(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[1],
                                        int32_t D) {
   using S = Shape<T, DP>;
-#pragma unroll
-  for (int k = 0; k < KB; ++k) {
-    s[k] = floatx16{};
-#pragma unroll
-    for (int i = 0; i < S::NQ; ++i) {
-      if (beyond<T>(i * 2 * S::E, D)) break;
-      multiply<S::kBf16>(s[k], key_chunk<S::RB>(lk, 32 * k, lane, i), qf[i]);
-    }
-  }
-}
-template <typename T, int DP, int RB>
-__device__ __forceinline__ void scores(const unsigned char *lk, const unsigned char *lq, int lane, floatx16 (&s)[RB], int32_t D) {
-  using S = Shape<T, DP>;
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) s[rb] = floatx16{};
+  s[0] = floatx16{};
 #pragma unroll
   for (int i = 0; i < S::NQ; ++i) {
     if (beyond<T>(i * 2 * S::E, D)) break;
-    const u32x4 kf = key_chunk<S::RB>(lk, 0, lane, i);
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) multiply<S::kBf16>(s[rb], kf, key_chunk<S::RB>(lq, rb * 32, lane, i));
-    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);         // not all operands in registers at a time
+    multiply<S::kBf16>(s[0], key_chunk<S::RB>(lk, 0, lane, i), qf[i]);
   }
 }
 
@@ -418,7 +403,7 @@ __device__ __forceinline__ void to_weights(floatx16 (&s)[KB], float c, float min
 // Nothing moves across: the order of instructions around it is the one written.
 __device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
-// scores in steps of one operand of keys, read kAhead steps ahead.
+// The same of KB blocks of 32 keys, in steps of one operand of keys that is read kAhead steps ahead.
 template <typename T, int DP, int KB>
 __device__ __forceinline__ void scores_in_steps(const unsigned char *lk, int lane, const u32x4 (&qf)[Shape<T, DP>::NQ], floatx16 (&s)[KB],
                                                 int32_t D) {
@@ -469,38 +454,19 @@ __device__ __forceinline__ float value_of(const unsigned char *lv, int base, int
   return *reinterpret_cast<const float *>(lv + value_at<RB, false>(row, d >> 2) + (d & 3) * 4);
 }
 
-// Adds weights times values of 32 keys, the first at row `base` of the tile, for RB blocks of rows.
-template <typename T, int DP, int RB>
-__device__ __forceinline__ void add_values(const unsigned char *lv, int base, int lane, const floatx16 (&p)[RB],
-                                           floatx16 (&o)[RB][Shape<T, DP>::NO], int32_t D) {
-  using S = Shape<T, DP>;
-  if constexpr (S::kBf16) {
+// Adds weights times values of 32 keys.
+template <int DP>
+__device__ __forceinline__ void add_values(const unsigned char *lv, int lane, const floatx16 &p, floatx16 (&o)[DP / 32], int32_t D) {
 #pragma unroll
-    for (int c16 = 0; c16 < 2; ++c16) {
-      bf16x8 pf[RB];
+  for (int r = 0; r < 16; ++r)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) pf[rb] = weights_of(p[rb], c16);
-#pragma unroll
-      for (int m = 0; m < S::NO; ++m) {
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, values_of<S::RB>(lv, base + c16 * 16, lane, m));
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) o[rb][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[rb], o[rb][m], 0, 0, 0);
-      }
+    for (int m = 0; m < DP / 32; ++m) {
+      if (beyond<float>(32 * m, D)) break;
+      o[m] = __builtin_amdgcn_mfma_f32_32x32x2f32(value_of<DP * 4>(lv, 0, lane, r, m), p[r], o[m], 0, 0, 0);
     }
-  } else {
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-      for (int m = 0; m < S::NO; ++m) {
-        if (beyond<T>(32 * m, D)) break;
-        const float x = value_of<S::RB>(lv, base, lane, r, m);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) o[rb][m] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[rb][r], o[rb][m], 0, 0, 0);
-      }
-  }
 }
 
-// The same for KB blocks of 32 keys and one block of rows, in steps with the operands read ahead.
+// The same of KB blocks of 32 keys, in steps with the operands read ahead.
 template <typename T, int DP, int KB>
 __device__ __forceinline__ void add_values_in_steps(const unsigned char *lv, int lane, const floatx16 (&p)[KB],
                                                     floatx16 (&o)[Shape<T, DP>::NO], int32_t D) {
@@ -690,7 +656,7 @@ __device__ __forceinline__ int32_t unit_tiles(const AttendArgs &a, Unit &u) {
   return (u.k_hi - u.k_lo + TK - 1) / TK;
 }
 
-// All units (requests, their shared heads, their row blocks, in this order) in a row, COST for what a unit costs beside its tiles
+// All units (requests, their shared heads, their row blocks, in this order) in a row, kCost for what a unit costs beside its tiles
 // and then 1 for each of them, are cut into `runs` runs of a length, one a workgroup; the first `longer` are one longer than `each`.
 struct Run {
   int32_t runs, longer, index;
@@ -712,7 +678,7 @@ struct Run {
 // Every workgroup adds the requests up by itself, a quarter of them a wave, a request a lane or (with many row blocks) a row block
 // a lane: for 64 requests that takes two microseconds, less than a launch ahead would.  Lengths are whole numbers below 2^53 in
 // double, whose running sums go through DPP.
-template <int R, int TK, int LEAST, int COST>
+template <int R, int TK, int LEAST>
 __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsigned char *lds, Unit &u, int64_t &into) {
   double *sums = reinterpret_cast<double *>(lds);
   int32_t *found = reinterpret_cast<int32_t *>(sums + kAttendWaves);
@@ -727,7 +693,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
       v.ctx = request_ctx(a, v.b);
     }
     v.r0 = 0;
-    one = v.rows > 0 && v.rows <= R ? unit_tiles<R, TK>(a, v) + COST : 0;
+    one = v.rows > 0 && v.rows <= R ? unit_tiles<R, TK>(a, v) + kCost : 0;
     for (uint64_t many = __builtin_amdgcn_ballot_w64(v.rows > R); many; many &= many - 1) {
       const int l = __ffsll((long long) many) - 1;
       Unit x;
@@ -736,7 +702,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
       double all = 0;
       for (int64_t r0 = (int64_t) lane * R; r0 < x.rows; r0 += kWave * R) {
         x.r0 = (int32_t) r0;
-        all += unit_tiles<R, TK>(a, x) + COST;
+        all += unit_tiles<R, TK>(a, x) + kCost;
       }
       all = wave_sum(all);
       if (lane == l) one = all;
@@ -798,7 +764,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
       for (int64_t c0 = 0; c0 < x.rows && x.rows > R; c0 += kWave * R) {
         const int64_t mine_r0 = c0 + (int64_t) lane * R;
         x.r0 = (int32_t) mine_r0;
-        const double t = mine_r0 < x.rows ? unit_tiles<R, TK>(a, x) + COST : 0, blocks = wave_scan(t);
+        const double t = mine_r0 < x.rows ? unit_tiles<R, TK>(a, x) + kCost : 0, blocks = wave_scan(t);
         const uint64_t in = __builtin_amdgcn_ballot_w64(blocks > ahead);
         if (in) {
           const int k = __ffsll((long long) in) - 1;
@@ -849,23 +815,23 @@ __device__ __forceinline__ void next_unit(const AttendArgs &a, Unit &u) {
 
 // Calls work(unit, first tile, tiles, part) for every unit or piece of one in this workgroup's run; part: NULL where the unit is
 // whole.  A workgroup has two places for parts: 1 for the unit that it begins and does not finish, 0 for one that another began.
-template <int DP, int R, int TK, int LEAST, int COST, typename Work>
+template <int DP, int R, int TK, int LEAST, typename Work>
 __device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *lds, Join *join, Part<DP, R> *parts, Work work) {
   Unit u;
   int64_t into = 0;
-  Run run = find_run<R, TK, LEAST, COST>(a, (int32_t) gridDim.x, lds, u, into);
+  Run run = find_run<R, TK, LEAST>(a, (int32_t) gridDim.x, lds, u, into);
   Join j{0, 0, 0, 0, 0};
   while (run.left > 0) {
     u = scalar(u);
     const int32_t all = scalar(unit_tiles<R, TK>(a, u));
-    const int64_t until = min((int64_t) all + COST, into + run.left);       // in the unit's length
-    const int32_t tile = into > COST ? (int32_t) into - COST : 0, tiles = until > COST ? (int32_t) until - COST - tile : 0;
+    const int64_t until = min((int64_t) all + kCost, into + run.left);       // in the unit's length
+    const int32_t tile = into > kCost ? (int32_t) into - kCost : 0, tiles = until > kCost ? (int32_t) until - kCost - tile : 0;
     run.left -= until - into;
     if (tiles > 0) {
       Part<DP, R> *part = tiles == all ? nullptr : parts + 2 * (int64_t) run.index + (tile == 0);
       if (part && tile == 0) {
         // this run and those that begin ahead of the unit's end
-        j.parts = run.ahead_of(run.begin(run.index + 1) - run.left + all + COST - until) - run.index;
+        j.parts = run.ahead_of(run.begin(run.index + 1) - run.left + all + kCost - until) - run.index;
         j.head = u.head;
         j.r0 = u.r0;
         j.rows = u.rows;
@@ -923,9 +889,13 @@ struct Thick {
   static constexpr int TK = 32 * KB * WK;
   static constexpr int kTile = TK * S::RB;
   static constexpr int kLds = 4 * kTile;            // keys and values, two of each
+  static constexpr int kRuns = 2 * kLds < 160 * 1024 ? 512 : 256;        // what fits the chip at a time
+  // See Run.  us with runs of 1, 2, 3 and 5 tiles at least, bf16, d = 128: 64 rows, 1 sequence of 1000 keys 13.6 14.5 18.1 20.6, of
+  // 8000 27 27 25 24, 8 of 2000 24 24 24 24; 128 rows, 1 of 1000 18 18 21 24, of 8000 39 39 32 28, 4 of 4000 (d = 64) 27 27 27 27.
+  static constexpr int kLeast = WK == 1 ? 5 : 1;
 };
 
-template <typename T, int DP, int WK, int PAGES>
+template <typename T, int DP, int WK, int PAGES, bool ONCE>
 __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
                                             int *odd, int turn, Part<DP, Thick<T, DP, WK>::R> *part) {
   using S = Shape<T, DP>;
@@ -935,7 +905,7 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
   asm("" : "+v"(tid));                  // what follows from it is formed here, not kept in registers from piece to piece
   const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
-  const Loader<T, DP, W::TK, kAttendWaves, PAGES> loader(a, u, lane, wave);
+  const Loader<T, DP, W::TK, kAttendWaves, PAGES, ONCE> loader(a, u, lane, wave);
   int32_t k0 = u.k_lo + tile * W::TK;
   const int32_t end = min(u.k_hi, k0 + tiles * W::TK);
   unsigned char *cur = lds, *nxt = lds + 2 * W::kTile;
@@ -1018,13 +988,14 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
   else store_row<T, DP>(a, w, half, o, sum);
 }
 
-template <typename T, int DP, int PAGES>
-__global__ __launch_bounds__(kAttendThreads, 2) void attend_thick_kernel(AttendArgs a, Join *join,
-                                                                         Part<DP, kThickRows> *parts) {
-  __shared__ __align__(16) unsigned char lds[Thick<T, DP, 1>::kLds];
+template <typename T, int DP, int WK, int PAGES, bool ONCE>
+__global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) void attend_thick_kernel(AttendArgs a, Join *join,
+                                                                                                       Part<DP, Thick<T, DP, WK>::R> *parts) {
+  using W = Thick<T, DP, WK>;
+  __shared__ __align__(16) unsigned char lds[W::kLds];
   __shared__ int odd;
-  work_on_run<DP, kThickRows, Thick<T, DP, 1>::TK, kThickLeast, kThickCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, kThickRows> *part) {
-    thick_piece<T, DP, 1, PAGES>(a, u, tile, tiles, lds, &odd, (int) blockIdx.x / kCUs, part);
+  work_on_run<DP, W::R, W::TK, W::kLeast>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
+    thick_piece<T, DP, WK, PAGES, ONCE>(a, u, tile, tiles, lds, &odd, (int) blockIdx.x / kCUs, part);
   });
 }
 
@@ -1074,7 +1045,7 @@ __device__ __forceinline__ bool find_prompt_unit(const AttendArgs &a, int32_t ra
 }
 
 template <typename T, int DP, int WK>
-__global__ __launch_bounds__(kAttendThreads, (2 * Thick<T, DP, WK>::kLds < 160 * 1024 ? 2 : 1)) void attend_prompt_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) void attend_prompt_kernel(AttendArgs a) {
   using W = Thick<T, DP, WK>;
   __shared__ __align__(16) unsigned char lds[W::kLds];
   __shared__ int odd;
@@ -1087,61 +1058,44 @@ __global__ __launch_bounds__(kAttendThreads, (2 * Thick<T, DP, WK>::kLds < 160 *
   if (!find_prompt_unit<W::R>(a, (int32_t) (rank / (uint32_t) a.heads_kv), u)) return;
   u.head = (int32_t) (rank % (uint32_t) a.heads_kv);
   const int32_t tiles = unit_tiles<W::R, W::TK>(a, u);
-  thick_piece<T, DP, WK, 0>(a, scalar(u), 0, scalar(tiles), lds, &odd, (int) round, nullptr);
+  thick_piece<T, DP, WK, 0, false>(a, scalar(u), 0, scalar(tiles), lds, &odd, (int) round, nullptr);
 }
 
-// ---- 32 or 64 rows a workgroup -----------------------------------------------------------------------------------------
+// ---- 32 rows of float32 a workgroup ------------------------------------------------------------------------------------
 
-template <typename T, int DP, int RB>
+template <int DP>
 struct Thin {
-  using S = Shape<T, DP>;
-  static constexpr int R = 32 * RB;
-  static constexpr int kTile = 32 * S::RB;
-  static constexpr int kQueries = RB > 1 ? R * S::RB : 0;       // two blocks' queries do not fit the registers
-  static constexpr int kLds = kAttendWaves * 2 * kTile + kQueries;
+  static constexpr int R = 32;
+  static constexpr int kTile = 32 * DP * 4;
+  static constexpr int kLds = kAttendWaves * 2 * kTile;
   static_assert(2 * R * (DP + 2) * 4 <= kLds, "two waves' rows on their way to the others");
   static constexpr int kRuns = 2 * kLds <= 160 * 1024 ? 512 : 256;       // what fits the chip at a time
 };
 
-template <typename T, int DP, int RB, int PAGES>
+template <int DP, int PAGES>
 __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
-                                           Part<DP, 32 * RB> *part) {
-  using S = Shape<T, DP>;
-  using W = Thin<T, DP, RB>;
+                                           Part<DP, 32> *part) {
+  using S = Shape<float, DP>;
+  using W = Thin<DP>;
   int tid = threadIdx.x;
   asm("" : "+v"(tid));                  // what follows from it is formed here, not kept in registers from piece to piece
   const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
-  const Loader<T, DP, 32, 1, PAGES> loader(a, u, lane, 0);
+  const Loader<float, DP, 32, 1, PAGES, true> loader(a, u, lane, 0);
   constexpr int NI = decltype(loader)::NI;
-  unsigned char *lk = lds + wave * 2 * W::kTile, *lv = lk + W::kTile, *lq = lds + kAttendWaves * 2 * W::kTile;
+  unsigned char *lk = lds + wave * 2 * W::kTile, *lv = lk + W::kTile;
   int32_t k0 = u.k_lo + tile * kThinKeys + wave * 32;
   const int32_t end = min(u.k_hi, u.k_lo + (tile + tiles) * kThinKeys);
-  bare_barrier();                      // nobody uses the piece before any more
+  bare_barrier();                       // nobody uses the piece before any more
+  const Row w = row_at(a, u, u.r0 + l32);
+  const int32_t pos = w.pos;
+  auto before = [&] { return a.window > 0 ? pos - a.window : -1; };
   u32x4 qf[S::NQ];
-  int32_t pos[RB];
+  load_query<float, DP>(a, w, half, qf);
+  floatx16 o[S::NO];
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) pos[rb] = row_at(a, u, u.r0 + rb * 32 + l32).pos;
-  if constexpr (RB == 1) {
-    load_query<T, DP>(a, row_at(a, u, u.r0 + l32), half, qf);
-  } else {
-    if (wave < RB) {
-      load_query<T, DP>(a, row_at(a, u, u.r0 + wave * 32 + l32), half, qf);
-#pragma unroll
-      for (int i = 0; i < S::NQ; ++i)
-        *reinterpret_cast<u32x4 *>(lq + key_at<S::RB>(wave * 32 + l32, 2 * i + half)) = qf[i];
-    }
-    bare_barrier();
-  }
-  floatx16 o[RB][S::NO];
-  float ref[RB], sum[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-    for (int n = 0; n < S::NO; ++n) o[rb][n] = floatx16{};
-    ref[rb] = -INFINITY;
-    sum[rb] = 0.f;
-  }
+  for (int n = 0; n < S::NO; ++n) o[n] = floatx16{};
+  float ref = -INFINITY, sum = 0.f;
   const int32_t begin = k0;
   auto at_edge = [&](int32_t k) { return k + 32 > u.min_hi || k < u.max_lo; };
   bool odd = false;
@@ -1151,36 +1105,26 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
     const bool more = k0 < end;
     if (!now && !more) break;
     const int32_t k = k0 - kThinKeys;
-    floatx16 s[RB];
+    floatx16 s[1];
     if (now) {
       wait_vm<NI>();                    // keys are in, values may be on their way
       loader.clear_keys(lk);
-      if constexpr (RB == 1) {
-        scores<T, DP, 1>(lk, lane, qf, reinterpret_cast<floatx16(&)[1]>(s[0]), a.D);
-      } else {
-        int away = (int) (lq - lk);
-        asm volatile("" : "+s"(away));  // an addition a read, instead of as many addresses in registers
-        scores<T, DP, RB>(lk, lk + away, lane, s, a.D);
-      }
+      scores<float, DP>(lk, lane, qf, s, a.D);
       wait_lds();
     }
     if (more) loader.template load<false>(k0, pages, lk);
     if (now) {
       const bool edge = at_edge(k);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        if (edge) hide(s[rb], k, half, pos[rb], a.window > 0 ? pos[rb] - a.window : -1);
-        floatx16(&one)[1] = reinterpret_cast<floatx16(&)[1]>(s[rb]);
-        follow<S::NO>(row_max<1>(one, a.c), ref[rb], sum[rb], o[rb]);
-        to_weights<1>(one, a.c, minus_ref(ref[rb]), sum[rb]);
-      }
+      if (edge) hide(s[0], k, half, pos, before());
+      follow<S::NO>(row_max<1>(s, a.c), ref, sum, o);
+      to_weights<1>(s, a.c, minus_ref(ref), sum);
       if (more) wait_vm<NI>();
       else wait_vm<0>();
       if (edge) {
-        odd = __builtin_amdgcn_ballot_w64(clear_odd_values<S::kBf16>(lv, W::kTile, lane, kWave)) != 0 || odd;
+        odd = __builtin_amdgcn_ballot_w64(clear_odd_values<false>(lv, W::kTile, lane, kWave)) != 0 || odd;
         wait_lds();
       }
-      add_values<T, DP, RB>(lv, 0, lane, s, o, a.D);
+      add_values<DP>(lv, lane, s[0], o, a.D);
       wait_lds();
     }
     if (!more) break;
@@ -1188,58 +1132,35 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
     pages = loader.look_up(k0 + kThinKeys);
   }
   if (odd) {
-    for (k0 = begin; k0 < end; k0 += kThinKeys) {
-      if (!at_edge(k0)) continue;
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-        add_odd_values<T, DP, PAGES != 0>(a, u, k0, min(k0 + 32, u.k_hi), half, pos[rb], a.window > 0 ? pos[rb] - a.window : -1, o[rb]);
-    }
+    for (k0 = begin; k0 < end; k0 += kThinKeys)
+      if (at_edge(k0)) add_odd_values<float, DP, PAGES != 0>(a, u, k0, min(k0 + 32, u.k_hi), half, pos, before(), o);
   }
 
-  // The waves' sums: 2 to 0 and 3 to 1, then 1 to 0 (with two blocks of rows 0 also gives its second to 1).
+  // The waves' sums: 2 to 0 and 3 to 1, then 1 to 0.
   float *room = reinterpret_cast<float *>(lds);
-  constexpr int kBlock = kRowsFloats<DP>;
-  auto give = [&](float *to, int rb) { give_rows<DP>(to, lane, o[rb], ref[rb], sum[rb]); };
-  auto take = [&](const float *from, int rb) { take_rows<DP>(from, lane, o[rb], ref[rb], sum[rb]); };
   bare_barrier();
-  if (wave >= 2) {
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) give(room + ((wave - 2) * RB + rb) * kBlock, rb);
-  }
+  if (wave >= 2) give_rows<DP>(room + (wave - 2) * kRowsFloats<DP>, lane, o, ref, sum);
   bare_barrier();
-  if (wave < 2) {
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) take(room + (wave * RB + rb) * kBlock, rb);
-  }
+  if (wave < 2) take_rows<DP>(room + wave * kRowsFloats<DP>, lane, o, ref, sum);
   bare_barrier();
-  if (wave == 1) give(room, 0);
-  if (RB > 1 && wave == 0) give(room + kBlock, RB - 1);
+  if (wave == 1) give_rows<DP>(room, lane, o, ref, sum);
   bare_barrier();
-  auto finish = [&](int rb) {
-    const float all = pair_sum(sum[rb]);
-    int32_t r = rb * 32 + l32;
-    asm("" : "+v"(r));                  // formed here, not kept in registers since the beginning
-    const Row w = row_at(a, u, u.r0 + r);
-    if (part) store_part<DP, 32 * RB>(part, r, half, w.there, o[rb], ref[rb], all);
-    else store_row<T, DP>(a, w, half, o[rb], all);
-  };
-  if (wave == 0) {
-    take(room, 0);
-    finish(0);
-  }
-  if (RB > 1 && wave == 1) {
-    take(room + kBlock, RB - 1);
-    finish(RB - 1);
-  }
+  if (wave > 0) return;
+  take_rows<DP>(room, lane, o, ref, sum);
+  sum = pair_sum(sum);
+  int32_t r = l32;
+  asm("" : "+v"(r));                    // formed here, not kept in registers since the beginning
+  const Row out = row_at(a, u, u.r0 + r);
+  if (part) store_part<DP, 32>(part, r, half, out.there, o, ref, sum);
+  else store_row<float, DP>(a, out, half, o, sum);
 }
 
-template <typename T, int DP, int RB, int PAGES>
-__global__ __launch_bounds__(kAttendThreads, (Thin<T, DP, RB>::kRuns / 256)) void attend_thin_kernel(AttendArgs a,
-                                                                                                  Join *join,
-                                                                                                  Part<DP, 32 * RB> *parts) {
-  __shared__ __align__(16) unsigned char lds[Thin<T, DP, RB>::kLds];
-  work_on_run<DP, 32 * RB, kThinKeys, kThinLeast, kThinCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32 * RB> *part) {
-    thin_piece<T, DP, RB, PAGES>(a, u, tile, tiles, lds, part);
+template <int DP, int PAGES>
+__global__ __launch_bounds__(kAttendThreads, (Thin<DP>::kRuns / 256)) void attend_thin_kernel(AttendArgs a, Join *join,
+                                                                                          Part<DP, 32> *parts) {
+  __shared__ __align__(16) unsigned char lds[Thin<DP>::kLds];
+  work_on_run<DP, 32, kThinKeys, kThinLeast>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32> *part) {
+    thin_piece<DP, PAGES>(a, u, tile, tiles, lds, part);
   });
 }
 
@@ -1321,8 +1242,6 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------
 
-constexpr int32_t kThickRuns = 512;
-
 constexpr size_t join_bytes(int32_t runs) { return ((size_t) runs * sizeof(Join) + 255) / 256 * 256; }
 
 template <typename T, int DP, int R>
@@ -1339,30 +1258,48 @@ hipError_t split_launch(Kernel kernel, int32_t runs, const AttendArgs &a, void *
   return hipGetLastError();
 }
 
-// Rows of a request up to which the thin kernel takes a block of them at a time.
-template <typename T, int DP, int RB>
+template <int DP>
 hipError_t go_thin(const AttendArgs &a, bool shared_pages, void *workspace, hipStream_t stream) {
-  constexpr int32_t runs = Thin<T, DP, RB>::kRuns;
-  if (shared_pages) return split_launch<T, DP, 32 * RB>(attend_thin_kernel<T, DP, RB, 1>, runs, a, workspace, stream);
-  return split_launch<T, DP, 32 * RB>(attend_thin_kernel<T, DP, RB, 2>, runs, a, workspace, stream);
+  if (shared_pages) return split_launch<float, DP, 32>(attend_thin_kernel<DP, 1>, Thin<DP>::kRuns, a, workspace, stream);
+  return split_launch<float, DP, 32>(attend_thin_kernel<DP, 2>, Thin<DP>::kRuns, a, workspace, stream);
+}
+
+template <typename T, int DP, int WK, bool ONCE>
+hipError_t go_thick(const AttendArgs &a, bool shared_pages, void *workspace, hipStream_t stream) {
+  using W = Thick<T, DP, WK>;
+  if (shared_pages) return split_launch<T, DP, W::R>(attend_thick_kernel<T, DP, WK, 1, ONCE>, W::kRuns, a, workspace, stream);
+  return split_launch<T, DP, W::R>(attend_thick_kernel<T, DP, WK, 2, ONCE>, W::kRuns, a, workspace, stream);
 }
 
 template <typename T, int DP>
 hipError_t go_cache(const AttendArgs &a, int64_t longest, void *workspace, hipStream_t stream) {
-  // 16 keys share a page, and lie within 32 bits of each other
+  // 16 keys share a page, and lie within 32 bits of each other.  us with pages looked up for 16 keys and for each lane, bf16: 32
+  // sequences of 4000 keys with 9 new tokens 121 and 133, 8 of 2000 35.2 and 37.1; fp32: 369 and 459, 76 and 91.
   const bool shared_pages = a.page_size % 16 == 0 && a.k_tok * 16 * (int64_t) sizeof(T) < (int64_t) 1 << 31;
   const int64_t rows = longest * a.G;
-  if (rows <= 32) return go_thin<T, DP, 1>(a, shared_pages, workspace, stream);
-  if (rows <= 64) return go_thin<T, DP, 2>(a, shared_pages, workspace, stream);
-  if (shared_pages) return split_launch<T, DP, kThickRows>(attend_thick_kernel<T, DP, 1>, kThickRuns, a, workspace, stream);
-  return split_launch<T, DP, kThickRows>(attend_thick_kernel<T, DP, 2>, kThickRuns, a, workspace, stream);
+  // The keys are read as often as a request has blocks of rows: once, if they fit one.  In bf16 two waves on the keys of 64 rows
+  // hide more of memory's delay than four on 128, most of which are not there, and than four with streams of their own; in fp32
+  // the products bound, and a wave whose rows are not there does none.  us with 32, 64 and 128 rows a workgroup, d = 128:
+  //   bf16, 4 rows:   1 sequence of 1000 keys 15 14 19;  8 of 2000 26 24 24;  32 of 4000 103 94 96
+  //   bf16, 36 rows:  8 of 2000 37 29 29;  32 of 4000 141 103 107
+  //   bf16, 68 rows:  8 of 2000 47 46 32;  32 of 4000 304 149 128
+  //   fp32, 20 rows:  8 of 2000 54 67 88;  32 rows, 32 of 4000: 231 391 577
+  //   fp32, 36 rows:  8 of 2000 81 69 93;  32 of 4000 452 393 579
+  //   fp32, 68 rows:  8 of 2000 109 122 98;  32 of 4000 678 733 588
+  if constexpr (sizeof(T) == 4) {
+    if (rows <= 32) return go_thin<DP>(a, shared_pages, workspace, stream);
+  }
+  if (rows <= 64) return go_thick<T, DP, 2, true>(a, shared_pages, workspace, stream);
+  // in fp32 the hint changes nothing here (586 and 588 us)
+  if (sizeof(T) == 2 && rows <= kThickRows) return go_thick<T, DP, 1, sizeof(T) == 2>(a, shared_pages, workspace, stream);
+  return go_thick<T, DP, 1, false>(a, shared_pages, workspace, stream);
 }
 
 template <typename T, int DP>
 size_t cache_bytes(int64_t rows) {
-  if (rows <= 32) return parts_bytes<T, DP, 32>(Thin<T, DP, 1>::kRuns);
-  if (rows <= 64) return parts_bytes<T, DP, 64>(Thin<T, DP, 2>::kRuns);
-  return parts_bytes<T, DP, kThickRows>(kThickRuns);
+  if (sizeof(T) == 4 && rows <= 32) return parts_bytes<T, DP, 32>(Thin<DP>::kRuns);
+  if (rows <= 64) return parts_bytes<T, DP, 64>(Thick<T, DP, 2>::kRuns);
+  return parts_bytes<T, DP, kThickRows>(Thick<T, DP, 1>::kRuns);
 }
 
 }  // namespace

@@ -7,7 +7,6 @@
 namespace pcg {
 
 constexpr int32_t kPagesMaxRequests = 65536;
-constexpr int64_t kPagesFillRows = 4096;      // rows of the slot map up to which the first launch fills them
 
 struct PagesArgs {
   int32_t B, num_pages, page_size, max_blocks;

@@ -9,6 +9,7 @@ namespace {
 constexpr int kPagesThreads = 1024;
 constexpr int kPagesWaves = kPagesThreads / kWave;
 constexpr int kWriteThreads = 256;
+constexpr int kFillAtOnce = 4;
 
 // Inclusive running sum over the workgroup of WAVES waves, and the sum of all.  `part` holds a value per wave.
 template <int WAVES, typename T>
@@ -74,27 +75,42 @@ __device__ __forceinline__ int run_of(const int32_t *upto, int32_t i) {
   return lo;
 }
 
-// Slot and position of new token `row`: the request by bisection of q_start (in LDS where it fits).
-__device__ __forceinline__ void place_token(const PagesArgs &p, const int32_t *starts, const int32_t *lens, int32_t total,
-                                            int64_t row) {
-  int32_t slot = -1, position = 0;
-  if (row < total) {
-    int32_t lo = 0, hi = p.B;            // starts[lo] <= row < starts[hi]
-    while (hi - lo > 1) {
-      const int32_t mid = (lo + hi) >> 1;
-      if (starts[mid] <= row) lo = mid;
-      else hi = mid;
-    }
-    position = lens[lo] + (int32_t) row - starts[lo];
-    const int32_t block = position / p.page_size;
-    slot = p.table[(int64_t) lo * p.table_stride + block] * p.page_size + (position - block * p.page_size);
+// Slots and positions of N new tokens, `row` and then every `step`-th: their requests by bisection of the starts (in LDS where they
+// fit), N beside each other because each is a chain of waits.
+template <int N>
+__device__ __forceinline__ void place_tokens(const PagesArgs &p, const int32_t *starts, const int32_t *lens, int32_t total,
+                                             int64_t row, int32_t step) {
+  int32_t lo[N], block[N], page[N], position[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) lo[i] = 0;
+  for (int32_t n = p.B; n > 1; n -= n >> 1) {             // starts[lo] <= row, and row is ahead of starts[lo + n]
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (starts[lo[i] + (n >> 1)] <= row + (int64_t) i * step) lo[i] += n >> 1;
   }
-  p.slots[row] = slot;
-  if (p.positions) p.positions[row] = position;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int64_t at = row + (int64_t) i * step;
+    position[i] = page[i] = 0;
+    if (at >= total) continue;
+    position[i] = lens[lo[i]] + (int32_t) at - starts[lo[i]];
+    block[i] = position[i] / p.page_size;
+    page[i] = p.table[(int64_t) lo[i] * p.table_stride + block[i]];
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int64_t at = row + (int64_t) i * step;
+    if (at >= p.max_tokens) continue;
+    p.slots[at] = at < total ? page[i] * p.page_size + (position[i] - block[i] * p.page_size) : -1;
+    if (p.positions) p.positions[at] = position[i];
+  }
 }
 
-// As many threads as requests, or more: every request is read once and stays in registers.  Bound by trips to memory one after the
-// other (state, pages that come back, pages taken, the table for the slots); the running sums are two where nobody is refused.
+// New lengths, page counts, pages and first rows of all requests: running sums over the requests, of the tokens (who fits the batch)
+// and of the pages given back and taken (who gets which).  One workgroup, because each sum needs all of the one before and a grid's
+// meeting costs more than the work; as many threads as requests, or more, so that every request is read once and stays in registers.
+// Bound by trips to memory one after the other (state, pages that come back, pages taken, the table for the slots): 3.4 us for a
+// request, 4.4 for 64 with 9 tokens each, 7.4 for 300; the running sums are two where nobody is refused.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void pages_step_kernel(PagesArgs p, int32_t fill_rows) {
   constexpr int W = THREADS / kWave;
@@ -157,10 +173,10 @@ __global__ __launch_bounds__(THREADS) void pages_step_kernel(PagesArgs p, int32_
   }
   if (!fill_rows) return;
   if (given > 0) __syncthreads();        // the table is whole
-  for (int64_t row = tid; row < p.max_tokens; row += THREADS) place_token(p, starts, lens, all, row);
+  for (int64_t row = tid; row < p.max_tokens; row += kFillAtOnce * THREADS) place_tokens<kFillAtOnce>(p, starts, lens, all, row, THREADS);
 }
 
-// More requests than threads: two passes over them.
+// More requests than threads: the same in two passes over them, because who gets pages depends on all that come back.
 __global__ __launch_bounds__(kPagesThreads) void pages_step_large_kernel(PagesArgs p, int32_t fill_rows) {
   __shared__ int64_t part64[kPagesWaves];
   __shared__ int32_t part[kPagesWaves];
@@ -242,16 +258,20 @@ __global__ __launch_bounds__(kPagesThreads) void pages_step_large_kernel(PagesAr
   }
   if (!fill_rows) return;
   __syncthreads();
-  for (int64_t row = tid; row < p.max_tokens; row += kPagesThreads) place_token(p, p.q_start, p.state_out, starts, row);
+  for (int64_t row = tid; row < p.max_tokens; row += kFillAtOnce * kPagesThreads)
+    place_tokens<kFillAtOnce>(p, p.q_start, p.state_out, starts, row, kPagesThreads);
 }
 
+// A row a thread, where the rows are too many for the workgroup that knows the requests: 65 536 rows of 1024 requests in 9.9 us for
+// both launches.
 __global__ __launch_bounds__(256) void pages_slots_kernel(PagesArgs p) {
   const int32_t total = p.q_start[p.B];
   const int64_t row = (int64_t) blockIdx.x * 256 + threadIdx.x;
-  if (row < p.max_tokens) place_token(p, p.q_start, p.state_out, total, row);
+  if (row < p.max_tokens) place_tokens<1>(p, p.q_start, p.state_out, total, row, 0);
 }
 
-// One 16-byte part of a token's keys and of its values a thread.
+// One 16-byte part of a token's keys and of its values a thread.  Bound by memory, each part read and written once: 32 MB of float32
+// prompts read and as many written in 17 us, 3.9 TB/s (the launch itself is 3 of them); a step of 576 rows of 2 x 2 KB 3.3 us.
 __global__ __launch_bounds__(kWriteThreads) void cache_write_kernel(WriteArgs w) {
   const int64_t i = (int64_t) blockIdx.x * kWriteThreads + threadIdx.x;
   const int64_t row = i / w.parts;
@@ -275,9 +295,13 @@ __global__ __launch_bounds__(kWriteThreads) void cache_write_kernel(WriteArgs w)
 }  // namespace
 
 hipError_t launch_pages_step(const PagesArgs &p, hipStream_t stream) {
-  const bool fill = p.max_tokens <= kPagesFillRows;
-  // fewer waves meet sooner
-  if (p.B <= 256) pages_step_kernel<256><<<1, 256, 0, stream>>>(p, fill);
+  // Fewer waves meet sooner, more move more pages at a time.  us with 256 and with 1024 threads: 1 request 3.4 and 5.1, 64 requests
+  // 4.4 and 6.1; 64 requests that take 1024 pages 7.4 and 8.0, 4000 pages 11.7 and 9.4.
+  const bool few = p.B <= 256 && p.max_tokens / p.page_size <= 2048;
+  // One launch, or another one with as many threads as rows.  us with one and with two, of 256 threads: 4 rows 3.4 and 4.6, 576
+  // 4.4 and 6.2, 2304 7.3 and 6.9, 4096 9.1 and 6.9; of 1024: 2700 7.4 and 8.7, 32 768 26.5 and 9.5.
+  const bool fill = p.max_tokens <= (few ? 2048 : 4096);
+  if (few) pages_step_kernel<256><<<1, 256, 0, stream>>>(p, fill);
   else if (p.B <= kPagesThreads) pages_step_kernel<kPagesThreads><<<1, kPagesThreads, 0, stream>>>(p, fill);
   else pages_step_large_kernel<<<1, kPagesThreads, 0, stream>>>(p, fill);
   hipError_t e = hipGetLastError();
