@@ -71,7 +71,7 @@ typedef enum {
   PCG_ERR_MISALIGNED = -9,         /* workspace not 256-byte aligned, logits not element-aligned */
   PCG_ERR_CAPACITY = -10,          /* pcg_asg_build: a group or the member array did not fit      */
   PCG_ERR_SCRATCH_TOO_SMALL = -11, /* pcg_verify_static: the step needs more than PCG_STATIC_SCRATCH_BYTES */
-  PCG_ERR_BAD_SCALE = -12          /* attention: scale is not a finite number > 0                 */
+  PCG_ERR_BAD_SCALE = -12          /* attention: scale * log2(e) is not a finite number > 0       */
 } pcg_status;
 
 #define PCG_MAX_K 64               /* largest number of draft positions per step           */
@@ -540,8 +540,8 @@ int pcg_pages_step(const pcg_pages *pages, const int32_t *state_in, int32_t *sta
 
 /*
  * k_new, v_new (DEVICE, T rows of kv_heads * head_dim; row t, head h at t * tok_stride + h * head_stride, strides in elements
- * and multiples of 16 bytes, 16-byte aligned) to the slots slots[t] of the cache.  Rows whose slot is negative or past the
- * cache's last are left out.  A slot must not be named twice.  T == 0 is a no-op.
+ * and multiples of 16 bytes, 16-byte aligned) to the slots slots[t] of the cache.  T times the 16-byte
+ * parts of a row < 2^31.  Rows whose slot is negative or past the cache's last are left out.  A slot must not be named twice.  T == 0 is a no-op.
  */
 int pcg_cache_write(const pcg_kv_cache *cache, const void *k_new, const void *v_new, int64_t T, int64_t k_tok_stride,
                     int64_t k_head_stride, int64_t v_tok_stride, int64_t v_head_stride, const int32_t *slots,
@@ -556,7 +556,7 @@ int pcg_cache_write(const pcg_kv_cache *cache, const void *k_new, const void *v_
  * multiply values.  A row that sees no key, or none whose score is above -infinity, gives zeros.  What stands in keys and values that a
  * row does not see has no effect on it, infinities and NaN included.
  *   q, out        DEVICE [T, heads, head_dim] of the cache's dtype, strides in elements as in pcg_cache_write; out must not
- *                 overlap q.  Rows behind q_start[B] are not read and not written.
+ *                 overlap what is read.  T * heads < 2^28, B * kv_heads < 2^22.  Rows behind q_start[B] are not read and not written.
  *   block_table   DEVICE as in pcg_pages.  Keys in pages outside [0, num_pages) or past max_blocks read as zeros.
  *   lens          DEVICE int32 [B]; q_start DEVICE int32 [B + 1], q_start[0] = 0, non-decreasing, q_start[B] <= T
  *   heads         a multiple of kv_heads

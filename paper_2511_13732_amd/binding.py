@@ -601,6 +601,13 @@ def _int32(t: torch.Tensor, n: int, dev, what: str):
         raise ValueError(f"{what} must be a contiguous int32 tensor [{n}] on {dev}")
 
 
+def _int31(x: int, what: str, least: int = 0) -> int:
+    """An argument that the library takes in 32 bits: a larger one would arrive as another number."""
+    if not least <= x < 1 << 31:
+        raise ValueError(f"{what} must be from {least} to 2^31 - 1, got {x}")
+    return x
+
+
 @dataclass
 class Pages:
     """The pages of a K/V cache that B requests hold (pcg_pages and its state): ``block_table`` int32 [B, max_blocks] (rows
@@ -621,6 +628,7 @@ class Pages:
         _int32(self.free_pages, self.num_pages, t.device, "free_pages")
         _int32(self.state, 3 * self.B + 1, t.device, "state")
         self.device = t.device
+        _int31(self.page_size, "page_size", 1)
         self._ref = C.pointer(_PagesStruct(self.B, self.num_pages, self.page_size, self.max_blocks, t.data_ptr(),
                                     t.stride(0) if self.B > 1 else self.max_blocks, self.free_pages.data_ptr()))
 
@@ -657,6 +665,13 @@ class PagesStep:
     positions: torch.Tensor    # int32 [max_tokens], 0 behind the last request's rows
     refused: torch.Tensor      # int32 [1]
 
+    def __post_init__(self):
+        self.device = self.q_start.device
+        for name in ("q_start", "slots", "positions"):
+            t = getattr(self, name)
+            _int32(t, t.numel(), self.device, name)
+        _int32(self.refused, 1, self.device, "refused")
+
 
 def pages_step_outputs(B: int, max_tokens: int, device) -> PagesStep:
     new = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
@@ -672,8 +687,8 @@ def pages_step(pages: Pages, add, *, max_tokens: int, commit: Optional[torch.Ten
     dev, B = pages.device, pages.B
     if out is None:
         out = pages_step_outputs(B, max_tokens, dev)
-    if out.slots.numel() < max_tokens or out.positions.numel() < max_tokens or out.q_start.numel() != B + 1:
-        raise ValueError("the outputs have room for another number of rows or requests")
+    if out.slots.numel() < max_tokens or out.positions.numel() < max_tokens or out.q_start.numel() != B + 1 or out.device != dev:
+        raise ValueError("the outputs have room for another number of rows or requests, or are on another device")
     each = isinstance(add, torch.Tensor)
     if each:
         _int32(add, B, dev, "add")
@@ -684,8 +699,8 @@ def pages_step(pages: Pages, add, *, max_tokens: int, commit: Optional[torch.Ten
     else:
         _int32(state_out, 3 * B + 1, dev, "state_out")
     _call(dev, "pcg_pages_step", lib().pcg_pages_step, pages._ref, pages.state.data_ptr(), state_out.data_ptr(),
-          None if commit is None else commit.data_ptr(), commit_extra, add.data_ptr() if each else None,
-          0 if each else add, max_tokens, out.q_start.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(),
+          None if commit is None else commit.data_ptr(), _int31(commit_extra, "commit_extra", -1 << 31),
+          add.data_ptr() if each else None, 0 if each else _int31(add, "add", -1 << 31), max_tokens, out.q_start.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(),
           out.refused.data_ptr())
     return out
 
@@ -738,7 +753,7 @@ def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, len
     """Attention of new tokens over the cache that holds their own keys and values already: ``q`` [T, heads, head_dim], the
     rows q_start[b] .. q_start[b + 1] of request b at positions lens[b], lens[b] + 1, .. (pages_step: ``pages.lens``), each
     seeing the keys up to itself, with ``window`` the last that many of them.  ``longest`` bounds the new tokens of a request
-    (it decides how the work is cut; without it: the mean).  ``scale`` is 1 / sqrt(head_dim) unless given.  Rows of ``out`` behind
+    (it decides how the work is cut; without it: the mean).  ``out`` must not overlap what is read.  ``scale`` is 1 / sqrt(head_dim) unless given.  Rows of ``out`` behind
     the last request's stay as they were (zeros where ``out`` is not given)."""
     T, heads, head_dim = q.shape
     dev, B = cache.device, lens.numel()
@@ -755,9 +770,12 @@ def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, len
         longest = -(-T // max(B, 1))
     if workspace is None:
         workspace = _workspace(dev, cache_attend_workspace_bytes(B, T, heads, cache.kv_heads, head_dim, longest))
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
     _call(dev, "pcg_cache_attend", lib().pcg_cache_attend, cache._ref, q.data_ptr(), *qs, heads, T, block_table.data_ptr(),
           block_table.stride(0), block_table.shape[1], lens.data_ptr(), q_start.data_ptr(), B, longest,
-          head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), *os_, workspace.data_ptr(), workspace.numel())
+          head_dim ** -0.5 if scale is None else scale, _int31(window, "window"), out.data_ptr(), *os_, workspace.data_ptr(),
+          workspace.numel())
     return out
 
 
@@ -778,7 +796,7 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: to
         longest = -(-T // max(B, 1))
     _call(dev, "pcg_prompt_attend", lib().pcg_prompt_attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q), T, heads,
           kv_heads, head_dim, *qs, *ks, *vs, q_start.data_ptr(), B, longest, head_dim ** -0.5 if scale is None else scale,
-          window, out.data_ptr(), *os_)
+          _int31(window, "window"), out.data_ptr(), *os_)
     return out
 
 

@@ -1166,8 +1166,11 @@ __global__ __launch_bounds__(kAttendThreads, (Thin<DP>::kRuns / 256)) void atten
 
 // ---- units in parts ----------------------------------------------------------------------------------------------------------
 
-// Workgroups (i, y) join the parts of the unit that run i began and did not finish, a wave a row, every second part to each half
-// of it.  A trip to memory takes a microsecond: 16 parts are asked for at a time.
+// Workgroups (i, y) join the parts of the unit that run i began and did not finish: outputs, references and sums of the parts are
+// brought to the largest reference, added and divided.  A wave a row, every second part to each half of it.  Bound by trips to
+// memory, a microsecond each: references, sums and first outputs are asked for together, 16 parts at a time, no more than there are.
+// 64 sequences (two or three parts a unit) 7.0 us, prompts by pieces (33 MB of parts) 18 us, 2 x 120 000 tokens (64 parts) 6 us.  A
+// kernel of its own because the next launch's start is the one meeting of all workgroups that a graph can hold.
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a, const Join *join, const Part<DP, R> *parts) {
   const Join j = join[blockIdx.x];
@@ -1189,10 +1192,13 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
     vec o = {};
     float sum = 0.f, top = -INFINITY;
     vec x[kAtOnce];
+    // One, four or all eight (one by one: prompts by pieces 1 % faster, a single token's 64 parts 2 % slower; always eight:
+    // 5 % slower and the same).
+    auto from = [](int32_t k) { return k < 1 ? 0 : k < 4 ? 2 : 8; };
     auto ask = [&](int32_t p0, int32_t i, int32_t n) {
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k)
-        x[k] = *reinterpret_cast<const vec *>(&part_at(p0 + min(i + 2 * k + half, n - 1)).o[row][l32 * kEach]);
+        if (i + from(k) < n) x[k] = *reinterpret_cast<const vec *>(&part_at(p0 + min(i + 2 * k + half, n - 1)).o[row][l32 * kEach]);
     };
     for (int32_t p0 = 0; p0 < j.parts; p0 += kWave) {
       // references and sums of 64 parts, one a lane, and the first outputs beside them
@@ -1211,6 +1217,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
         if (i) ask(p0, i, n);
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
+          if (i + from(k) >= n) break;
           const int32_t p = i + 2 * k + half;
           const float fp = __shfl(f, min(p, n - 1));
 #pragma unroll

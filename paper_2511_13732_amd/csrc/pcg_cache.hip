@@ -270,8 +270,8 @@ __global__ __launch_bounds__(256) void pages_slots_kernel(PagesArgs p) {
   if (row < p.max_tokens) place_tokens<1>(p, p.q_start, p.state_out, total, row, 0);
 }
 
-// One 16-byte part of a token's keys and of its values a thread.  Bound by memory, each part read and written once: 32 MB of float32
-// prompts read and as many written in 17 us, 3.9 TB/s (the launch itself is 3 of them); a step of 576 rows of 2 x 2 KB 3.3 us.
+// One 16-byte part of a token's keys and of its values a thread.  Bound by memory, each part read and written once: 45 MB of float32
+// prompts read and as many written in 15.1 us; a step of 576 rows, 2 x 2 KB each, 3.6 us, which a launch alone takes too.
 __global__ __launch_bounds__(kWriteThreads) void cache_write_kernel(WriteArgs w) {
   const int64_t i = (int64_t) blockIdx.x * kWriteThreads + threadIdx.x;
   const int64_t row = i / w.parts;

@@ -55,9 +55,10 @@ int check_queries(AttendArgs &a, const void *q, int64_t q_tok, int64_t q_head, p
                   int32_t window, void *out, int64_t o_tok, int64_t o_head) {
   if (int rc = check_heads(heads, kv_heads, head_dim)) return rc;
   if (B < 0 || T < 0 || longest < 0 || longest >= kInt31 || window < 0) return PCG_ERR_BAD_SHAPE;
-  // rows of a shared head and workgroups are counted in 32 bits
-  if (T * (heads / kv_heads) >= kInt31 || (T * (heads / kv_heads) / 32 + B) * kv_heads >= kInt31) return PCG_ERR_BAD_SHAPE;
-  if (!(std::isfinite(scale) && scale > 0.0f)) return PCG_ERR_BAD_SCALE;
+  // a grid's threads are counted in 32 bits: 256 for every 64 rows of a shared head, and for what a request leaves over
+  if (T >= kInt31 || T * heads >= (int64_t) 1 << 28 || (int64_t) B * kv_heads >= (int64_t) 1 << 22) return PCG_ERR_BAD_SHAPE;
+  const float c = (float) (1.4426950408889634074 * (double) scale);
+  if (!(std::isfinite(c) && c > 0.0f)) return PCG_ERR_BAD_SCALE;
   std::memset(&a, 0, sizeof a);
   if (B == 0 || T == 0) return PCG_OK;
   if (!q || !out || !q_start) return PCG_ERR_NULL_ARG;
@@ -81,7 +82,7 @@ int check_queries(AttendArgs &a, const void *q, int64_t q_tok, int64_t q_head, p
   a.magic_G = magic(a.G);
   a.page_size = 1;
   a.magic_page = magic(1);
-  a.c = (float) (1.4426950408889634074 * (double) scale);
+  a.c = c;
   return PCG_OK;
 }
 
@@ -137,8 +138,8 @@ int pcg_cache_write(const pcg_kv_cache *cache, const void *k_new, const void *v_
   w.part_elems = 16 / w.elem;
   w.head_parts = c.head_dim / w.part_elems;
   w.parts = (int64_t) w.head_parts * c.kv_heads;
-  // workgroups are counted in 32 bits
-  if (T >= kInt31 || T * w.parts / 256 >= kInt31 - 1) return PCG_ERR_BAD_SHAPE;
+  // a grid's threads, one a part, are counted in 32 bits
+  if (T >= kInt31 || T * w.parts >= kInt31) return PCG_ERR_BAD_SHAPE;
   if (T == 0) return PCG_OK;
   if (!k_new || !v_new || !slots) return PCG_ERR_NULL_ARG;
   if (!stride16(k_tok_stride, c.dt, T == 1) || !stride16(v_tok_stride, c.dt, T == 1) ||
