@@ -164,6 +164,40 @@ def test_tensors_that_do_not_fit_are_refused():
             pcg.pages_step(pages, max_tokens=8, **bad)
 
 
+def test_sizes_whose_grids_do_not_fit_are_refused():
+    assert attend(T=1 << 26) == prompt(T=1 << 26) == BAD_SHAPE                    # 4 heads
+    assert attend(B=1 << 21) == prompt(B=1 << 21) == BAD_SHAPE                    # 2 shared heads
+    assert write(T=1 << 27) == BAD_SHAPE                                          # 16 parts a row
+    assert attend(scale=3e38) == prompt(scale=3e38) == BAD_SCALE
+
+
+def test_numbers_that_the_library_would_take_for_others_are_refused():
+    f = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype)  # noqa: E731
+    i = lambda *s: f(*s, dtype=torch.int32)  # noqa: E731
+    cache = pcg.KvCache(f(4, 16, 2, 64), f(4, 16, 2, 64))
+    good = dict(q=f(3, 4, 64), block_table=i(2, 3), lens=i(2), q_start=i(3), workspace=f(1 << 10, dtype=torch.uint8))
+    for bad in (dict(window=1 << 32), dict(window=-1), dict(workspace=f(1, dtype=torch.uint8).expand(1 << 30)),
+                dict(workspace=torch.zeros(1 << 10, dtype=torch.uint8, device="meta"))):
+        with pytest.raises(ValueError):
+            pcg.cache_attend(cache, **{**good, **bad})
+    with pytest.raises(ValueError):
+        pcg.prompt_attend(f(3, 4, 64), f(3, 2, 64), f(3, 2, 64), i(2), window=(1 << 32) + 5)
+    for size in (0, -16, (1 << 32) + 16):
+        with pytest.raises(ValueError):
+            pcg.Pages(i(4, 3), i(10), i(13), size)
+    pages = pcg.Pages.empty(4, 10, 16, 3, "cpu")
+    for bad in (dict(add=1 << 32), dict(add=1, commit=i(4), commit_extra=1 << 32)):
+        with pytest.raises(ValueError):
+            pcg.pages_step(pages, max_tokens=8, **bad)
+    for bad in ((i(5), i(8), i(8), i(2)), (i(5), f(8), i(8), i(1)), (i(5), i(16)[::2], i(8), i(1)),
+                (i(5), i(8), torch.zeros(8, dtype=torch.int32, device="meta"), i(1))):
+        with pytest.raises(ValueError):
+            pcg.PagesStep(*bad)
+    elsewhere = pcg.pages_step_outputs(4, 8, "meta")
+    with pytest.raises(ValueError):
+        pcg.pages_step(pages, 1, max_tokens=8, out=elsewhere)
+
+
 # ------------------------------------------------------------------ the plain forms, by hand
 
 def test_plain_pages_by_hand():

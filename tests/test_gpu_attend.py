@@ -89,6 +89,14 @@ def test_single_tokens(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("page_size,D,window", [(16, 128, 0), (24, 40, 0), (32, 72, 50), (5, 96, 70)])
+@pytest.mark.parametrize("chunk", [8, 9, 16, 17, 32, 33])
+def test_rows_on_both_sides_of_a_block(dtype, page_size, D, window, chunk):
+    """Four query heads a shared head: 32, 36, 64, 68, 128 and 132 rows at most, each with its own cut of the work."""
+    run_cache([210, 0, 77], [chunk, 1, chunk - 3], 8, 2, D, dtype, page_size=page_size, window=window, seed=chunk)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("longest", [1, 16, 400])
 def test_long_and_short_chunks_together(dtype, longest):
     """Whatever bound on the chunks is named, the rows are the same."""
@@ -176,6 +184,12 @@ def test_a_long_cache_is_split(dtype, G, H, ctx):
     run_cache([ctx], [1], H, G, 128, dtype, page_size=64, layout="heads", seed=ctx + 1)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_row_in_more_parts_than_a_wave_has_lanes(dtype):
+    run_cache([21000], [1], 1, 1, 64, dtype, page_size=64, seed=21)
+    run_cache([21000], [40], 1, 1, 64, dtype, page_size=16, seed=22)
+
+
 def test_offsets_past_32_bits():
     """Pages so far apart that elements and bytes are counted past 2^32."""
     D, G, ps, dt = 64, 1, 16, torch.bfloat16
@@ -235,14 +249,23 @@ def test_one_prompt(dtype, n):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(dtype):
+@pytest.mark.parametrize("D,window", [(64, 0), (128, 0), (24, 0), (80, 40)])
+def test_prompts_whose_waves_have_rows_of_their_own(dtype, D, window):
+    """No prompt is named as long beside the chip's load: blocks of 128 rows."""
+    run_prompt([1, 0, 33, 2, 64, 400], 8, 2, D, dtype, window=window, seed=D, longest=1)
+    run_prompt([129] * 6, 12, 12, D, dtype, window=window, seed=D + 1, longest=1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("longest", [1, 300])
+def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(dtype, longest):
     dt, n, H, G, D = DTYPES[dtype], 300, 4, 2, 64
     q = torch.randn((n, H, D), generator=gen(1)).to(dt).cuda()
     k, v = (torch.randn((n, G, D), generator=gen(s)).to(dt).cuda() for s in (2, 3))
-    clean = pcg.prompt_attend(q, k, v, torch.tensor([0, n], dtype=torch.int32).cuda(), longest=n)
+    clean = pcg.prompt_attend(q, k, v, torch.tensor([0, n], dtype=torch.int32).cuda(), longest=longest)
     v[200, 0, 5] = -math.inf
     v[250] = math.nan
-    out = pcg.prompt_attend(q, k, v, torch.tensor([0, n], dtype=torch.int32).cuda(), longest=n)
+    out = pcg.prompt_attend(q, k, v, torch.tensor([0, n], dtype=torch.int32).cuda(), longest=longest)
     want = ref.attend_rows(q[:200], k[:200], v[:200], 0, D ** -0.5)
     ref.check(out[:200], want, dt)
     assert torch.isnan(out[250:]).all()
