@@ -880,7 +880,11 @@ __device__ __forceinline__ void take_rows(const float *from, int lane, floatx16 
     for (int i = 0; i < 16; ++i) o[n][i] = o[n][i] * f0 + from[(n * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) * 32 + l32] * f1;
 }
 
-// WK waves share 32 rows and take the keys of a tile in turn, KB blocks of 32 each.
+// WK waves share 32 rows and take the keys of a tile in turn, KB blocks of 32 each: R rows a workgroup, tiles of 64 keys (fp32: 32
+// where every wave has rows of its own), two in LDS, one in use while the other comes.  64 keys of 128 elements, twice, are 64 KB:
+// two workgroups a CU, whose waves fill each other's waits (a third would not find registers: queries, outputs, scores
+// and operands on their way take 200 to 224 a lane).  Four waves on 32 rows each bring a tile once for 128 rows; reading
+// the operands then keeps LDS busy a quarter of the time.
 template <typename T, int DP, int WK>
 struct Thick {
   using S = Shape<T, DP>;
@@ -988,6 +992,10 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
   else store_row<T, DP>(a, w, half, o, sum);
 }
 
+// A cache's rows.  Few of them (WK 2): bound by memory, 32 sequences of 4000 keys with 9 new tokens 526 MB in 103 us, 5.1 TB/s, 2 of
+// 120 000 keys 5.7 TB/s, more than a copy reaches because nothing is written; one token of one sequence of 1500 keys is two
+// launches and the waits of one tile, 10.5 and 3.6 us.  Prompts by pieces (WK 1): 213 GFLOP in 300 to 318 us with the joining, 670 to
+// 710 TFLOP/s; bound as attend_prompt_kernel is, with 67 MB of parts written and read between.
 template <typename T, int DP, int WK, int PAGES, bool ONCE>
 __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) void attend_thick_kernel(AttendArgs a, Join *join,
                                                                                                        Part<DP, Thick<T, DP, WK>::R> *parts) {
@@ -1044,6 +1052,13 @@ __device__ __forceinline__ bool find_prompt_unit(const AttendArgs &a, int32_t ra
   return true;
 }
 
+// A unit a workgroup, no parts: there are enough of them.  Bound by the SIMDs' issue: products keep the matrix units busy 49 % of
+// the time (bf16, d = 128; no LDS conflicts), exponentials, maxima, sums and rounding beside them are 7.4 vector instructions for
+// every product.  27 000 tokens of prompts up to 8000, 32 heads: 1.23 PFLOP in 1275 us, 968 TFLOP/s (a library product of
+// 8192 x 8192 reaches 1117 here).  Left out of it for a measurement: the exponential 1147, the loads 1095, the weights' product
+// 924, the scores' 945 us.  Scores of the next tile beside the weights of this one (1382 us), 256 rows a workgroup by eight waves
+// (1275) or by four with two blocks of rows (2096) were not faster.  fp32, d = 64, 9 prompts of 1111 tokens: 80 TFLOP/s, 95 us, the
+// matrix units busy half of the time too.
 template <typename T, int DP, int WK>
 __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) void attend_prompt_kernel(AttendArgs a) {
   using W = Thick<T, DP, WK>;
@@ -1155,6 +1170,11 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   else store_row<float, DP>(a, out, half, o, sum);
 }
 
+// 32 rows of float32 over a cache.  A product of 32 x 32 x 2 keeps a SIMD 64 cycles whether 32 rows are there or 4, so that the four
+// waves of a CU have to share the keys, 32 each, with the loads of a wave's next keys ahead of its products with these: 32
+// sequences of 4000 keys, 8 new tokens of 4 heads a shared head, d = 128: 1053 MB in 231 us, 4.6 TB/s; 32 rows shared by two waves
+// 391 us, by one 577.  A short window (12 sequences, 1000 keys, d = 80, 39 MB) takes 38 us: 256 workgroups, one a CU, with some
+// tiles each, whose waits (for the run's first unit, its pages, its keys, the other waves' sums) nothing fills.
 template <int DP, int PAGES>
 __global__ __launch_bounds__(kAttendThreads, (Thin<DP>::kRuns / 256)) void attend_thin_kernel(AttendArgs a, Join *join,
                                                                                           Part<DP, 32> *parts) {
