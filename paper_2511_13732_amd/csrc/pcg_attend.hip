@@ -36,7 +36,6 @@ typedef short shortx8 __attribute__((ext_vector_type(8)));
 constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = kAttendWaves * kWave;
 constexpr int kThickRows = 32 * kAttendWaves;
-constexpr int kThinKeys = 32 * kAttendWaves;      // keys a turn of the four waves takes
 constexpr int kCUs = 256;
 // See Run.  kCost 0, 1, 2, 4: 64 sequences with 9 new tokens 102, 97, 100, 99 us.
 constexpr int kCost = 1, kThinLeast = 1;
@@ -675,15 +674,15 @@ struct Run {
 };
 
 // Finds this workgroup's run, of `count` at most, LEAST long at least (but for the last): its first unit and how far into it.
-// Every workgroup adds the requests up by itself, a quarter of them a wave, a request a lane or (with many row blocks) a row block
+// Every workgroup adds the requests up by itself, each wave its share of them, a request a lane or (with many row blocks) a row block
 // a lane: for 64 requests that takes two microseconds, less than a launch ahead would.  Lengths are whole numbers below 2^53 in
 // double, whose running sums go through DPP.
-template <int R, int TK, int LEAST>
+template <int R, int TK, int LEAST, int NW>
 __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsigned char *lds, Unit &u, int64_t &into) {
   double *sums = reinterpret_cast<double *>(lds);
-  int32_t *found = reinterpret_cast<int32_t *>(sums + kAttendWaves);
+  int32_t *found = reinterpret_cast<int32_t *>(sums + NW);
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int32_t quarter = (a.B + kAttendWaves - 1) / kAttendWaves, b_lo = min(wave * quarter, a.B), b_hi = min(b_lo + quarter, a.B);
+  const int32_t share = (a.B + NW - 1) / NW, b_lo = min(wave * share, a.B), b_hi = min(b_lo + share, a.B);
   // running sum of the lengths of requests b0 .. b0 + lane, all shared heads
   auto lengths = [&](int32_t b0, Unit &v, double &one) -> double {
     v.b = b0 + lane;
@@ -720,7 +719,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
   Run run;
   double sum = 0, before = 0;
 #pragma unroll
-  for (int w = 0; w < kAttendWaves; ++w) {
+  for (int w = 0; w < NW; ++w) {
     const double x = sums[w];
     if (w < wave) before += x;
     sum += x;
@@ -742,7 +741,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
   double ahead = (double) begin - before;
   if (0 <= ahead && ahead < mine) {
     for (int32_t b0 = b_lo; b0 < b_hi; b0 += kWave) {
-      if (quarter > kWave) upto = lengths(b0, v, one);
+      if (share > kWave) upto = lengths(b0, v, one);
       const uint64_t past = __builtin_amdgcn_ballot_w64(upto > ahead);
       if (!past) {
         ahead -= read_lane(upto, kWave - 1);
@@ -815,11 +814,11 @@ __device__ __forceinline__ void next_unit(const AttendArgs &a, Unit &u) {
 
 // Calls work(unit, first tile, tiles, part) for every unit or piece of one in this workgroup's run; part: NULL where the unit is
 // whole.  A workgroup has two places for parts: 1 for the unit that it begins and does not finish, 0 for one that another began.
-template <int DP, int R, int TK, int LEAST, typename Work>
+template <int DP, int R, int TK, int LEAST, int NW, typename Work>
 __device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *lds, Join *join, Part<DP, R> *parts, Work work) {
   Unit u;
   int64_t into = 0;
-  Run run = find_run<R, TK, LEAST>(a, (int32_t) gridDim.x, lds, u, into);
+  Run run = find_run<R, TK, LEAST, NW>(a, (int32_t) gridDim.x, lds, u, into);
   Join j{0, 0, 0, 0, 0};
   while (run.left > 0) {
     u = scalar(u);
@@ -1002,7 +1001,7 @@ __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) vo
   using W = Thick<T, DP, WK>;
   __shared__ __align__(16) unsigned char lds[W::kLds];
   __shared__ int odd;
-  work_on_run<DP, W::R, W::TK, W::kLeast>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
+  work_on_run<DP, W::R, W::TK, W::kLeast, kAttendWaves>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
     thick_piece<T, DP, WK, PAGES, ONCE>(a, u, tile, tiles, lds, &odd, (int) blockIdx.x / kCUs, part);
   });
 }
@@ -1078,12 +1077,16 @@ __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) vo
 
 // ---- 32 rows of float32 a workgroup ------------------------------------------------------------------------------------
 
+// Two waves of a workgroup where keys and values of four would fill the CU's shared memory: two workgroups then, less to join in each
+// (four waves and two, d = 128: 64 sequences of 500 keys with 5 new tokens 88 and 74 us, 4 of 4000 with one 55 and 47, 32 of 4000
+// with 8 240 and 244, 1 of 8000 with 8 40 and 43).
 template <int DP>
 struct Thin {
-  static constexpr int R = 32;
+  static constexpr int NW = DP == 64 ? 4 : 2;
+  static constexpr int R = 32, TK = 32 * NW;         // keys a turn of the waves takes
   static constexpr int kTile = 32 * DP * 4;
-  static constexpr int kLds = kAttendWaves * 2 * kTile;
-  static_assert(2 * R * (DP + 2) * 4 <= kLds, "two waves' rows on their way to the others");
+  static constexpr int kLds = NW * 2 * kTile;
+  static_assert(NW / 2 * R * (DP + 2) * 4 <= kLds, "half of the waves' rows on their way to the others");
   static constexpr int kRuns = 2 * kLds <= 160 * 1024 ? 512 : 256;       // what fits the chip at a time
 };
 
@@ -1099,8 +1102,8 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   const Loader<float, DP, 32, 1, PAGES, true> loader(a, u, lane, 0);
   constexpr int NI = decltype(loader)::NI;
   unsigned char *lk = lds + wave * 2 * W::kTile, *lv = lk + W::kTile;
-  int32_t k0 = u.k_lo + tile * kThinKeys + wave * 32;
-  const int32_t end = min(u.k_hi, u.k_lo + (tile + tiles) * kThinKeys);
+  int32_t k0 = u.k_lo + tile * W::TK + wave * 32;
+  const int32_t end = min(u.k_hi, u.k_lo + (tile + tiles) * W::TK);
   bare_barrier();                       // nobody uses the piece before any more
   const Row w = row_at(a, u, u.r0 + l32);
   const int32_t pos = w.pos;
@@ -1115,11 +1118,11 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   auto at_edge = [&](int32_t k) { return k + 32 > u.min_hi || k < u.max_lo; };
   bool odd = false;
   auto pages = loader.look_up(k0);      // of the keys that are brought next
-  // A turn works on keys k0 - kThinKeys and brings keys k0 behind it: one place in the code for each load.
-  for (bool now = false;; k0 += kThinKeys, now = true) {
+  // A turn works on keys k0 - W::TK and brings keys k0 behind it: one place in the code for each load.
+  for (bool now = false;; k0 += W::TK, now = true) {
     const bool more = k0 < end;
     if (!now && !more) break;
-    const int32_t k = k0 - kThinKeys;
+    const int32_t k = k0 - W::TK;
     floatx16 s[1];
     if (now) {
       wait_vm<NI>();                    // keys are in, values may be on their way
@@ -1144,24 +1147,24 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
     }
     if (!more) break;
     loader.template load<true>(k0, pages, lv);
-    pages = loader.look_up(k0 + kThinKeys);
+    pages = loader.look_up(k0 + W::TK);
   }
   if (odd) {
-    for (k0 = begin; k0 < end; k0 += kThinKeys)
+    for (k0 = begin; k0 < end; k0 += W::TK)
       if (at_edge(k0)) add_odd_values<float, DP, PAGES != 0>(a, u, k0, min(k0 + 32, u.k_hi), half, pos, before(), o);
   }
 
   // The waves' sums: 2 to 0 and 3 to 1, then 1 to 0.
   float *room = reinterpret_cast<float *>(lds);
   bare_barrier();
-  if (wave >= 2) give_rows<DP>(room + (wave - 2) * kRowsFloats<DP>, lane, o, ref, sum);
-  bare_barrier();
-  if (wave < 2) take_rows<DP>(room + wave * kRowsFloats<DP>, lane, o, ref, sum);
-  bare_barrier();
-  if (wave == 1) give_rows<DP>(room, lane, o, ref, sum);
-  bare_barrier();
+#pragma unroll
+  for (int n = W::NW / 2; n > 0; n /= 2) {
+    if (wave >= n && wave < 2 * n) give_rows<DP>(room + (wave - n) * kRowsFloats<DP>, lane, o, ref, sum);
+    bare_barrier();
+    if (wave < n) take_rows<DP>(room + wave * kRowsFloats<DP>, lane, o, ref, sum);
+    if (n > 1) bare_barrier();
+  }
   if (wave > 0) return;
-  take_rows<DP>(room, lane, o, ref, sum);
   sum = pair_sum(sum);
   int32_t r = l32;
   asm("" : "+v"(r));                    // formed here, not kept in registers since the beginning
@@ -1170,16 +1173,16 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   else store_row<float, DP>(a, out, half, o, sum);
 }
 
-// 32 rows of float32 over a cache.  A product of 32 x 32 x 2 keeps a SIMD 64 cycles whether 32 rows are there or 4, so that the four
+// 32 rows of float32 over a cache.  A product of 32 x 32 x 2 keeps a SIMD 64 cycles whether 32 rows are there or 4, so that the
 // waves of a CU have to share the keys, 32 each, with the loads of a wave's next keys ahead of its products with these: 32
-// sequences of 4000 keys, 8 new tokens of 4 heads a shared head, d = 128: 1053 MB in 231 us, 4.6 TB/s; 32 rows shared by two waves
-// 391 us, by one 577.  A short window (12 sequences, 1000 keys, d = 80, 39 MB) takes 38 us: 256 workgroups, one a CU, with some
-// tiles each, whose waits (for the run's first unit, its pages, its keys, the other waves' sums) nothing fills.
+// sequences of 4000 keys, 8 new tokens of 4 heads a shared head, d = 128: 1053 MB in 231 to 245 us, 4.3 to 4.6 TB/s; 32 rows shared
+// by two waves 391 us, by one 577.  A short window (12 sequences, 1000 keys, d = 80, 39 MB) takes 36 us: a run has a tile or two, whose
+// waits (for the run's first unit, its pages, its keys, the other waves' sums) nothing fills.
 template <int DP, int PAGES>
-__global__ __launch_bounds__(kAttendThreads, (Thin<DP>::kRuns / 256)) void attend_thin_kernel(AttendArgs a, Join *join,
+__global__ __launch_bounds__(Thin<DP>::NW * kWave, (Thin<DP>::kRuns * Thin<DP>::NW / 1024)) void attend_thin_kernel(AttendArgs a, Join *join,
                                                                                           Part<DP, 32> *parts) {
   __shared__ __align__(16) unsigned char lds[Thin<DP>::kLds];
-  work_on_run<DP, 32, kThinKeys, kThinLeast>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32> *part) {
+  work_on_run<DP, 32, Thin<DP>::TK, kThinLeast, Thin<DP>::NW>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32> *part) {
     thin_piece<DP, PAGES>(a, u, tile, tiles, lds, part);
   });
 }
@@ -1275,10 +1278,10 @@ template <typename T, int DP, int R>
 size_t parts_bytes(int32_t runs) { return join_bytes(runs) + 2 * (size_t) runs * sizeof(Part<DP, R>); }
 
 template <typename T, int DP, int R, typename Kernel>
-hipError_t split_launch(Kernel kernel, int32_t runs, const AttendArgs &a, void *workspace, hipStream_t stream) {
+hipError_t split_launch(Kernel kernel, int32_t runs, int threads, const AttendArgs &a, void *workspace, hipStream_t stream) {
   Join *join = reinterpret_cast<Join *>(workspace);
   Part<DP, R> *parts = reinterpret_cast<Part<DP, R> *>(reinterpret_cast<char *>(workspace) + join_bytes(runs));
-  kernel<<<runs, kAttendThreads, 0, stream>>>(a, join, parts);
+  kernel<<<runs, threads, 0, stream>>>(a, join, parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   attend_join_kernel<T, DP, R><<<dim3(runs, R == 128 ? 8 : R / 4), kJoinThreads, 0, stream>>>(a, join, parts);
@@ -1287,15 +1290,15 @@ hipError_t split_launch(Kernel kernel, int32_t runs, const AttendArgs &a, void *
 
 template <int DP>
 hipError_t go_thin(const AttendArgs &a, bool shared_pages, void *workspace, hipStream_t stream) {
-  if (shared_pages) return split_launch<float, DP, 32>(attend_thin_kernel<DP, 1>, Thin<DP>::kRuns, a, workspace, stream);
-  return split_launch<float, DP, 32>(attend_thin_kernel<DP, 2>, Thin<DP>::kRuns, a, workspace, stream);
+  if (shared_pages) return split_launch<float, DP, 32>(attend_thin_kernel<DP, 1>, Thin<DP>::kRuns, Thin<DP>::NW * kWave, a, workspace, stream);
+  return split_launch<float, DP, 32>(attend_thin_kernel<DP, 2>, Thin<DP>::kRuns, Thin<DP>::NW * kWave, a, workspace, stream);
 }
 
 template <typename T, int DP, int WK, bool ONCE>
 hipError_t go_thick(const AttendArgs &a, bool shared_pages, void *workspace, hipStream_t stream) {
   using W = Thick<T, DP, WK>;
-  if (shared_pages) return split_launch<T, DP, W::R>(attend_thick_kernel<T, DP, WK, 1, ONCE>, W::kRuns, a, workspace, stream);
-  return split_launch<T, DP, W::R>(attend_thick_kernel<T, DP, WK, 2, ONCE>, W::kRuns, a, workspace, stream);
+  if (shared_pages) return split_launch<T, DP, W::R>(attend_thick_kernel<T, DP, WK, 1, ONCE>, W::kRuns, kAttendThreads, a, workspace, stream);
+  return split_launch<T, DP, W::R>(attend_thick_kernel<T, DP, WK, 2, ONCE>, W::kRuns, kAttendThreads, a, workspace, stream);
 }
 
 template <typename T, int DP>
