@@ -994,7 +994,7 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
 // A cache's rows.  Few of them (WK 2): bound by memory, 32 sequences of 4000 keys with 9 new tokens 526 MB in 103 us, 5.1 TB/s, 2 of
 // 120 000 keys 5.7 TB/s, more than a copy reaches because nothing is written; one token of one sequence of 1500 keys is two
 // launches and the waits of one tile, 10.5 and 3.6 us.  Prompts by pieces (WK 1): 213 GFLOP in 300 to 318 us with the joining, 670 to
-// 710 TFLOP/s; bound as attend_prompt_kernel is, with 67 MB of parts written and read between.
+// 710 TFLOP/s; bound as attend_prompt_kernel is, with 60 MB of parts written and read between.
 template <typename T, int DP, int WK, int PAGES, bool ONCE>
 __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) void attend_thick_kernel(AttendArgs a, Join *join,
                                                                                                        Part<DP, Thick<T, DP, WK>::R> *parts) {
@@ -1192,7 +1192,7 @@ __global__ __launch_bounds__(Thin<DP>::NW * kWave, (Thin<DP>::kRuns * Thin<DP>::
 // Workgroups (i, y) join the parts of the unit that run i began and did not finish: outputs, references and sums of the parts are
 // brought to the largest reference, added and divided.  A wave a row, every second part to each half of it.  Bound by trips to
 // memory, a microsecond each: references, sums and first outputs are asked for together, 16 parts at a time, no more than there are.
-// 64 sequences (two or three parts a unit) 7.0 us, prompts by pieces (33 MB of parts) 18 us, 2 x 120 000 tokens (64 parts) 6 us.  A
+// 64 sequences (two or three parts a unit) 8 us, prompts by pieces (60 MB of parts) 20 us, 2 x 120 000 tokens (64 parts) 8 us.  A
 // kernel of its own because the next launch's start is the one meeting of all workgroups that a graph can hold.
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a, const Join *join, const Part<DP, R> *parts) {
