@@ -18,6 +18,8 @@ def test_kernels_fit(part, variants):
     assert len(mine) == variants
     for k in mine:
         assert not k[".vgpr_spill_count"] and not k[".private_segment_fixed_size"], k[".name"]
-        # two workgroups of four waves a compute unit, but for those whose keys and values fill its shared memory
+        # two workgroups a compute unit, but for those whose keys and values fill its shared memory: 512 registers a lane on each of
+        # four SIMDs
         if "attend" in part and k[".group_segment_fixed_size"] <= 80 * 1024:
-            assert k[".vgpr_count"] <= 256, k[".name"]
+            waves = -(-2 * k[".max_flat_workgroup_size"] // 64 // 4)
+            assert k[".vgpr_count"] * waves <= 512, k[".name"]
