@@ -1022,8 +1022,8 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
 
 // A cache's rows.  Few of them (WK 2): bound by memory, 32 sequences of 4000 keys with 9 new tokens 526 MB in 103 us, 5.1 TB/s, 2 of
 // 120 000 keys 5.7 TB/s, more than a copy reaches because nothing is written; one token of one sequence of 1500 keys is two
-// launches and the waits of one tile, 10.5 and 3.6 us.  Prompts by pieces (WK 1): 213 GFLOP in 300 to 318 us with the joining, 670 to
-// 710 TFLOP/s; bound as attend_prompt_kernel is, with 60 MB of parts written and read between.
+// launches and the waits of one tile, 10.5 and 3.6 us.  Prompts by pieces (WK 1): 213 GFLOP in 295 to 310 us with the joining, 690 to
+// 720 TFLOP/s; bound as attend_prompt_kernel is, with 60 MB of parts written and read between.
 template <typename T, int DP, int WK, int PAGES, bool ONCE>
 __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) void attend_thick_kernel(AttendArgs a, Join *join,
                                                                                                        Part<DP, Thick<T, DP, WK>::R> *parts) {
