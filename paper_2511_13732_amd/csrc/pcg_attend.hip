@@ -41,6 +41,7 @@ constexpr int kCUs = 256;
 constexpr int kCost = 1, kThinLeast = 1;
 constexpr int kJoinThreads = 256;
 constexpr float kLag = 8.f;        // how far (in powers of two) a maximum may run ahead of the one in use
+constexpr float kFar = 16777216.f; // where half a step of a reference is a factor of two
 
 // What is read where there is nothing to read: keys behind the last, columns behind D.
 __device__ const u32x4 kZeros = {0, 0, 0, 0};
@@ -369,11 +370,15 @@ __device__ __forceinline__ float row_max(const floatx16 (&s)[KB], float c) {
   return pair_max(fmaxf(m[0], m[1])) * c;
 }
 
+__device__ __forceinline__ float minus_ref(float ref) { return ref == -INFINITY ? 0.f : -ref; }
+
 // The rows' reference maxima follow the maxima where one runs more than kLag ahead (weights stay below 2^kLag, and sums
-// and outputs are rarely rescaled).
-template <int NO>
-__device__ __forceinline__ void follow(float mx, float &ref, float &sum, floatx16 (&o)[NO]) {
-  if (__builtin_amdgcn_ballot_w64(mx > ref + kLag) == 0) return;
+// and outputs are rarely rescaled).  What the row's scores are to be multiplied by for the weights is returned: c, and the exponent
+// c s - ref is then rounded once.  A reference is the rounded c m, though, half a step off, and beyond kFar that is a power of two of
+// its own, 2^8 where c m is 2^32: there the scores are replaced by the rounded c s, as the reference is, and 1 is returned.
+template <int NO, int KB>
+__device__ __forceinline__ float follow(float mx, float &ref, float &sum, floatx16 (&o)[NO], floatx16 (&s)[KB], float c) {
+  if (__builtin_amdgcn_ballot_w64(mx > ref + kLag || fabsf(minus_ref(ref)) > kFar) == 0) return c;
   const float now = fmaxf(ref, mx);
   const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
   ref = now;
@@ -382,10 +387,16 @@ __device__ __forceinline__ void follow(float mx, float &ref, float &sum, floatx1
   for (int n = 0; n < NO; ++n)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[n][r] *= f;
+  const bool far = fabsf(minus_ref(ref)) > kFar;
+  if (__builtin_amdgcn_ballot_w64(far) == 0) return c;
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[k][r] *= far ? c : 1.f;
+  return far ? 1.f : c;
 }
 
 // Scores to weights 2^(c s - ref), and their sum.
-__device__ __forceinline__ float minus_ref(float ref) { return ref == -INFINITY ? 0.f : -ref; }
 template <int KB>
 __device__ __forceinline__ void to_weights(floatx16 (&s)[KB], float c, float minus, float &sum) {
   float z[4] = {0.f, 0.f, 0.f, 0.f};
@@ -990,8 +1001,8 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
 #pragma unroll
         for (int i = 0; i < W::KB; ++i) hide(s[i], k + 32 * i, half, w.pos, lo);
       }
-      follow<S::NO>(row_max<W::KB>(s, a.c), ref, sum, o);
-      to_weights<W::KB>(s, a.c, minus_ref(ref), sum);
+      const float c = follow<S::NO, W::KB>(row_max<W::KB>(s, a.c), ref, sum, o, s, a.c);
+      to_weights<W::KB>(s, c, minus_ref(ref), sum);
       if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(1);
       add_values_in_steps<T, DP, W::KB>(lv, lane, s, o, a.D);
       if constexpr (S::kBf16) __builtin_amdgcn_s_setprio(0);
@@ -1163,8 +1174,8 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
     if (now) {
       const bool edge = at_edge(k);
       if (edge) hide(s[0], k, half, pos, before());
-      follow<S::NO>(row_max<1>(s, a.c), ref, sum, o);
-      to_weights<1>(s, a.c, minus_ref(ref), sum);
+      const float c = follow<S::NO, 1>(row_max<1>(s, a.c), ref, sum, o, s, a.c);
+      to_weights<1>(s, c, minus_ref(ref), sum);
       if (more) wait_vm<NI>();
       else wait_vm<0>();
       if (edge) {

@@ -1,0 +1,103 @@
+"""Attention where scores, weights or values are at the ends of what float32 holds, over the paged cache (pcg_cache_attend) and of
+packed prompts (pcg_prompt_attend).  Run with ``-m gpu`` on an MI355X."""
+import pytest
+import torch
+
+import paper_2511_13732_amd as pcg
+from test_gpu_attend import DTYPES, gen
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(*x):
+    return torch.tensor(x, dtype=torch.int32).cuda()
+
+
+def over_cache(q, k, v, window=0, scale=None, page_size=16):
+    """The last q.shape[0] tokens of one request of k.shape[0]."""
+    n, G, D = k.shape
+    m, blocks = q.shape[0], -(-n // page_size)
+    pad = lambda x: torch.cat([x, x.new_zeros((blocks * page_size - n, G, D))]).view(blocks, page_size, G, D).cuda()  # noqa: E731
+    table = torch.arange(blocks, dtype=torch.int32).view(1, -1).cuda()
+    return pcg.cache_attend(pcg.KvCache(pad(k), pad(v)), q.cuda(), table, ints(n - m), ints(0, m), longest=m, window=window, scale=scale).cpu()
+
+
+def as_prompt(q, k, v, window=0, scale=None, longest=None):
+    n = q.shape[0]
+    return pcg.prompt_attend(q.cuda(), k.cuda(), v.cuda(), ints(0, n), longest=longest or n, window=window, scale=scale).cpu()
+
+
+# ------------------------------------------------------------------------------------------------ scores
+
+# A score of 2^24 in powers of two is rounded by one; these are 2^16, 2^23 and more, up to 2^60.
+LARGE = [16, 23, 25, 31, 37, 60]
+
+
+def rounding(dtype):
+    """Relative to sum w |v|: a weight is w = 2^x of an exact x within [-2, 2] where keys are alike, the same for all; its rounding to
+    bf16, and of the output, half a step each; in float32 a sum of n products and one of n weights, a reciprocal and a product, within
+    (2 n + 8) steps of 2^-23."""
+    return (lambda n: (2 * n + 8) * 2.0 ** -23) if dtype == torch.float32 else (lambda n: 2.0 ** -8 * 2.02 + (2 * n + 8) * 2.0 ** -23)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", LARGE)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_keys_alike_count_alike_however_large_their_scores(dtype, D, power, sign):
+    """All keys the same: every row is the mean of the values that it sees, whatever the score."""
+    dt, n, H, G = DTYPES[dtype], 150, 4, 2
+    scale = 0.3
+    q = torch.randn((n, H, D), generator=gen(power)).abs() + 0.1
+    # q . k is D times 2^power or so, in powers of two
+    q = (q * 2.0 ** (power / 2)).to(dt)
+    k = (sign * (torch.randn((1, G, D), generator=gen(2)).abs() + 0.1) * 2.0 ** (power / 2)).to(dt).expand(n, G, D).contiguous()
+    v = torch.randn((n, G, D), generator=gen(3)).to(dt)
+    for window in (0, 1, 40):
+        lo = [max(0, t - window + 1) if window else 0 for t in range(n)]
+        mean = torch.stack([v[lo[t]:t + 1].double().mean(0) for t in range(n)]).repeat_interleave(H // G, 1)
+        mag = torch.stack([v[lo[t]:t + 1].double().abs().mean(0) for t in range(n)]).repeat_interleave(H // G, 1)
+        tol = rounding(dt)(n) * mag
+        for m in (1, 9, 70):
+            got = over_cache(q[n - m:], k, v, window, scale).double()
+            assert ((got - mean[n - m:]).abs() <= tol[n - m:]).all(), (window, m)
+        for longest in (1, n):
+            got = as_prompt(q, k, v, window, scale, longest).double()
+            assert ((got - mean).abs() <= tol).all(), (window, longest)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("best", [0, 63, 64, 100, 190])
+@pytest.mark.parametrize("long", [200, 9000])
+def test_the_largest_of_large_scores_has_all_the_weight(dtype, best, long):
+    """One key's score is 2^35 or more above all others: its value is the output."""
+    dt, H, G, D, m = DTYPES[dtype], 6, 3, 64, 5
+    n = long
+    q = ((torch.randn((m, H, D), generator=gen(best)).abs() + 0.1) * 2.0 ** 16).to(dt)
+    k = ((torch.randn((n, G, D), generator=gen(1)).abs() + 0.1) * 2.0 ** 16).to(dt)
+    k[best] = (k[best] * 0 + 2.0 ** 24).to(dt)
+    v = torch.randn((n, G, D), generator=gen(4)).to(dt)
+    want = v[best].double().repeat_interleave(H // G, 0)
+    got = over_cache(q, k, v).double()
+    assert ((got - want).abs() <= rounding(dt)(1) * want.abs()).all()
+    if n <= 200:
+        rows = torch.cat([q] * (n // m))
+        for longest in (1, n):
+            got = as_prompt(rows, k, v, longest=longest).double()[best:]
+            assert ((got - want).abs() <= rounding(dt)(1) * want.abs()).all()
+
+
+def test_a_far_row_does_not_move_the_others():
+    """Rows of the same block with ordinary scores keep their bits beside one whose scores are far out."""
+    dt, n, H, G, D = torch.float32, 96, 4, 1, 64
+    q, k, v = (torch.randn((n, h, D), generator=gen(s)).to(dt) for s, h in ((1, H), (2, G), (3, G)))
+    clean = as_prompt(q, k, v)
+    near = q.clone()
+    near[40, 2] *= 2.0 ** 30
+    far = as_prompt(near, k, v)
+    others = torch.ones((n, H), dtype=torch.bool)
+    others[40, 2] = False
+    # the references of a block may follow earlier beside it: the same sums from another reference, off by 2 n + 64 steps each way
+    off = (far - clean).abs()[others]
+    assert (off <= 2 * (2 * n + 64) * 2.0 ** -23 * v.abs().max()).all()
+    assert torch.isfinite(far).all()
