@@ -575,6 +575,16 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Unit &
   }
 }
 
+// A row without a score above -infinity is zeros, also where a value was not finite and its product with the weight zero is NaN.
+template <int NO>
+__device__ __forceinline__ void clear_empty(float sum, floatx16 (&o)[NO]) {
+  if (__builtin_amdgcn_ballot_w64(sum == 0.f) == 0) return;
+#pragma unroll
+  for (int n = 0; n < NO; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[n][r] = sum == 0.f ? 0.f : o[n][r];
+}
+
 // Where a row's query and output are, and its position.
 struct Row {
   bool there;
@@ -1027,6 +1037,7 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
     take_rows<DP>(room, lane, o, ref, sum);
   }
   sum = pair_sum(sum);
+  clear_empty<S::NO>(sum, o);
   if (part) store_part<DP, W::R>(part, row, half, w.there, o, ref, sum);
   else store_row<T, DP>(a, w, half, o, sum);
 }
@@ -1206,6 +1217,7 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   }
   if (wave > 0) return;
   sum = pair_sum(sum);
+  clear_empty<S::NO>(sum, o);
   int32_t r = l32;
   asm("" : "+v"(r));                    // formed here, not kept in registers since the beginning
   const Row out = row_at(a, u, u.r0 + r);
@@ -1290,10 +1302,13 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = 1.f / sum;
     T *out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) o[e] = pair_sum(o[e]) * inv;
+    for (int e = 0; e < kEach; ++e) {
+      o[e] = pair_sum(o[e]) * inv;
+      if (sum == 0.f) o[e] = 0.f;       // no score above -infinity, see clear_empty
+    }
     const int d = l32 * kEach;
     if (half || d >= a.D) continue;
     if constexpr (sizeof(T) == 2) {

@@ -101,3 +101,20 @@ def test_a_far_row_does_not_move_the_others():
     off = (far - clean).abs()[others]
     assert (off <= 2 * (2 * n + 64) * 2.0 ** -23 * v.abs().max()).all()
     assert torch.isfinite(far).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("n,m", [(40, 2), (40, 30), (300, 100), (7000, 1)])
+def test_rows_without_a_score_above_minus_infinity_are_zeros_whatever_the_values(dtype, bad, n, m):
+    """Every score -infinity, in one tile, several and in parts that are joined."""
+    dt, H, G, D = DTYPES[dtype], 3, 1, 64
+    q, k = torch.ones((m, H, D), dtype=dt), torch.full((n, G, D), -float("inf"), dtype=dt)
+    v = torch.randn((n, G, D), generator=gen(n)).to(dt)
+    v[::3, 0, 5] = bad
+    v[n // 2] = bad
+    for window in (0, 17):
+        assert (over_cache(q, k, v, window) == 0).all()
+        if m > 1:
+            for longest in (1, m):
+                assert (as_prompt(q, k[:m], v[:m], window, longest=longest) == 0).all()
