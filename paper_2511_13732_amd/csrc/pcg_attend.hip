@@ -520,7 +520,7 @@ __device__ __forceinline__ void add_values_in_steps(const unsigned char *lv, int
 
 // Zero times a value that is not finite would be NaN in the rows that do not see the value.  Where not all rows see all keys of a
 // tile, such values are therefore taken out of it (`threads` threads, this one `index`, `bytes` of values) and, if there were
-// any, put back afterwards where they are seen (add_odd_values).
+// any, added afterwards where they are seen (add_odd_values).
 template <bool BF16>
 __device__ __forceinline__ bool clear_odd_values(unsigned char *lv, int bytes, int index, int threads) {
   bool odd = false;
@@ -542,43 +542,94 @@ __device__ __forceinline__ bool clear_odd_values(unsigned char *lv, int bytes, i
   return odd;
 }
 
-// Adds the values that are not finite among keys [k0, k1) to the rows that see them.  (Their weights are positive, or so small that
-// they became zero, and then the product is NaN by the formula as well as here for a NaN.)
+// Whether an element is infinite or NaN.
+template <int NO>
+__device__ __forceinline__ bool any_odd(const floatx16 (&o)[NO]) {
+  float x = 0.f;                        // 0 * o is NaN then
+#pragma unroll
+  for (int n = 0; n < NO; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x = fmaf(o[n][r], 0.f, x);
+  return x != 0.f;
+}
+
+// Elements of rows that see a value among keys [k0, k1) which is not finite: the sum of those that the row sees, whatever their
+// weights.  By the formula every weight is positive; one that became zero, here or where a reference moved on, would make NaN of an
+// infinity, and which ones do depends on the tiles.  A wave looks at 64 keys at a time, a key a lane, and ends where all is NaN.
 template <typename T, int DP, bool PAGED>
-__device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Unit &u, int32_t k0, int32_t k1, int half, int32_t pos,
+__device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Unit &u, int32_t k0, int32_t k1, int lane, bool there, int32_t pos,
                                                int32_t lo, floatx16 (&o)[DP / 32]) {
-#pragma nounroll
-  for (int32_t key = k0; key < k1; ++key) {
+  using S = Shape<T, DP>;
+  const int half = lane >> 5;
+  auto find = [&](int32_t key) -> const T * {             // NULL: reads as zeros
     int64_t at = (int64_t) (u.first + key) * a.v_tok;
     if constexpr (PAGED) {
       uint32_t block, slot;
       split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
-      if (block >= (uint32_t) a.max_blocks) return;
-      const int32_t page = fixed_at(a.table, (int64_t) u.b * a.table_stride + block);
-      if ((uint32_t) page >= (uint32_t) a.num_pages) continue;
+      if (block >= (uint32_t) a.max_blocks) return nullptr;
+      const int32_t page = a.table[(int64_t) u.b * a.table_stride + block];
+      if ((uint32_t) page >= (uint32_t) a.num_pages) return nullptr;
       at = (int64_t) page * a.v_page + (int64_t) slot * a.v_tok;
     }
-    const T *v = reinterpret_cast<const T *>(a.v) + at + (int64_t) u.head * a.v_head;
-    const bool seen = key <= pos && key > lo;
+    return reinterpret_cast<const T *>(a.v) + at + (int64_t) u.head * a.v_head;
+  };
+  floatx16 odd[DP / 32];
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m) odd[m] = floatx16{};
+#pragma nounroll
+  for (; k0 < k1; k0 += kWave) {
+    bool here = false;
+    const T *v = k0 + lane < k1 ? find(k0 + lane) : nullptr;
+    if (v) {
+#pragma nounroll
+      for (int d = 0; d < a.D; d += S::E) here = not_finite<S::kBf16>(*reinterpret_cast<const u32x4 *>(v + d)) || here;
+    }
+    uint64_t who = __builtin_amdgcn_ballot_w64(here);
+    if (!who) continue;
+#pragma nounroll
+    for (; who; who &= who - 1) {
+      const int32_t key = k0 + __ffsll((long long) who) - 1;
+      const T *x = find(key);
+      const bool seen = key <= pos && key > lo;
+#pragma unroll
+      for (int m = 0; m < DP / 32; ++m) {
+        asm volatile("" ::: "memory");  // one block of columns after the other: there are no registers for all at a time
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = m * 32 + j * 8 + half * 4;
+          if (d >= a.D) continue;
+          floatx4 y;
+          if constexpr (S::kBf16) {
+            const u32x2 z = *reinterpret_cast<const u32x2 *>(x + d);
+            y = floatx4{__uint_as_float(z[0] << 16), __uint_as_float(z[0] & 0xffff0000u), __uint_as_float(z[1] << 16),
+                        __uint_as_float(z[1] & 0xffff0000u)};
+          } else {
+            y = *reinterpret_cast<const floatx4 *>(x + d);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (seen && !(fabsf(y[i]) < INFINITY)) odd[m][4 * j + i] += y[i];
+        }
+      }
+    }
+    bool open = false;
 #pragma unroll
     for (int m = 0; m < DP / 32; ++m)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int d = m * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-        float x = 0.f;
-        if (d < a.D) {
-          if constexpr (sizeof(T) == 2) x = __uint_as_float((uint32_t) v[d] << 16);
-          else x = v[d];
-        }
-        if (seen && !(fabsf(x) < INFINITY)) o[m][r] += x;
-      }
+      for (int r = 0; r < 16; ++r) open = open || (m * 32 + (r >> 2) * 8 + half * 4 < a.D && odd[m][r] == odd[m][r]);
+    if (__builtin_amdgcn_ballot_w64(open && there) == 0) break;
   }
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (odd[m][r] != 0.f) o[m][r] = odd[m][r];
 }
 
 // A row without a score above -infinity is zeros, also where a value was not finite and its product with the weight zero is NaN.
 template <int NO>
 __device__ __forceinline__ void clear_empty(float sum, floatx16 (&o)[NO]) {
-  if (__builtin_amdgcn_ballot_w64(sum == 0.f) == 0) return;
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(sum == 0.f) == 0, 1)) return;
 #pragma unroll
   for (int n = 0; n < NO; ++n)
 #pragma unroll
@@ -1022,11 +1073,7 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
     nxt = x;
   }
   bare_barrier();
-  if (*odd) {
-    for (k0 = begin; k0 < end; k0 += W::TK)
-      if (at_edge(k0))
-        add_odd_values<T, DP, PAGES != 0>(a, u, k0 + first_key, min(k0 + first_key + 32 * W::KB, u.k_hi), half, w.pos, lo, o);
-  }
+  const int cleared = *odd;
   if constexpr (WK > 1) {
     static_assert(WK == 2 && WR * kRowsFloats<DP> * 4 <= W::kLds, "the rows of the second half of the keys");
     float *room = reinterpret_cast<float *>(lds) + wave % WR * kRowsFloats<DP>;
@@ -1037,7 +1084,10 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
     take_rows<DP>(room, lane, o, ref, sum);
   }
   sum = pair_sum(sum);
-  clear_empty<S::NO>(sum, o);
+  // (of a row whose sum is NaN everything is)
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64((cleared || any_odd<S::NO>(o)) && sum == sum) != 0, 0))
+    add_odd_values<T, DP, PAGES != 0>(a, u, begin, end, lane, w.there, w.pos, lo, o);
+  if (!part) clear_empty<S::NO>(sum, o);
   if (part) store_part<DP, W::R>(part, row, half, w.there, o, ref, sum);
   else store_row<T, DP>(a, w, half, o, sum);
 }
@@ -1143,7 +1193,7 @@ struct Thin {
 
 template <int DP, int PAGES>
 __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
-                                           Part<DP, 32> *part) {
+                                           int *odd, Part<DP, 32> *part) {
   using S = Shape<float, DP>;
   using W = Thin<DP>;
   int tid = threadIdx.x;
@@ -1165,9 +1215,7 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
 #pragma unroll
   for (int n = 0; n < S::NO; ++n) o[n] = floatx16{};
   float ref = -INFINITY, sum = 0.f;
-  const int32_t begin = k0;
   auto at_edge = [&](int32_t k) { return k + 32 > u.min_hi || k < u.max_lo; };
-  bool odd = false;
   auto pages = loader.look_up(k0);      // of the keys that are brought next
   // A turn works on keys k0 - W::TK and brings keys k0 behind it: one place in the code for each load.
   for (bool now = false;; k0 += W::TK, now = true) {
@@ -1190,7 +1238,7 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
       if (more) wait_vm<NI>();
       else wait_vm<0>();
       if (edge) {
-        odd = __builtin_amdgcn_ballot_w64(clear_odd_values<false>(lv, W::kTile, lane, kWave)) != 0 || odd;
+        if (clear_odd_values<false>(lv, W::kTile, lane, kWave)) *odd = 1;
         wait_lds();
       }
       add_values<DP>(lv, lane, s[0], o, a.D);
@@ -1199,10 +1247,6 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
     if (!more) break;
     loader.template load<true>(k0, pages, lv);
     pages = loader.look_up(k0 + W::TK);
-  }
-  if (odd) {
-    for (k0 = begin; k0 < end; k0 += W::TK)
-      if (at_edge(k0)) add_odd_values<float, DP, PAGES != 0>(a, u, k0, min(k0 + 32, u.k_hi), half, pos, before(), o);
   }
 
   // The waves' sums: 2 to 0 and 3 to 1, then 1 to 0.
@@ -1217,10 +1261,15 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   }
   if (wave > 0) return;
   sum = pair_sum(sum);
-  clear_empty<S::NO>(sum, o);
   int32_t r = l32;
   asm("" : "+v"(r));                    // formed here, not kept in registers since the beginning
   const Row out = row_at(a, u, u.r0 + r);
+  // (of a row whose sum is NaN everything is)
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64((*odd || any_odd<S::NO>(o)) && sum == sum) != 0, 0))
+    add_odd_values<float, DP, PAGES != 0>(a, u, u.k_lo + tile * W::TK, end, lane, out.there, out.pos,
+                                          a.window > 0 ? out.pos - a.window : -1, o);
+  *odd = 0;                             // for the next piece, which begins with a barrier
+  if (!part) clear_empty<S::NO>(sum, o);
   if (part) store_part<DP, 32>(part, r, half, out.there, o, ref, sum);
   else store_row<float, DP>(a, out, half, o, sum);
 }
@@ -1234,8 +1283,10 @@ template <int DP, int PAGES>
 __global__ __launch_bounds__(Thin<DP>::NW * kWave, (Thin<DP>::kRuns * Thin<DP>::NW / 1024)) void attend_thin_kernel(AttendArgs a, Join *join,
                                                                                           Part<DP, 32> *parts) {
   __shared__ __align__(16) unsigned char lds[Thin<DP>::kLds];
+  __shared__ int odd;
+  if (threadIdx.x == 0) odd = 0;        // pieces come behind barriers
   work_on_run<DP, 32, Thin<DP>::TK, kThinLeast, Thin<DP>::NW>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32> *part) {
-    thin_piece<DP, PAGES>(a, u, tile, tiles, lds, part);
+    thin_piece<DP, PAGES>(a, u, tile, tiles, lds, &odd, part);
   });
 }
 
@@ -1287,7 +1338,10 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
       const float f = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
       top = now;
       sum = sum * before + (lane < n ? f * mine_sum : 0.f);
-      o *= before;
+      // what is not finite stays so where a factor has become zero, see add_odd_values
+      auto odd_at = [](float y, float by) { return by == 0.f && !(fabsf(y) < INFINITY); };
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) o[e] *= odd_at(o[e], before) ? 1.f : before;
       for (int32_t i = 0; i < n; i += 2 * kAtOnce) {
         if (i) ask(p0, i, n);
 #pragma unroll
@@ -1296,7 +1350,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
           const int32_t p = i + 2 * k + half;
           const float fp = __shfl(f, min(p, n - 1));
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) o[e] = p < n ? fmaf(fp, x[k][e], o[e]) : o[e];
+          for (int e = 0; e < kEach; ++e) o[e] = p < n ? fmaf(odd_at(x[k][e], fp) ? 1.f : fp, x[k][e], o[e]) : o[e];
         }
       }
     }

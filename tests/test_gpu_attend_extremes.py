@@ -3,6 +3,7 @@ packed prompts (pcg_prompt_attend).  Run with ``-m gpu`` on an MI355X."""
 import pytest
 import torch
 
+import attention as ref
 import paper_2511_13732_amd as pcg
 from test_gpu_attend import DTYPES, gen
 
@@ -118,3 +119,83 @@ def test_rows_without_a_score_above_minus_infinity_are_zeros_whatever_the_values
         if m > 1:
             for longest in (1, m):
                 assert (as_prompt(q, k[:m], v[:m], window, longest=longest) == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------ values
+
+def odd_rows(kind, n, G, D, dt, places, seed):
+    """Keys and values of which those at `places` are not finite: +infinity in column 3, -infinity in column 5, in column 7 first one and
+    then the other, NaN in column D - 1 of the last place.  "low": their weights are e^-500 or so beside the others'; "rising": so are those of the
+    first half of all keys."""
+    k, v = (torch.randn((n, G, D), generator=gen(s)) for s in (seed, seed + 1))
+    k *= 0.1
+    if kind == "low":
+        k[list(places)] = -8.0
+    if kind == "rising":
+        k[:n // 2] -= 8.0
+    k, v = k.to(dt), v.to(dt)
+    for i, j in enumerate(places):
+        v[j, 0, 3], v[j, 0, 5] = float("inf"), -float("inf")
+        v[j, 0, 7] = float("inf") if i % 2 == 0 else -float("inf")
+    v[places[-1], G - 1, D - 1] = float("nan")
+    return k, v
+
+
+def check_odd(got, q, k, v, first, window, dt):
+    """Rows of q at positions first, first + 1, ..: where a row sees values that are not finite their sum, and the definition elsewhere."""
+    m, H, D = q.shape
+    G = k.shape[1]
+    odd = torch.where(torch.isfinite(v), torch.zeros_like(v), v)
+    finite = torch.where(torch.isfinite(v), v, torch.zeros_like(v))
+    want = ref.attend_rows(q, k, finite, first, 1.0, window)
+    sums = torch.zeros((m, H, D), dtype=torch.float64)
+    for t in range(m):
+        p = first + t
+        lo = max(0, p - window + 1) if window else 0
+        sums[t] = odd[lo:p + 1].double().sum(0).repeat_interleave(H // G, 0)
+    plain = sums == 0
+    ref.check(torch.where(plain, got.double(), 0.0), tuple(torch.where(plain, x, 0.0) for x in want), dt)
+    bad = ~plain
+    same = (got.double() == sums) | (torch.isnan(got) & torch.isnan(sums))
+    assert same[bad].all(), (bad & ~same).nonzero()[0].tolist()
+
+
+KINDS = ["plain", "low", "rising"]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("places", [(0,), (5, 40), (63, 64, 200), (130, 299), (20, 21, 22, 90, 150)])
+def test_an_infinity_counts_whatever_its_weight_and_wherever_it_lies_in_a_prompt(dtype, D, kind, places):
+    dt, n, H, G = DTYPES[dtype], 300, 4, 2
+    k, v = odd_rows(kind, n, G, D, dt, places, D)
+    q = (torch.ones((n, H, D)) + 0.01 * torch.randn((n, H, D), generator=gen(9))).to(dt)
+    for window in (0, 90):
+        for longest in (1, n):
+            check_odd(as_prompt(q, k, v, window, 1.0, longest), q, k, v, 0, window, dt)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D,page_size", [(64, 16), (128, 16), (96, 5)])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,places", [(300, (0,)), (300, (70, 150)), (300, (31, 64, 299)), (9000, (10, 4000)), (9000, (2500, 8999))])
+def test_an_infinity_counts_whatever_its_weight_and_wherever_it_lies_in_a_cache(dtype, D, page_size, kind, n, places):
+    dt, H, G = DTYPES[dtype], 6, 2
+    k, v = odd_rows(kind, n, G, D, dt, places, D)
+    for m in (1, 9, 20, 70):
+        q = (torch.ones((m, H, D)) + 0.01 * torch.randn((m, H, D), generator=gen(m))).to(dt)
+        for window in (0, 120):
+            check_odd(over_cache(q, k, v, window, 1.0, page_size), q, k, v, n - m, window, dt)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_everything_not_finite(dtype):
+    """All values NaN, or all infinite: every element is, in as much time as one tile takes."""
+    dt, n, H, G, D = DTYPES[dtype], 2000, 4, 2, 128
+    k = torch.randn((n, G, D), generator=gen(1)).to(dt)
+    q = torch.randn((n, H, D), generator=gen(2)).to(dt)
+    for x in (float("nan"), float("inf")):
+        v = torch.full_like(k, x)
+        for got in (over_cache(q[:50], k, v), as_prompt(q[:300], k[:300], v[:300])):
+            assert (torch.isnan(got) if x != x else got == x).all()
