@@ -170,13 +170,14 @@ __device__ __forceinline__ int32_t request_ctx(const AttendArgs &a, int32_t b) {
 // 16 bytes a lane from memory to 1024 bytes of LDS in a row.  Written as instructions because the compiler waits for all such
 // loads in flight ahead of a transposing read of LDS (ds_read_b64_tr_b16), whatever buffer they fill; the kernels wait themselves
 // (wait_vm).  They bring nothing into registers, and what the compiler counts of its own loads stays right: it only waits longer.
-// The place in LDS is handed over in m0 as an operand, so that the compiler knows what m0 holds; a load may follow the move to m0 only
-// after another instruction.
+// The place in LDS is handed over in m0 as an operand, so that the compiler knows what m0 holds.  It sees no load in these, though, and
+// leaves no room ahead of one: a load may take an address from scalar registers five wait states after a vector instruction (a spilled
+// scalar's way back is one) wrote them, and m0 after one.  Hence s_nop 4.
 __device__ __forceinline__ uint32_t lds_address(const unsigned char *p) {
   return (uint32_t) (uintptr_t) (const __attribute__((address_space(3))) unsigned char *) p;
 }
 __device__ __forceinline__ void bring(const char *from, const unsigned char *to) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(from), "{m0}"(lds_address(to)) : "memory");
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(from), "{m0}"(lds_address(to)) : "memory");
 }
 // N of them to N KB in a row, load i from base + offset[i] - kBias + 1024 i: what an instruction's own offset adds to the place in
 // LDS it adds to the address as well.
@@ -186,14 +187,14 @@ constexpr uint32_t kBias = 3 * 1024;
 // have kept from call to call, 30 and 29; prompts by pieces, whose keys others read too, 370 and 316.
 #define PCG_BRING(HINT) \
   if constexpr (N == 4) { \
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %4" HINT "\n\tglobal_load_lds_dwordx4 %1, %4 offset:0x400" HINT \
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %4" HINT "\n\tglobal_load_lds_dwordx4 %1, %4 offset:0x400" HINT \
                  "\n\tglobal_load_lds_dwordx4 %2, %4 offset:0x800" HINT "\n\tglobal_load_lds_dwordx4 %3, %4 offset:0xc00" HINT \
                  :: "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base), "{m0}"(m) : "memory"); \
   } else if constexpr (N == 2) { \
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" HINT "\n\tglobal_load_lds_dwordx4 %1, %2 offset:0x400" HINT \
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %2" HINT "\n\tglobal_load_lds_dwordx4 %1, %2 offset:0x400" HINT \
                  :: "v"(offset[0]), "v"(offset[1]), "s"(base), "{m0}"(m) : "memory"); \
   } else { \
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" HINT :: "v"(offset[0]), "s"(base), "{m0}"(m) : "memory"); \
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" HINT :: "v"(offset[0]), "s"(base), "{m0}"(m) : "memory"); \
   }
 template <int N, bool ONCE>
 __device__ __forceinline__ void bring_some(const char *base, const uint32_t *offset, const unsigned char *to) {

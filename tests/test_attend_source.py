@@ -20,3 +20,16 @@ def test_no_instruction_written_by_hand_changes_m0_unseen():
                 assert '"{m0}"' in asm, (name, asm)
                 found += 1
     assert found >= 4
+
+
+def test_loads_written_by_hand_wait_for_scalars_that_the_vector_unit_wrote():
+    """Five wait states between a vector instruction that writes a scalar register and a load that takes its address from it: the
+    compiler keeps them for its own loads only."""
+    found = 0
+    for name in sorted(os.listdir(CSRC)):
+        text = open(os.path.join(CSRC, name)).read()
+        for asm in re.findall(r"asm volatile\((.*?)\);", text, re.S):
+            if "global_load_lds" in asm:
+                assert asm.lstrip().startswith('"s_nop 4\\n'), (name, asm)
+                found += 1
+    assert found >= 4
