@@ -683,7 +683,8 @@ def pages_step(pages: Pages, add, *, max_tokens: int, commit: Optional[torch.Ten
     """Between two forward passes: keeps ``commit + commit_extra`` tokens of every request's last chunk (all without
     ``commit``; after ``verify``: ``commit=out.accept_len, commit_extra=1``), adjusts the pages that it holds to ``add``
     new tokens (an int for all, or int32 [B]; negative: the request has ended) and says where each of them goes.
-    The state is updated in place, or written to ``state_out``."""
+    The state is updated in place, or written to ``state_out``.  ``out`` may have more rows than ``max_tokens``: no request gets
+    them, and they are filled like all others behind the last request's."""
     dev, B = pages.device, pages.B
     if out is None:
         out = pages_step_outputs(B, max_tokens, dev)
@@ -702,6 +703,9 @@ def pages_step(pages: Pages, add, *, max_tokens: int, commit: Optional[torch.Ten
           None if commit is None else commit.data_ptr(), _int31(commit_extra, "commit_extra", -1 << 31),
           add.data_ptr() if each else None, 0 if each else _int31(add, "add", -1 << 31), max_tokens, out.q_start.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(),
           out.refused.data_ptr())
+    for t, nothing in ((out.slots, -1), (out.positions, 0)):
+        if t.numel() > max_tokens:
+            t[max_tokens:].fill_(nothing)
     return out
 
 
