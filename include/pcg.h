@@ -518,7 +518,8 @@ typedef struct {
  * Between two forward passes: what is kept of the last chunk, pages back from those that need fewer, pages for the
  * next chunk, and where every new token goes.  For every request:
  *   kept = chunk, or with `commit` min(max(commit[b] + commit_extra, 0), chunk); after pcg_verify commit is its accept_len
- *          and commit_extra 1 (the token that the chunk began with and the accepted ones)
+ *          and commit_extra 1 (the token that the chunk began with and the accepted ones).  With `commit` it is read for every
+ *          request: for one whose last chunk was a prompt or a piece of one, which stays whole, it has to be the chunk's length or more
  *   len += kept; add (add[b], or add_all with add NULL) new tokens follow; add < 0: the request has ended, len = 0 and
  *   all of its pages go back (an empty place, to which a later call with add > 0 brings a new request)
  * and holds ceil((len + add) / page_size) pages afterwards.  Pages that are given back are pushed on the stack in the

@@ -681,7 +681,8 @@ def pages_step_outputs(B: int, max_tokens: int, device) -> PagesStep:
 def pages_step(pages: Pages, add, *, max_tokens: int, commit: Optional[torch.Tensor] = None, commit_extra: int = 0,
                state_out: Optional[torch.Tensor] = None, out: Optional[PagesStep] = None) -> PagesStep:
     """Between two forward passes: keeps ``commit + commit_extra`` tokens of every request's last chunk (all without
-    ``commit``; after ``verify``: ``commit=out.accept_len, commit_extra=1``), adjusts the pages that it holds to ``add``
+    ``commit``; after ``verify``: ``commit=out.accept_len, commit_extra=1``, with 1 << 30 or so for a request whose chunk was a
+    prompt or a piece of one and stays whole), adjusts the pages that it holds to ``add``
     new tokens (an int for all, or int32 [B]; negative: the request has ended) and says where each of them goes.
     The state is updated in place, or written to ``state_out``.  ``out`` may have more rows than ``max_tokens``: no request gets
     them, and they are filled like all others behind the last request's."""
