@@ -608,8 +608,25 @@ def _int31(x: int, what: str, least: int = 0) -> int:
     return x
 
 
+class _Handle:
+    """A dataclass whose ``__post_init__`` checks its fields and forms ``_ref``, the library's structure with their addresses: a field
+    that is given another value is checked and taken over, or stays what it was."""
+
+    def __setattr__(self, name, value):
+        if name not in self.__dataclass_fields__ or "_ref" not in self.__dict__:
+            return object.__setattr__(self, name, value)
+        was = getattr(self, name)
+        object.__setattr__(self, name, value)
+        try:
+            self.__post_init__()
+        except Exception:
+            object.__setattr__(self, name, was)
+            self.__post_init__()
+            raise
+
+
 @dataclass
-class Pages:
+class Pages(_Handle):
     """The pages of a K/V cache that B requests hold (pcg_pages and its state): ``block_table`` int32 [B, max_blocks] (rows
     may be strided), ``free_pages`` int32 [num_pages], a stack whose first ``free_count`` entries nobody holds, and
     ``state`` int32 [3 B + 1]: tokens in the cache for good, pages held and tokens of the last chunk of every request, then
@@ -711,7 +728,7 @@ def pages_step(pages: Pages, add, *, max_tokens: int, commit: Optional[torch.Ten
 
 
 @dataclass
-class KvCache:
+class KvCache(_Handle):
     """Keys and values of one layer, [num_pages, page_size, kv_heads, head_dim] each, float32 or bfloat16, the last axis
     contiguous and the same strides in both ([num_pages, kv_heads, page_size, head_dim] transposed is as good)."""
     k: torch.Tensor
