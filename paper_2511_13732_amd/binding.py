@@ -625,6 +625,12 @@ class _Handle:
             raise
 
 
+def _sizes31(any_of: int):
+    """Refuses sizes of tensors, or-ed, that the library would take for others in 32 bits."""
+    if any_of >> 31:
+        raise ValueError("a tensor has a size of 2^31 or more")
+
+
 @dataclass
 class Pages(_Handle):
     """The pages of a K/V cache that B requests hold (pcg_pages and its state): ``block_table`` int32 [B, max_blocks] (rows
@@ -646,6 +652,7 @@ class Pages(_Handle):
         _int32(self.state, 3 * self.B + 1, t.device, "state")
         self.device = t.device
         _int31(self.page_size, "page_size", 1)
+        _sizes31(self.B | self.max_blocks | self.num_pages)
         self._ref = C.pointer(_PagesStruct(self.B, self.num_pages, self.page_size, self.max_blocks, t.data_ptr(),
                                     t.stride(0) if self.B > 1 else self.max_blocks, self.free_pages.data_ptr()))
 
@@ -741,6 +748,7 @@ class KvCache(_Handle):
         if k.stride(3) != 1:
             raise ValueError("the last axis of the cache must be contiguous")
         self.num_pages, self.page_size, self.kv_heads, self.head_dim = k.shape
+        _sizes31(self.num_pages | self.page_size | self.kv_heads | self.head_dim)
         self.device, self.dtype = k.device, k.dtype
         self._ref = C.pointer(_KvCacheStruct(k.data_ptr(), v.data_ptr(), _dtype_code(k), *k.shape, *k.stride()[:3]))
 
@@ -788,6 +796,7 @@ def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, len
         raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
     _int32(lens, B, dev, "lens")
     _int32(q_start, B + 1, dev, "q_start")
+    _sizes31(heads | B | block_table.shape[1])
     if longest is None:
         longest = -(-T // max(B, 1))
     if workspace is None:
@@ -814,6 +823,7 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: to
         out = torch.zeros((T, heads, head_dim), dtype=dtype, device=dev)
     os_ = _rows(out, T, heads, head_dim, dtype, dev, "out")
     _int32(q_start, B + 1, dev, "q_start")
+    _sizes31(heads | kv_heads | head_dim | B)
     if longest is None:
         longest = -(-T // max(B, 1))
     _call(dev, "pcg_prompt_attend", lib().pcg_prompt_attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q), T, heads,

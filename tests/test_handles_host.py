@@ -46,3 +46,26 @@ def test_a_pool_whose_tensors_are_replaced_names_the_new_ones():
     # two states in turn, as a caller does who keeps the last one
     pages.state, other = i(13), pages.state
     assert other is state
+
+
+def test_sizes_that_the_library_would_take_for_others_are_refused():
+    """Beyond 2^31, on a device that holds no memory."""
+    far = (1 << 32) + 8
+    new = lambda *s, dtype=torch.bfloat16: torch.empty(s, dtype=dtype, device="meta")  # noqa: E731
+    i = lambda *s: new(*s, dtype=torch.int32)  # noqa: E731
+    for shape in ((far, 1, 1, 8), (1, far, 1, 8), (1, 1, far, 8), (1, 1, 1, far)):
+        with pytest.raises(ValueError):
+            pcg.KvCache(new(*shape), new(*shape))
+    for table, free in ((i(far, 1), i(4)), (i(1, far), i(4)), (i(1, 1), i(far))):
+        with pytest.raises(ValueError):
+            pcg.Pages(table, free, i(3 * table.shape[0] + 1), 1)
+    cache = pcg.KvCache(new(4, 16, 1, 8), new(4, 16, 1, 8))
+    ws = torch.empty(1 << 10, dtype=torch.uint8, device="meta")
+    good = dict(q=new(3, 2, 8), block_table=i(2, 3), lens=i(2), q_start=i(3))
+    for bad in (dict(q=new(1, far, 8)), dict(block_table=i(2, far)), dict(block_table=i(far, 3), lens=i(far), q_start=i(far + 1))):
+        with pytest.raises(ValueError):
+            pcg.cache_attend(cache, workspace=ws, **{**good, **bad})
+    for q, k, b in ((new(1, far, 8), new(1, 1, 8), 2), (new(1, far, 8), new(1, far, 8), 2), (new(1, 1, far), new(1, 1, far), 2),
+                    (new(1, 1, 8), new(1, 1, 8), far + 1)):
+        with pytest.raises(ValueError):
+            pcg.prompt_attend(q, k, k, i(b))
