@@ -1360,10 +1360,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
       const float f = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
       top = now;
       sum = sum * before + (lane < n ? f * mine_sum : 0.f);
-      // what is not finite stays so where a factor has become zero, see add_odd_values
-      auto odd_at = [](float y, float by) { return by == 0.f && !(fabsf(y) < INFINITY); };
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) o[e] *= odd_at(o[e], before) ? 1.f : before;
+      o *= before;
       for (int32_t i = 0; i < n; i += 2 * kAtOnce) {
         if (i) ask(p0, i, n);
 #pragma unroll
@@ -1372,7 +1369,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
           const int32_t p = i + 2 * k + half;
           const float fp = __shfl(f, min(p, n - 1));
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) o[e] = p < n ? fmaf(odd_at(x[k][e], fp) ? 1.f : fp, x[k][e], o[e]) : o[e];
+          for (int e = 0; e < kEach; ++e) o[e] = p < n ? fmaf(fp, x[k][e], o[e]) : o[e];
         }
       }
     }
@@ -1381,10 +1378,26 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
     const float inv = 1.f / sum;
     T *out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      o[e] = pair_sum(o[e]) * inv;
-      if (sum == 0.f) o[e] = 0.f;       // no score above -infinity, see clear_empty
+    for (int e = 0; e < kEach; ++e) o[e] = pair_sum(o[e]);
+    float odd = 0.f;                    // NaN if an element is not finite
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) odd = fmaf(o[e], 0.f, odd);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0.f) != 0, 0)) {
+      // what is not finite in a part is so in the sum, also where its factor is zero, see add_odd_values
+      vec all = {};
+#pragma nounroll
+      for (int32_t p = 0; p < j.parts; ++p) {
+        const vec y = *reinterpret_cast<const vec *>(&part_at(p).o[row][l32 * kEach]);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+          if (!(fabsf(y[e]) < INFINITY)) all[e] += y[e];
+      }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (all[e] != 0.f) o[e] = all[e];
     }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) o[e] = sum == 0.f ? 0.f : o[e] * inv;        // see clear_empty
     const int d = l32 * kEach;
     if (half || d >= a.D) continue;
     if constexpr (sizeof(T) == 2) {
