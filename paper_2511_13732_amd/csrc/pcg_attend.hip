@@ -523,7 +523,7 @@ __device__ __forceinline__ void add_values_in_steps(const unsigned char *lv, int
 
 // Zero times a value that is not finite would be NaN in the rows that do not see the value.  Where not all rows see all keys of a
 // tile, such values are therefore taken out of it (`threads` threads, this one `index`, `bytes` of values) and, if there were
-// any, added afterwards where they are seen (add_odd_values).
+// any, put afterwards where they are seen (put_odd_values).
 template <bool BF16>
 __device__ __forceinline__ bool clear_odd_values(unsigned char *lv, int bytes, int index, int threads) {
   bool odd = false;
@@ -557,11 +557,12 @@ __device__ __forceinline__ bool any_odd(const floatx16 (&o)[NO]) {
 }
 
 // Elements of rows that see a value among keys [k0, k1) which is not finite: the sum of those that the row sees, whatever their
-// weights.  By the formula every weight is positive; one that became zero, here or where a reference moved on, would make NaN of an
-// infinity, and which ones do depends on the tiles.  A wave looks at 64 keys at a time, a key a lane, and ends where all is NaN.
-template <typename T, int DP, bool PAGED>
-__device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Unit &u, int32_t k0, int32_t k1, int lane, bool there, int32_t pos,
-                                               int32_t lo, floatx16 (&o)[DP / 32]) {
+// weights, goes to put(column, sum).  By the formula every weight is positive; one that became zero, here or where a reference moved
+// on, would make NaN of an infinity, and which ones do depends on the tiles.  A wave looks at 64 keys at a time, a key a lane, and ends
+// where all is NaN.  Called when the rows are stored, so that it needs none of their registers.
+template <typename T, int DP, bool PAGED, typename Put>
+__device__ __forceinline__ void put_odd_values(const AttendArgs &a, const Unit &u, int32_t k0, int32_t k1, int lane, bool there, int32_t pos,
+                                               int32_t lo, Put put) {
   using S = Shape<T, DP>;
   const int half = lane >> 5;
   auto find = [&](int32_t key) -> const T * {             // NULL: reads as zeros
@@ -626,17 +627,7 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Unit &
   for (int m = 0; m < DP / 32; ++m)
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      if (odd[m][r] != 0.f) o[m][r] = odd[m][r];
-}
-
-// A row without a score above -infinity is zeros, also where a value was not finite and its product with the weight zero is NaN.
-template <int NO>
-__device__ __forceinline__ void clear_empty(float sum, floatx16 (&o)[NO]) {
-  if (__builtin_expect(__builtin_amdgcn_ballot_w64(sum == 0.f) == 0, 1)) return;
-#pragma unroll
-  for (int n = 0; n < NO; ++n)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[n][r] = sum == 0.f ? 0.f : o[n][r];
+      if (there && odd[m][r] != 0.f) put(m * 32 + (r >> 2) * 8 + half * 4 + (r & 3), odd[m][r]);
 }
 
 // Where a row's query and output are, and its position.
@@ -667,13 +658,15 @@ __device__ __forceinline__ void load_query(const AttendArgs &a, const Row &w, in
   }
 }
 
-// A row's output from its half in this lane: d = 32 n + 8 j + 4 half + i in register 4 j + i of o[n].
+// A row's output from its half in this lane: d = 32 n + 8 j + 4 half + i in register 4 j + i of o[n].  A row without a score above
+// -infinity is zeros, also where a value was not finite and its product with the weight zero is NaN.
 template <typename T, int DP>
 __device__ __forceinline__ void store_row(const AttendArgs &a, const Row &w, int half, const floatx16 (&o)[Shape<T, DP>::NO],
                                           float sum) {
   using S = Shape<T, DP>;
   if (!w.there) return;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = 1.f / sum;
+  auto of = [&](float x) { return sum == 0.f ? 0.f : x * inv; };
   T *out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
 #pragma unroll
   for (int n = 0; n < S::NO; ++n)
@@ -682,14 +675,28 @@ __device__ __forceinline__ void store_row(const AttendArgs &a, const Row &w, int
       const int d = n * 32 + j * 8 + half * 4;
       if (d >= a.D) continue;
       if constexpr (S::kBf16) {
-        const floatx2 x = {o[n][4 * j] * inv, o[n][4 * j + 1] * inv}, y = {o[n][4 * j + 2] * inv, o[n][4 * j + 3] * inv};
+        const floatx2 x = {of(o[n][4 * j]), of(o[n][4 * j + 1])}, y = {of(o[n][4 * j + 2]), of(o[n][4 * j + 3])};
         *reinterpret_cast<u32x2 *>(out + d) = u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2)),
                                                     __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2))};
       } else {
-        *reinterpret_cast<floatx4 *>(out + d) = floatx4{o[n][4 * j] * inv, o[n][4 * j + 1] * inv, o[n][4 * j + 2] * inv,
-                                                        o[n][4 * j + 3] * inv};
+        *reinterpret_cast<floatx4 *>(out + d) = floatx4{of(o[n][4 * j]), of(o[n][4 * j + 1]), of(o[n][4 * j + 2]), of(o[n][4 * j + 3])};
       }
     }
+}
+
+// One element of it that is not finite.
+template <typename T>
+__device__ __forceinline__ void put_out(const AttendArgs &a, const Row &w, int d, float x) {
+  T *out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
+  if constexpr (sizeof(T) == 2) out[d] = __builtin_bit_cast(uint16_t, (__bf16) x);
+  else out[d] = x;
+}
+
+// Whether rows of this wave need put_odd_values: values were taken out of a tile, or an element is not finite.  (Of a row whose sum is NaN
+// everything is.)
+template <int NO>
+__device__ __forceinline__ bool odd_rows(bool cleared, const floatx16 (&o)[NO], float sum) {
+  return __builtin_amdgcn_ballot_w64((cleared || any_odd<NO>(o)) && sum == sum) != 0;
 }
 
 // ---- parts of a unit whose keys are split over workgroups ------------------------------------------------------------------
@@ -1087,12 +1094,16 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
     take_rows<DP>(room, lane, o, ref, sum);
   }
   sum = pair_sum(sum);
-  // (of a row whose sum is NaN everything is)
-  if (__builtin_expect(__builtin_amdgcn_ballot_w64((cleared || any_odd<S::NO>(o)) && sum == sum) != 0, 0))
-    add_odd_values<T, DP, PAGES != 0>(a, u, begin, end, lane, w.there, w.pos, lo, o);
-  if (!part) clear_empty<S::NO>(sum, o);
+  const bool again = odd_rows<S::NO>(cleared, o, sum);
   if (part) store_part<DP, W::R>(part, row, half, w.there, o, ref, sum);
   else store_row<T, DP>(a, w, half, o, sum);
+  if (__builtin_expect(again, 0)) {
+    const bool put = w.there && (part || sum != 0.f);
+    put_odd_values<T, DP, PAGES != 0>(a, u, begin, end, lane, put, w.pos, lo, [&](int d, float x) {
+      if (part) part->o[row][d] = x;
+      else put_out<T>(a, w, d, x);
+    });
+  }
 }
 
 // A cache's rows.  Few of them (WK 2): bound by memory, 32 sequences of 4000 keys with 9 new tokens 526 MB in 103 us, 5.1 TB/s, 2 of
@@ -1286,14 +1297,18 @@ __device__ __forceinline__ void thin_piece(const AttendArgs &a, const Unit &u, i
   int32_t r = l32;
   asm("" : "+v"(r));                    // formed here, not kept in registers since the beginning
   const Row out = row_at(a, u, u.r0 + r);
-  // (of a row whose sum is NaN everything is)
-  if (__builtin_expect(__builtin_amdgcn_ballot_w64((*odd || any_odd<S::NO>(o)) && sum == sum) != 0, 0))
-    add_odd_values<float, DP, PAGES != 0>(a, u, u.k_lo + tile * W::TK, end, lane, out.there, out.pos,
-                                          a.window > 0 ? out.pos - a.window : -1, o);
+  const bool again = odd_rows<S::NO>(*odd, o, sum);
   *odd = 0;                             // for the next piece, which begins with a barrier
-  if (!part) clear_empty<S::NO>(sum, o);
   if (part) store_part<DP, 32>(part, r, half, out.there, o, ref, sum);
   else store_row<float, DP>(a, out, half, o, sum);
+  if (__builtin_expect(again, 0)) {
+    const bool put = out.there && (part || sum != 0.f);
+    put_odd_values<float, DP, PAGES != 0>(a, u, u.k_lo + tile * W::TK, end, lane, put, out.pos, a.window > 0 ? out.pos - a.window : -1,
+                                          [&](int d, float x) {
+      if (part) part->o[r][d] = x;
+      else put_out<float>(a, out, d, x);
+    });
+  }
 }
 
 // 32 rows of float32 over a cache.  A product of 32 x 32 x 2 keeps a SIMD 64 cycles whether 32 rows are there or 4, so that the
@@ -1383,7 +1398,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
 #pragma unroll
     for (int e = 0; e < kEach; ++e) odd = fmaf(o[e], 0.f, odd);
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0.f) != 0, 0)) {
-      // what is not finite in a part is so in the sum, also where its factor is zero, see add_odd_values
+      // what is not finite in a part is so in the sum, also where its factor is zero, see put_odd_values
       vec all = {};
 #pragma nounroll
       for (int32_t p = 0; p < j.parts; ++p) {
@@ -1397,7 +1412,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
         if (all[e] != 0.f) o[e] = all[e];
     }
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) o[e] = sum == 0.f ? 0.f : o[e] * inv;        // see clear_empty
+    for (int e = 0; e < kEach; ++e) o[e] = sum == 0.f ? 0.f : o[e] * inv;        // see store_row
     const int d = l32 * kEach;
     if (half || d >= a.D) continue;
     if constexpr (sizeof(T) == 2) {
