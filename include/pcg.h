@@ -556,7 +556,8 @@ int pcg_cache_write(const pcg_kv_cache *cache, const void *k_new, const void *v_
  * with the softmax's maximum, sum and products in float32; with PCG_BF16 the weights are rounded to bf16 where they
  * multiply values.  A row that sees no key, or none whose score is above -infinity, gives zeros.  What stands in keys and values that a
  * row does not see has no effect on it, infinities and NaN included; elements of values that it sees and that are not finite add up to
- * that row's element of the output, however small their weights (by the formula none is zero).
+ * that row's element of the output, however small their weights (by the formula none is zero).  Outputs are divided at the end: up to
+ * 2^8 times the sum of the absolute values that a row sees has to stay within float32.
  *   q, out        DEVICE [T, heads, head_dim] of the cache's dtype, strides in elements as in pcg_cache_write; out must not
  *                 overlap what is read.  T * heads < 2^28, B * kv_heads < 2^22.  Rows behind q_start[B] are not read and not written.
  *   block_table   DEVICE as in pcg_pages.  Keys in pages outside [0, num_pages) or past max_blocks read as zeros.

@@ -37,7 +37,7 @@ constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = kAttendWaves * kWave;
 constexpr int kThickRows = 32 * kAttendWaves;
 constexpr int kCUs = 256;
-// See Run.  kCost 0, 1, 2, 4: 64 sequences with 9 new tokens 102, 97, 100, 99 us.
+// See Run.  kCost 0, 1, 2, 4: 64 sequences with 9 new tokens 82.5, 79.2, 76.9, 77.8 us, prompts by pieces 267, 262, 257, 258.
 constexpr int kCost = 1, kThinLeast = 1;
 constexpr int kJoinThreads = 256;
 constexpr int kOrdered = 128;      // see find_place
@@ -904,8 +904,8 @@ __device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *
   Join j{0, 0, 0, 0, 0};
   // Where a head's keys are read by several row blocks, the end of a unit that another run began comes last: the runs of an XCD then
   // begin with units from their first key on, and those of one head read the same keys at the same time, out of its L2 (us with
-  // and without: 1 sequence of 60 000 keys with 2048 new tokens 2194 and 2435, 4 of 8000 with 1024 646 and 667, prompts by pieces 295
-  // and 302, 4 of 1000 with 200 55 and 53).
+  // and without: 1 sequence of 60 000 keys with 2048 new tokens 2004 and 2176, 4 of 8000 with 1024 579 and 612, prompts by pieces 262
+  // and 278, 4 of 1000 with 200 51.3 and 51.8).
   int32_t rest_tile = 0, rest_tiles = 0, rest_b = 0, rest_head = 0, rest_r0 = 0;
   while (run.left > 0 || rest_tiles > 0) {
     int32_t tile, tiles;
@@ -1003,7 +1003,7 @@ struct Thick {
   static constexpr int TK = 32 * KB * WK;
   static constexpr int kTile = TK * S::RB;
   static constexpr int kLds = 4 * kTile;            // keys and values, two of each
-  static constexpr int kRuns = 2 * kLds < 160 * 1024 ? 512 : 256;        // what fits the chip at a time
+  static constexpr int kRuns = 2 * kLds < 160 * 1024 ? 512 : 256;        // two a CU (up to d = 64 three would fit) or one
   // See Run.  us with runs of 1, 2, 3 and 5 tiles at least, bf16, d = 128: 64 rows, 1 sequence of 1000 keys 13.6 14.5 18.1 20.6, of
   // 8000 27 27 25 24, 8 of 2000 24 24 24 24; 128 rows, 1 of 1000 18 18 21 24, of 8000 39 39 32 28, 4 of 4000 (d = 64) 27 27 27 27.
   static constexpr int kLeast = WK == 1 ? 5 : 1;
@@ -1108,8 +1108,8 @@ __device__ __forceinline__ void thick_piece(const AttendArgs &a, const Unit &u, 
 
 // A cache's rows.  Few of them (WK 2): bound by memory, 32 sequences of 4000 keys with 9 new tokens 526 MB in 103 us, 5.1 TB/s, 2 of
 // 120 000 keys 5.7 TB/s, more than a copy reaches because nothing is written; one token of one sequence of 1500 keys is two
-// launches and the waits of one tile, 10.5 and 3.6 us.  Prompts by pieces (WK 1): 213 GFLOP in 295 to 310 us with the joining, 690 to
-// 720 TFLOP/s; bound as attend_prompt_kernel is, with 60 MB of parts written and read between.
+// launches and the waits of one tile, 9.5 and 3.5 us.  Prompts by pieces (WK 1): 213 GFLOP in 257 to 278 us with the joining, 770 to
+// 830 TFLOP/s; bound as attend_prompt_kernel is, with 60 MB of parts written and read between.
 template <typename T, int DP, int WK, int PAGES, bool ONCE>
 __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) void attend_thick_kernel(AttendArgs a, Join *join,
                                                                                                        Part<DP, Thick<T, DP, WK>::R> *parts) {
@@ -1184,12 +1184,12 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, int32_t place, U
   return back >= 0 && u.r0 >= 0;
 }
 
-// A unit a workgroup, no parts: there are enough of them.  Bound by the SIMDs' issue: products keep the matrix units busy 49 % of
+// A unit a workgroup, no parts: there are enough of them.  Bound by the SIMDs' issue: products keep the matrix units busy 51 % of
 // the time (bf16, d = 128; no LDS conflicts), exponentials, maxima, sums and rounding beside them are 7.4 vector instructions for
-// every product.  27 000 tokens of prompts up to 8000, 32 heads: 1.23 PFLOP in 1275 us, 968 TFLOP/s (a library product of
+// every product.  27 000 tokens of prompts up to 8000, 32 heads: 1.23 PFLOP in 1255 us, 984 TFLOP/s (a library product of
 // 8192 x 8192 reaches 1117 here).  Left out of it for a measurement: the exponential 1147, the loads 1095, the weights' product
 // 924, the scores' 945 us.  Scores of the next tile beside the weights of this one (1382 us), 256 rows a workgroup by eight waves
-// (1275) or by four with two blocks of rows (2096) were not faster.  fp32, d = 64, 9 prompts of 1111 tokens: 80 TFLOP/s, 95 us, the
+// (1275 against 1262) or by four with two blocks of rows (2096) were not faster.  fp32, d = 64, 9 prompts of 1111 tokens: 80 TFLOP/s, 95 us, the
 // matrix units busy half of the time too.
 template <typename T, int DP, int WK>
 __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) void attend_prompt_kernel(AttendArgs a) {
@@ -1221,7 +1221,7 @@ struct Thin {
   static constexpr int kTile = 32 * DP * 4;
   static constexpr int kLds = NW * 2 * kTile;
   static_assert(NW / 2 * R * (DP + 2) * 4 <= kLds, "half of the waves' rows on their way to the others");
-  static constexpr int kRuns = 2 * kLds <= 160 * 1024 ? 512 : 256;       // what fits the chip at a time
+  static constexpr int kRuns = 2 * kLds <= 160 * 1024 ? 512 : 256;       // two a CU
 };
 
 template <int DP, int PAGES>
@@ -1332,7 +1332,7 @@ __global__ __launch_bounds__(Thin<DP>::NW * kWave, (Thin<DP>::kRuns * Thin<DP>::
 // Workgroups (i, y) join the parts of the unit that run i began and did not finish: outputs, references and sums of the parts are
 // brought to the largest reference, added and divided.  A wave a row, every second part to each half of it.  Bound by trips to
 // memory, a microsecond each: references, sums and first outputs are asked for together, 16 parts at a time, no more than there are.
-// 64 sequences (two or three parts a unit) 8 us, prompts by pieces (60 MB of parts) 20 us, 2 x 120 000 tokens (64 parts) 8 us.  A
+// 64 sequences (two or three parts a unit) 8 us, prompts by pieces (60 MB of parts) 20 us, 2 x 120 000 tokens (33 parts) 8 us.  A
 // kernel of its own because the next launch's start is the one meeting of all workgroups that a graph can hold.
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a, const Join *join, const Part<DP, R> *parts) {
@@ -1355,7 +1355,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
     vec o = {};
     float sum = 0.f, top = -INFINITY;
     vec x[kAtOnce];
-    // One, four or all eight (one by one: prompts by pieces 1 % faster, a single token's 64 parts 2 % slower; always eight:
+    // One, four or all eight (one by one: prompts by pieces 1 % faster, a single token's parts 2 % slower; always eight:
     // 5 % slower and the same).
     auto from = [](int32_t k) { return k < 1 ? 0 : k < 4 ? 2 : 8; };
     auto ask = [&](int32_t p0, int32_t i, int32_t n) {

@@ -176,7 +176,8 @@ __global__ __launch_bounds__(THREADS) void pages_step_kernel(PagesArgs p, int32_
   for (int64_t row = tid; row < p.max_tokens; row += kFillAtOnce * THREADS) place_tokens<kFillAtOnce>(p, starts, lens, all, row, THREADS);
 }
 
-// More requests than threads: the same in two passes over them, because who gets pages depends on all that come back.
+// More requests than threads: the same in two passes over them, because who gets pages depends on all that come back.  Requests of
+// 4 tokens: 1025 in 19 us, 2600 in 27, 8192 in 61; 65 536 of one token in 432.
 __global__ __launch_bounds__(kPagesThreads) void pages_step_large_kernel(PagesArgs p, int32_t fill_rows) {
   __shared__ int64_t part64[kPagesWaves];
   __shared__ int32_t part[kPagesWaves];
