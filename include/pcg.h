@@ -549,7 +549,37 @@ int pcg_cache_write(const pcg_kv_cache *cache, const void *k_new, const void *v_
                     void *hip_stream);
 
 /*
- * Attention of the new tokens of B requests over the cache, their own keys and values written before (pcg_cache_write).
+ * How keys and queries are turned by their positions.  The structure is HOST; table is DEVICE float32, row p (of position p) at
+ * table + p * stride: the cosines of dim / 2 angles, then their sines.  dim is even, from 2 to head_dim; elements of a head
+ * behind the first dim stay as they are.  Pair i, turned by angle i, are elements i and i + dim / 2, or with `interleaved` 2 i and 2 i + 1:
+ *   (x, y) -> (x cos - y sin, y cos + x sin)
+ * formed in double and rounded once to float32, and from there to the type that it is stored in.
+ */
+typedef struct {
+  const float *table;
+  int64_t stride;
+  int32_t positions, dim, interleaved;
+} pcg_rotation;
+
+/*
+ * pcg_cache_write with the rotation of a step's queries and keys on the way: keys k_new, turned, and values v_new, as they are, to the slots
+ * slots[t], queries q, turned, to q_out.  One launch for what otherwise takes a pass over the queries, one over the keys and pcg_cache_write.
+ *   rotation      HOST or NULL: keys are stored as they are, and q must be NULL
+ *   positions     DEVICE int32 [T]: every row's position (pcg_pages_step writes them); NULL without rotation
+ *   q, q_out      DEVICE [T, heads, head_dim] of the cache's dtype, strides in elements as in pcg_cache_write; q NULL: no queries.  q_out may
+ *                 be q itself with the same strides (rows are then turned in place), and must not overlap it otherwise
+ *   k_new, v_new, slots   as in pcg_cache_write; they must not overlap what is written
+ * Rows whose slot is negative or past the cache's last, or whose position is negative or past the table's last, are left out: nothing of
+ * them is written, their queries included.  A slot must not be named twice.  T * ((heads + 2 kv_heads) (head_dim / 4 + 2) + 32
+ * kv_heads + 512) < 2^31.  T == 0 is a no-op.
+ */
+int pcg_cache_append(const pcg_kv_cache *cache, const pcg_rotation *rotation, const int32_t *positions, const void *q,
+                     int64_t q_tok_stride, int64_t q_head_stride, int32_t heads, void *q_out, int64_t q_out_tok_stride,
+                     int64_t q_out_head_stride, const void *k_new, int64_t k_tok_stride, int64_t k_head_stride, const void *v_new,
+                     int64_t v_tok_stride, int64_t v_head_stride, int64_t T, const int32_t *slots, void *hip_stream);
+
+/*
+ * Attention of the new tokens of B requests over the cache, their own keys and values written before (pcg_cache_write, pcg_cache_append).
  * Row t of request b (row q_start[b] + t of the batch) is at position p = lens[b] + t and sees the keys j of its request with
  * p - window < j <= p (window 0: all j <= p):
  *   out = sum_j softmax_j(scale * q . k_j) v_j
@@ -586,6 +616,64 @@ int pcg_prompt_attend(const void *q, const void *k, const void *v, pcg_dtype dt,
                       int64_t k_head_stride, int64_t v_tok_stride, int64_t v_head_stride, const int32_t *q_start, int32_t B,
                       int64_t longest, float scale, int32_t window, void *out, int64_t out_tok_stride,
                       int64_t out_head_stride, void *hip_stream);
+
+/*
+ * The keys and values of one layer in pages, in 4 bits: about a quarter of the memory of bfloat16, and of the bytes that attention reads.
+ * An element is scale * code.  A code has a sign (bit 3), two bits of exponent and one of mantissa: 0 .. 7 are 0, 1/2, 1, 3/2, 2, 3, 4, 6, 8 .. 15
+ * their negatives.  Every token has a bfloat16 scale for its key and one for its value in each shared head.
+ *   k, v     element i of the key of slot s of page p for shared head h: the low (i even) or high half of byte
+ *            k[p * page_stride + s * slot_stride + h * head_stride + i / 2]; a head takes ceil(head_dim / 32) * 16 bytes, the last of
+ *            which may lie behind head_dim and mean nothing.  Aligned to 16 bytes; strides in bytes, positive multiples of 16
+ *   scales   scales[2 * (p * scale_page_stride + s * scale_slot_stride + h * scale_head_stride)] is the key's, the one behind it the
+ *            value's; strides in such pairs, positive.  Aligned to 4 bytes.  A scale that is not finite makes all of its elements NaN
+ *   kv_heads, head_dim, num_pages, page_size   as in pcg_kv_cache
+ * The pages of a request (pcg_pages) are the same as for any cache.  Attention reads fastest where a head's slots of a page lie in a row:
+ * [page, head, slot, bytes].
+ */
+typedef struct {
+  uint8_t *k, *v;
+  uint16_t *scales;
+  int32_t num_pages, page_size, kv_heads, head_dim;
+  int64_t page_stride, slot_stride, head_stride;
+  int64_t scale_page_stride, scale_slot_stride, scale_head_stride;
+} pcg_kv4_cache;
+
+/*
+ * pcg_cache_append into a cache of 4 bits; rows of q, k_new, v_new and q_out are of type dt.  Of a head's elements x (keys turned and
+ * rounded to float32):
+ *   scale = max |x| / 6 rounded to bfloat16 (nearest, ties to even; at most 0x1.54p125, so that 6 scales are finite)
+ *   code  = the nearest of the eight values to |x| / scale, ties to the even code, and the sign of x; 0 where scale is 0
+ * exactly: both are what exact arithmetic on those float32 numbers gives.  Where an element is infinite or NaN the scale is NaN and
+ * the codes are 0: the whole key or value of that head is NaN.  Codes behind head_dim are 0.  Slots of a page that are not named keep what
+ * they hold.
+ */
+int pcg_cache4_append(const pcg_kv4_cache *cache, pcg_dtype dt, const pcg_rotation *rotation, const int32_t *positions, const void *q,
+                      int64_t q_tok_stride, int64_t q_head_stride, int32_t heads, void *q_out, int64_t q_out_tok_stride,
+                      int64_t q_out_head_stride, const void *k_new, int64_t k_tok_stride, int64_t k_head_stride, const void *v_new,
+                      int64_t v_tok_stride, int64_t v_head_stride, int64_t T, const int32_t *slots, void *hip_stream);
+
+/*
+ * What the cache holds at slots[t], as values: rows t of k_out and v_out (DEVICE [T, kv_heads, head_dim] of type dt, strides as in
+ * pcg_cache_write), scale * code, exact in float32, rounded to dt.  Rows whose slot is negative or
+ * past the cache's last stay as they were.  A slot may be named more than once.  T * (kv_heads * head_dim / 4 + 256) < 2^31.
+ */
+int pcg_cache4_read(const pcg_kv4_cache *cache, pcg_dtype dt, void *k_out, int64_t k_tok_stride, int64_t k_head_stride, void *v_out,
+                    int64_t v_tok_stride, int64_t v_head_stride, int64_t T, const int32_t *slots, void *hip_stream);
+
+/*
+ * pcg_cache_attend over a cache of 4 bits; queries and outputs are of type dt.  Keys and values are the scale * code that the cache stands for, not
+ * rounded to dt; with PCG_BF16 a weight times its value's scale is rounded to bfloat16 where it multiplies codes, with PCG_F32 all 24 bits of it and
+ * of the queries are multiplied.  A value that is NaN makes all elements of its head NaN in the rows that see it.  Everything else as there.
+ *   workspace     DEVICE, >= pcg_cache4_attend_workspace_bytes(B, T, heads, kv_heads, head_dim, longest)
+ */
+int pcg_cache4_attend(const pcg_kv4_cache *cache, pcg_dtype dt, const void *q, int64_t q_tok_stride, int64_t q_head_stride,
+                      int32_t heads, int64_t T, const int32_t *block_table, int64_t table_stride, int32_t max_blocks,
+                      const int32_t *lens, const int32_t *q_start, int32_t B, int64_t longest, float scale, int32_t window,
+                      void *out, int64_t out_tok_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes,
+                      void *hip_stream);
+
+size_t pcg_cache4_attend_workspace_bytes(int32_t B, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                         int64_t longest);
 
 /* ---- per-kernel timing (for the benchmark) ------------------------------------------------ */
 

@@ -56,6 +56,19 @@ class _KvCacheStruct(C.Structure):
                 ("head_stride", C.c_int64)]
 
 
+class _RotationStruct(C.Structure):
+    """Mirror of pcg_rotation."""
+    _fields_ = [("table", C.c_void_p), ("stride", C.c_int64), ("positions", C.c_int32), ("dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class _KvCache4Struct(C.Structure):
+    """Mirror of pcg_kv4_cache."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("scales", C.c_void_p), ("num_pages", C.c_int32), ("page_size", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("scale_page_stride", C.c_int64), ("scale_slot_stride", C.c_int64),
+                ("scale_head_stride", C.c_int64)]
+
+
 class Diag(C.Structure):
     """Mirror of pcg_diag (eight uint32 counters)."""
     _fields_ = [(n, C.c_uint32) for n in
@@ -139,6 +152,19 @@ def lib() -> C.CDLL:
                                        C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64,
                                        C.c_float, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_size_t,
                                        C.c_void_p]
+        rows = [C.POINTER(_RotationStruct), C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_int64,
+                C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p]
+        L.pcg_cache_append.restype = C.c_int
+        L.pcg_cache_append.argtypes = [C.POINTER(_KvCacheStruct)] + rows
+        L.pcg_cache4_append.restype = C.c_int
+        L.pcg_cache4_append.argtypes = [C.POINTER(_KvCache4Struct), C.c_int] + rows
+        L.pcg_cache4_read.restype = C.c_int
+        L.pcg_cache4_read.argtypes = [C.POINTER(_KvCache4Struct), C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64,
+                                      C.c_int64, C.c_int64, C.c_void_p, C.c_void_p]
+        L.pcg_cache4_attend_workspace_bytes.restype = C.c_size_t
+        L.pcg_cache4_attend_workspace_bytes.argtypes = L.pcg_cache_attend_workspace_bytes.argtypes
+        L.pcg_cache4_attend.restype = C.c_int
+        L.pcg_cache4_attend.argtypes = [C.POINTER(_KvCache4Struct), C.c_int] + L.pcg_cache_attend.argtypes[1:]
         L.pcg_prompt_attend.restype = C.c_int
         L.pcg_prompt_attend.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32,
                                         C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
@@ -777,20 +803,16 @@ def cache_attend_workspace_bytes(B: int, rows: int, heads: int, kv_heads: int, h
     return lib().pcg_cache_attend_workspace_bytes(B, rows, heads, kv_heads, head_dim, longest)
 
 
-def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor, *,
-                 longest: Optional[int] = None, scale: Optional[float] = None, window: int = 0,
-                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Attention of new tokens over the cache that holds their own keys and values already: ``q`` [T, heads, head_dim], the
-    rows q_start[b] .. q_start[b + 1] of request b at positions lens[b], lens[b] + 1, .. (pages_step: ``pages.lens``), each
-    seeing the keys up to itself, with ``window`` the last that many of them.  ``longest`` bounds the new tokens of a request
-    (it decides how the work is cut; without it: the mean).  ``out`` must not overlap what is read.  ``scale`` is 1 / sqrt(head_dim) unless given.  Rows of ``out`` behind
-    the last request's stay as they were (zeros where ``out`` is not given)."""
+def _attend(name: str, cache, dtype: tuple, workspace_bytes, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor,
+            q_start: torch.Tensor, longest: Optional[int], scale: Optional[float], window: int, out: Optional[torch.Tensor],
+            workspace: Optional[torch.Tensor]) -> torch.Tensor:
+    """Checks and makes the library's call `name` over a cache; `dtype`: the queries' type, where the cache does not say it."""
     T, heads, head_dim = q.shape
-    dev, B = cache.device, lens.numel()
-    qs = _rows(q, T, heads, cache.head_dim, cache.dtype, dev, "q")
+    dev, B, of = cache.device, lens.numel(), q.dtype if dtype else cache.dtype
+    qs = _rows(q, T, heads, cache.head_dim, of, dev, "q")
     if out is None:
-        out = torch.zeros((T, heads, head_dim), dtype=q.dtype, device=dev)
-    os_ = _rows(out, T, heads, head_dim, cache.dtype, dev, "out")
+        out = torch.zeros((T, heads, head_dim), dtype=of, device=dev)
+    os_ = _rows(out, T, heads, head_dim, of, dev, "out")
     if block_table.dim() != 2 or block_table.dtype is not torch.int32 or block_table.shape[0] != B or block_table.device != dev or \
             (block_table.shape[1] > 1 and block_table.stride(1) != 1):
         raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
@@ -800,14 +822,157 @@ def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, len
     if longest is None:
         longest = -(-T // max(B, 1))
     if workspace is None:
-        workspace = _workspace(dev, cache_attend_workspace_bytes(B, T, heads, cache.kv_heads, head_dim, longest))
+        workspace = _workspace(dev, workspace_bytes(B, T, heads, cache.kv_heads, head_dim, longest))
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
-    _call(dev, "pcg_cache_attend", lib().pcg_cache_attend, cache._ref, q.data_ptr(), *qs, heads, T, block_table.data_ptr(),
+    _call(dev, name, getattr(lib(), name), cache._ref, *dtype, q.data_ptr(), *qs, heads, T, block_table.data_ptr(),
           block_table.stride(0), block_table.shape[1], lens.data_ptr(), q_start.data_ptr(), B, longest,
           head_dim ** -0.5 if scale is None else scale, _int31(window, "window"), out.data_ptr(), *os_, workspace.data_ptr(),
           workspace.numel())
     return out
+
+
+def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor, *,
+                 longest: Optional[int] = None, scale: Optional[float] = None, window: int = 0,
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of new tokens over the cache that holds their own keys and values already: ``q`` [T, heads, head_dim], the
+    rows q_start[b] .. q_start[b + 1] of request b at positions lens[b], lens[b] + 1, .. (pages_step: ``pages.lens``), each
+    seeing the keys up to itself, with ``window`` the last that many of them.  ``longest`` bounds the new tokens of a request
+    (it decides how the work is cut; without it: the mean).  ``out`` must not overlap what is read.  ``scale`` is 1 / sqrt(head_dim) unless given.  Rows of ``out`` behind
+    the last request's stay as they were (zeros where ``out`` is not given)."""
+    return _attend("pcg_cache_attend", cache, (), cache_attend_workspace_bytes, q, block_table, lens, q_start, longest, scale, window,
+                   out, workspace)
+
+
+@dataclass
+class Rotation(_Handle):
+    """How keys and queries are turned by their positions (pcg_rotation): ``table`` float32 [positions, dim], rows contiguous, the
+    cosines of dim / 2 angles and then their sines.  Pair i are elements i and i + dim / 2 of a head, with ``interleaved`` 2 i and
+    2 i + 1; elements behind the first dim stay as they are."""
+    table: torch.Tensor
+    interleaved: bool = False
+
+    def __post_init__(self):
+        t = self.table
+        if t.dim() != 2 or t.dtype is not torch.float32 or t.shape[0] < 1 or t.shape[1] < 2 or t.shape[1] % 2 or t.stride(1) != 1:
+            raise ValueError("table must be float32 [positions, dim], dim even, with contiguous rows")
+        self.positions, self.dim = t.shape
+        _sizes31(self.positions | self.dim)
+        self.device = t.device
+        self._ref = C.pointer(_RotationStruct(t.data_ptr(), t.stride(0) if self.positions > 1 else self.dim, self.positions, self.dim,
+                                              bool(self.interleaved)))
+
+    @classmethod
+    def of(cls, positions: int, dim: int, device, base: float = 10000.0, interleaved: bool = False) -> "Rotation":
+        """The table of the angles position * base^(-2 i / dim), formed in double."""
+        at = torch.arange(dim // 2, dtype=torch.float64, device=device)
+        angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * base ** (-2.0 * at / dim)
+        return cls(torch.cat([angle.cos(), angle.sin()], dim=1).float(), interleaved)
+
+
+def _append(name: str, cache, dtype: tuple, k, v, slots, rotation: Optional[Rotation], positions, q, q_out):
+    T, dev, of = slots.numel(), cache.device, k.dtype if dtype else cache.dtype
+    ks = _rows(k, T, cache.kv_heads, cache.head_dim, of, dev, "k")
+    vs = _rows(v, T, cache.kv_heads, cache.head_dim, of, dev, "v")
+    _int32(slots, T, dev, "slots")
+    if rotation is not None:
+        if rotation.device != dev:
+            raise ValueError(f"the rotation's table must be on {dev}")
+        if positions is None:
+            raise ValueError("a rotation needs positions")
+        _int32(positions, T, dev, "positions")
+    elif q is not None or positions is not None:
+        raise ValueError("queries and positions without a rotation")
+    heads, qs, os_ = 0, (0, 0), (0, 0)
+    if q is not None:
+        heads = q.shape[1]
+        qs = _rows(q, T, heads, cache.head_dim, of, dev, "q")
+        if q_out is None:
+            q_out = torch.zeros((T, heads, cache.head_dim), dtype=of, device=dev)
+        os_ = _rows(q_out, T, heads, cache.head_dim, of, dev, "q_out")
+        _sizes31(heads)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _call(dev, name, getattr(lib(), name), cache._ref, *dtype, None if rotation is None else rotation._ref,
+          None if rotation is None else positions.data_ptr(), None if q is None else q.data_ptr(), *qs, heads,
+          None if q is None else q_out.data_ptr(), *os_, k.data_ptr(), *ks, v.data_ptr(), *vs, T, slots.data_ptr())
+    return q_out
+
+
+def cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *, rotation: Optional[Rotation] = None,
+                 positions: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                 q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """``cache_write`` with the rotation on the way: keys [T, kv_heads, head_dim], turned by their ``positions`` (int32 [T], as
+    pages_step gives them), and values to their ``slots``; queries ``q`` [T, heads, head_dim], turned, to ``q_out``, which is returned (and
+    may be ``q``).  Rows whose slot is negative, or whose position the table does not have, are left out, their queries too (zeros where
+    ``q_out`` is not given)."""
+    return _append("pcg_cache_append", cache, (), k, v, slots, rotation, positions, q, q_out)
+
+
+@dataclass
+class KvCache4(_Handle):
+    """Keys and values of one layer in 4 bits (pcg_kv4_cache): ``k`` and ``v`` uint8 [num_pages, page_size, kv_heads,
+    ceil(head_dim / 32) * 16], two codes a byte, the last axis contiguous and the same strides in both; ``scales`` bfloat16 [num_pages,
+    page_size, kv_heads, 2], a key's and a value's, the last axis contiguous."""
+    k: torch.Tensor
+    v: torch.Tensor
+    scales: torch.Tensor
+    head_dim: int
+
+    def __post_init__(self):
+        k, v, s = self.k, self.v, self.scales
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype is not torch.uint8 or v.dtype is not torch.uint8 or \
+                k.device != v.device or k.stride(3) != 1 or k.shape[3] != -(-self.head_dim // 32) * 16:
+            raise ValueError("k and v must be alike: uint8 [num_pages, page_size, kv_heads, ceil(head_dim / 32) * 16], the last axis contiguous")
+        if s.shape != (*k.shape[:3], 2) or s.dtype is not torch.bfloat16 or s.device != k.device or s.stride(3) != 1 or \
+                any(n > 1 and x % 2 for n, x in zip(s.shape[:3], s.stride())):
+            raise ValueError("scales must be bfloat16 [num_pages, page_size, kv_heads, 2] beside k and v, in contiguous pairs")
+        self.num_pages, self.page_size, self.kv_heads = k.shape[:3]
+        _sizes31(self.num_pages | self.page_size | self.kv_heads)
+        _int31(self.head_dim, "head_dim", 8)
+        self.device = k.device
+        self._ref = C.pointer(_KvCache4Struct(k.data_ptr(), v.data_ptr(), s.data_ptr(), *k.shape[:3], self.head_dim, *k.stride()[:3],
+                                              *(x // 2 for x in s.stride()[:3])))
+
+    @classmethod
+    def empty(cls, num_pages: int, page_size: int, kv_heads: int, head_dim: int, device) -> "KvCache4":
+        """Zeros, a head's slots of a page in a row."""
+        new = lambda n, dtype: torch.zeros((num_pages, kv_heads, page_size, n), dtype=dtype, device=device).transpose(1, 2)  # noqa: E731
+        row = -(-head_dim // 32) * 16
+        return cls(new(row, torch.uint8), new(row, torch.uint8), new(2, torch.bfloat16), head_dim)
+
+
+def cache4_append(cache: KvCache4, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *, rotation: Optional[Rotation] = None,
+                  positions: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                  q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """``cache_append`` into a cache of 4 bits: every key and value of a head gets its scale and codes.  Rows are float32 or bfloat16."""
+    return _append("pcg_cache4_append", cache, (_dtype_code(k),), k, v, slots, rotation, positions, q, q_out)
+
+
+def cache4_read(cache: KvCache4, slots: torch.Tensor, *, dtype: torch.dtype = torch.bfloat16, out=None):
+    """What the cache holds at ``slots`` (int32 [T]; negative: left as it was), as values of ``dtype``: (k, v) [T, kv_heads, head_dim] each,
+    zeros where nothing is read, or the two tensors of ``out``."""
+    T, dev = slots.numel(), cache.device
+    if out is None:
+        out = tuple(torch.zeros((T, cache.kv_heads, cache.head_dim), dtype=dtype, device=dev) for _ in range(2))
+    k, v = out
+    ks = _rows(k, T, cache.kv_heads, cache.head_dim, k.dtype, dev, "out[0]")
+    vs = _rows(v, T, cache.kv_heads, cache.head_dim, k.dtype, dev, "out[1]")
+    _int32(slots, T, dev, "slots")
+    _call(dev, "pcg_cache4_read", lib().pcg_cache4_read, cache._ref, _dtype_code(k), k.data_ptr(), *ks, v.data_ptr(), *vs, T, slots.data_ptr())
+    return k, v
+
+
+def cache4_attend_workspace_bytes(B: int, rows: int, heads: int, kv_heads: int, head_dim: int, longest: int) -> int:
+    return lib().pcg_cache4_attend_workspace_bytes(B, rows, heads, kv_heads, head_dim, longest)
+
+
+def cache4_attend(cache: KvCache4, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor, *,
+                  longest: Optional[int] = None, scale: Optional[float] = None, window: int = 0,
+                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``cache_attend`` over a cache of 4 bits; queries and outputs are float32 or bfloat16."""
+    return _attend("pcg_cache4_attend", cache, (_dtype_code(q),), cache4_attend_workspace_bytes, q, block_table, lens, q_start, longest, scale,
+                   window, out, workspace)
 
 
 def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor, *, longest: Optional[int] = None,

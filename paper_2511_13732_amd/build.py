@@ -7,9 +7,10 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpcg.so")
-SOURCES = ["pcg_kernels.hip", "pcg_asg.hip", "pcg_cache.hip", "pcg_attend.hip", "pcg_api.cpp", "pcg_cache_api.cpp",
+SOURCES = ["pcg_kernels.hip", "pcg_asg.hip", "pcg_cache.hip", "pcg_attend.hip", "pcg_append.hip", "pcg_attend4.hip",
+           "pcg_api.cpp", "pcg_cache_api.cpp",
            "pcg_prepare.cpp"]
-HEADERS = ["pcg_kernels.h", "pcg_device.h", "pcg_layout.h", "pcg_cache.h", "pcg_attend.h",
+HEADERS = ["pcg_kernels.h", "pcg_device.h", "pcg_layout.h", "pcg_cache.h", "pcg_attend.h", "pcg_attend_device.h",
            os.path.join("..", "..", "include", "pcg.h")]
 
 HIPCC_FLAGS = [

@@ -22,8 +22,17 @@ struct AttendArgs {
   float c;                         // log2(e) * scale
 };
 
+// A cache of 4-bit codes: k and v are bytes, their strides in bytes; the scales of a token's key and value are two bfloat16 at
+// scales + page * s_page + slot * s_tok + head * s_head, strides in such pairs.
+struct Attend4Args : AttendArgs {
+  const uint32_t *scales;
+  int64_t s_page, s_tok, s_head;
+};
+
 size_t attend_workspace_bytes(int32_t G, int32_t D, int64_t longest);
 hipError_t launch_cache_attend(const AttendArgs &a, bool bf16, int64_t longest, void *workspace, hipStream_t stream);
+size_t attend4_workspace_bytes(int32_t G, int32_t D, int64_t longest);
+hipError_t launch_cache4_attend(const Attend4Args &a, bool bf16, int64_t longest, void *workspace, hipStream_t stream);
 hipError_t launch_prompt_attend(const AttendArgs &a, bool bf16, int64_t longest, hipStream_t stream);
 
 }  // namespace pcg

@@ -27,6 +27,13 @@ __device__ __forceinline__ const void *elem_ptr(const void *base, int64_t elems,
   return reinterpret_cast<const char *>(base) + elems * (bf16 ? 2 : 4);
 }
 
+// n / d and n % d for n < 2^32, magic = floor(2^32 / d), 2^32 - 1 for d = 1.
+__device__ __forceinline__ void split_by(uint32_t n, uint32_t d, uint32_t magic, uint32_t &q, uint32_t &r) {
+  q = __umulhi(n, magic);
+  r = n - q * d;
+  if (r >= d) { ++q; r -= d; }
+}
+
 // Where the rows of a call live: set 0 = target rows (b, i), i < npos0; set 1 = draft rows
 // (b, i), i < npos1.  Row ids are [0, B*npos0) for set 0 followed by [B*npos0, ...) for set 1.
 // pcg_group_probs uses set 0 alone with npos0 = 1 and bs0 = row stride.
