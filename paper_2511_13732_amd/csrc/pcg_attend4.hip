@@ -7,8 +7,12 @@
 // bfloat16 numbers each, which hold all of their 24 bits: three products of the fast kind, exact in every term, where one of float32
 // takes sixteen times as long.
 //
-// Every wave has 32 rows and a stream of keys of its own, 32 at a time, which it brings into its own part of LDS several steps ahead: nothing is
-// shared in the loop, and no wave waits for another one in it.  Rows, units, runs and parts are those of pcg_attend.hip.
+// Every wave has up to 48 rows, in blocks of 16 that share decoded keys and values, and a stream of keys of its own, which it brings into its own
+// part of LDS ahead of their use: nothing is shared in the loop, and no wave waits for another one in it.  Rows, units, runs and parts are those
+// of pcg_attend.hip.
+#include <algorithm>
+#include <type_traits>
+
 #include "pcg_attend_device.h"
 
 namespace pcg {
@@ -19,9 +23,14 @@ namespace {
 __device__ __forceinline__ void bring_word(const char *from, const unsigned char *to) {
   asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, off" :: "v"(from), "{m0}"(lds_address(to)) : "memory");
 }
-// 16 bytes a lane from base + offset.
-__device__ __forceinline__ void bring_from(const char *base, uint32_t offset, const unsigned char *to) {
-  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(base), "{m0}"(lds_address(to)) : "memory");
+// Four of 16 bytes a lane to 4 KB in a row, load i from base[i] + offset[i] - kBias + 1024 i: what an instruction's own offset adds to the
+// place in LDS it adds to the address as well.
+constexpr uint32_t kBias = 3 * 1024;
+__device__ __forceinline__ void bring_four(const char *const (&base)[4], const uint32_t (&offset)[4], const unsigned char *to) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %5 offset:0x400"
+               "\n\tglobal_load_lds_dwordx4 %2, %6 offset:0x800\n\tglobal_load_lds_dwordx4 %3, %7 offset:0xc00"
+               :: "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base[0]), "s"(base[1]), "s"(base[2]), "s"(base[3]),
+               "{m0}"(lds_address(to)) : "memory");
 }
 
 template <int DP>
@@ -29,119 +38,138 @@ struct Codes {
   static constexpr int RB = DP / 2;                 // bytes of a key
   static constexpr int CH = RB / 16;
   static constexpr int RPI = kWave / CH;            // keys that one load of a wave brings
-  static constexpr int NI = 32 / RPI;               // loads of 32 keys
-  static constexpr int kBytes = 32 * RB;
+  static constexpr int KEYS = 64;                   // of a stage
+  static constexpr int NI = KEYS / RPI;             // loads of their codes
+  static constexpr int NG = KEYS / 16;              // groups of 16 keys
+  static constexpr int kBytes = KEYS * RB;
   static constexpr int kStage = 2 * kBytes + 256;   // codes of keys, of values, scales
   static constexpr int kOps = 2 * NI + 1;           // loads of a stage
-  static constexpr int kStages = 4;                 // one in use, three on their way
-  static constexpr int kWaveLds = kStages * kStage + 256;     // and the scales in use, as float32
-  static constexpr int NQ = DP / 16, NO = DP / 32;
+  static constexpr int kRest = 8 * KEYS + 256;      // the scales in use as float32, pages of stages to come
+  static constexpr int NQ = DP / 32, NM = DP / 16;  // steps of the scores, blocks of 16 columns
 };
 
 // Which 16-byte chunk of key `row` lies at chunk position `pos` of its row in LDS, and the other way round: the keys that one read touches
-// (0-3, 16-19, 4-7, 20-23 and so on as scores, 0-15 and 16-31 as values) have to differ modulo 256 bytes.
+// (four in a row of each 16 as scores, 16 in a row as values) should differ modulo 256 bytes.
 template <int RB>
 __device__ __forceinline__ int code_swap(int row, int pos) {
-  if constexpr (RB == 64) return pos ^ ((row >> 2) & 3) ^ ((row >> 4) << 1);
+  if constexpr (RB == 64) return pos ^ (((row >> 2) ^ (row >> 4)) & 3);
   else return pos ^ (((row >> 3) ^ (row >> 4)) & 1);
 }
 
-// Brings 32 keys, values and scales of a unit into LDS.  PAGES 1: pages of a multiple of 16 slots, so that 16 keys in a row share one, which the
-// scalar unit looks up; 2: pages of any size, looked up by each lane.  Chunks behind D are the row's first ones: queries are zero
-// there, and the columns that values make there are not stored.
+__device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
+  return (int64_t) ((uint64_t) (uint32_t) __shfl((int) (x >> 32), lane) << 32 | (uint32_t) __shfl((int) x, lane));
+}
+
+// Brings the keys, values and scales of a wave's stages into LDS, stages `step` keys from each other.  Where they lie is worked out for many
+// stages at once: for 64 groups of 16 keys, one a lane, where such groups share a page (PAGES 1: pages of a multiple of 16 slots); for a stage's
+// keys, one a lane, where they do not (PAGES 2).  The pages for the next time are brought into LDS too, like codes.  Chunks behind D are the
+// row's first ones: queries are zero there, and the columns that values make there are not stored.
 template <int DP, int PAGES>
 struct Loader4 {
   using C = Codes<DP>;
+  static constexpr int kEach = PAGES == 1 ? kWave / C::NG : 1;      // stages that are worked out at once
   const Attend4Args &a;
   const Unit &u;
   const int lane;
+  const int32_t begin, step;
+  unsigned char *const ids;
   const int32_t *table;
   const char *kb, *vb, *sb;
-  uint32_t off[C::NI];        // of this lane from the first key of 16
+  uint32_t off[C::NI];        // of this lane from the first key of a group, see bring_four
+  int64_t codes, scales;      // where this lane's group or key lies
+  uint64_t there;             // lanes whose group or key there is
+  int64_t next;               // scales of this lane's key of the next stage
 
   __device__ __forceinline__ int row_of(int i) const { return i * C::RPI + lane / C::CH; }
   __device__ __forceinline__ int chunk(int row) const {
     const int ch = code_swap<C::RB>(row, lane % C::CH);
     return ch * 32 < a.D ? ch * 16 : 0;
   }
-  __device__ __forceinline__ Loader4(const Attend4Args &a_, const Unit &u_, int lane_)
-      : a(a_), u(u_), lane(lane_), table(a_.table + (int64_t) u_.b * a_.table_stride) {
+  __device__ __forceinline__ Loader4(const Attend4Args &a_, const Unit &u_, int lane_, int32_t begin_, int32_t step_, unsigned char *ids_)
+      : a(a_), u(u_), lane(lane_), begin(begin_), step(step_), ids(ids_), table(a_.table + (int64_t) u_.b * a_.table_stride) {
     kb = reinterpret_cast<const char *>(a.k) + (int64_t) u.head * a.k_head;
     vb = reinterpret_cast<const char *>(a.v) + (int64_t) u.head * a.k_head;
     sb = reinterpret_cast<const char *>(a.scales + (int64_t) u.head * a.s_head);
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i) off[i] = (uint32_t) (row_of(i) & 15) * (uint32_t) a.k_tok + (uint32_t) chunk(row_of(i));
+    for (int i = 0; i < C::NI; ++i)
+      off[i] = (PAGES == 1 ? (uint32_t) (row_of(i) & 15) * (uint32_t) a.k_tok : 0) + (uint32_t) chunk(row_of(i)) + (kBias - i * 1024);
+    place(0, table[block_of(key_of(0, lane))], lane);
   }
 
-  // Pages of the keys from k0 on: of 16 keys (PAGES 1); of each load's key of this lane, and of the key whose scales it brings.
-  static constexpr int NP = PAGES == 1 ? 2 : C::NI + 1;
-  struct Pages {
-    int32_t page[NP];
-  };
-  __device__ __forceinline__ int32_t key_of(int32_t k0, int i) const {
-    return k0 + (PAGES == 1 ? 16 * i : i < C::NI ? row_of(i) : lane & 31);
+  // The key whose place lane `lane` works out with stages n and on.
+  __device__ __forceinline__ int32_t key_of(int32_t n, int lane) const {
+    // far behind the last key it may wrap, and is then past the table
+    if constexpr (PAGES == 1) return (int32_t) ((uint32_t) begin + (uint32_t) (n + lane / C::NG) * (uint32_t) step + lane % C::NG * 16);
+    else return (int32_t) ((uint32_t) begin + (uint32_t) n * (uint32_t) step + lane % C::KEYS);
   }
-  __device__ __forceinline__ Pages look_up(int32_t k0) const {
-    Pages p;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      uint32_t block, slot;
-      split_by((uint32_t) key_of(k0, i), (uint32_t) a.page_size, a.magic_page, block, slot);
-      p.page[i] = fixed_at(table, min(block, (uint32_t) a.max_blocks - 1));
-    }
-    return p;
+  __device__ __forceinline__ uint32_t block_of(int32_t key) const {
+    uint32_t block, slot;
+    split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
+    return min(block, (uint32_t) a.max_blocks - 1);
+  }
+  __device__ __forceinline__ void place(int32_t n, int32_t page, int lane) {
+    const int32_t key = key_of(n, lane);
+    uint32_t block, slot;
+    split_by((uint32_t) key, (uint32_t) a.page_size, a.magic_page, block, slot);
+    there = __builtin_amdgcn_ballot_w64(key < u.k_hi && block < (uint32_t) a.max_blocks && (uint32_t) page < (uint32_t) a.num_pages);
+    codes = (int64_t) page * a.k_page + (int64_t) slot * a.k_tok;
+    scales = ((int64_t) page * a.s_page + (int64_t) slot * a.s_tok) * 4;
+    if constexpr (PAGES == 1) find_scales(0, lane);
+    else next = scales;
+  }
+  __device__ __forceinline__ void ask(int32_t n, int lane) const {
+    bring_word(reinterpret_cast<const char *>(table + block_of(key_of(n, lane))), ids);
   }
 
-  __device__ __forceinline__ void load(int32_t k0, const Pages &p, unsigned char *to) const {
-    int64_t codes[NP], scales[NP];
-    bool valid[NP], whole = PAGES == 1 && k0 + 32 <= u.k_hi;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      uint32_t block, slot;
-      split_by((uint32_t) key_of(k0, i), (uint32_t) a.page_size, a.magic_page, block, slot);
-      valid[i] = key_of(k0, i) < u.k_hi && block < (uint32_t) a.max_blocks && (uint32_t) p.page[i] < (uint32_t) a.num_pages;
-      whole = whole && valid[i];
-      codes[i] = (int64_t) p.page[i] * a.k_page + (int64_t) slot * a.k_tok;
-      scales[i] = ((int64_t) p.page[i] * a.s_page + (int64_t) slot * a.s_tok) * 4;
+  // Those of the key lane of the stage whose groups begin with g0.
+  __device__ __forceinline__ void find_scales(int g0, int lane) {
+    next = lane_value(scales, g0 + lane / 16) + (uint32_t) (lane & 15) * (uint32_t) a.s_tok * 4;
+  }
+
+  // Codes and scales of the keys of stage n (stages come in order), or afterwards the codes of its values.
+  template <bool VALUES>
+  __device__ __forceinline__ void load(int32_t n, unsigned char *to) {
+    int lane = this->lane;
+    asm("" : "+v"(lane));               // what follows from it is formed here, not kept in registers
+    if (!VALUES && n > 0 && n % kEach == 0) {
+      if constexpr (PAGES == 2) wait_vm<C::kOps>();          // asked for with the stage before; elsewhere many waits ago
+      place(n, reinterpret_cast<const int32_t *>(ids)[lane], lane);
+      wait_lds();
+      ask(n + kEach, lane);
     }
-    unsigned char *const values = to + C::kBytes, *const both = to + 2 * C::kBytes;
+    const char *const base = (VALUES ? vb : kb) - kBias;
+    unsigned char *const codes_to = VALUES ? to + C::kBytes : to, *const scales_to = to + 2 * C::kBytes;
     const char *const zeros = reinterpret_cast<const char *>(&kZeros);
-    if constexpr (PAGES == 1) {
-      const bool second = lane & 16;
-      const char *at_scales = sb + (second ? scales[1] : scales[0]) + (int64_t) (lane & 15) * a.s_tok * 4;
-      if (whole) {
+    const int32_t k0 = begin + n * step;
+    const int g0 = PAGES == 1 ? n % kEach * C::NG : 0;
+    // of the group of key `row`, or of the key
+    auto lane_of = [&](int row) { return PAGES == 1 ? g0 + row / 16 : row; };
+    auto has = [&](int row) { return (there >> lane_of(row) & 1) && k0 + row < u.k_hi; };
+    if (PAGES == 1 && k0 + C::KEYS <= u.k_hi && (~there >> g0 & ((1 << C::NG) - 1)) == 0) {
+      if constexpr (C::NI == 4) {
+        const char *from[4];
 #pragma unroll
-        for (int i = 0; i < C::NI; ++i) {
-          if constexpr (C::NI == 2) {
-            bring_from(kb + codes[i], off[i], to + i * 1024);
-            bring_from(vb + codes[i], off[i], values + i * 1024);
-          } else {
-            const int64_t at = (lane < 32 ? codes[0] : codes[1]) + off[0];
-            bring(kb + at, to);
-            bring(vb + at, values);
-          }
-        }
-        bring_word(at_scales, both);
+        for (int i = 0; i < 4; ++i)
+          from[i] = base + (int64_t) ((uint64_t) (uint32_t) read_lane((int32_t) (codes >> 32), g0 + i) << 32 | (uint32_t) read_lane((int32_t) codes, g0 + i));
+        bring_four(from, off, codes_to);
       } else {
-        // a unit's last keys, pages outside the cache: zeros where there is no key
 #pragma unroll
-        for (int i = 0; i < C::NI; ++i) {
-          const bool upper = row_of(i) & 16, there = (upper ? valid[1] : valid[0]) && k0 + row_of(i) < u.k_hi;
-          const int64_t at = (upper ? codes[1] : codes[0]) + off[i];
-          bring(there ? kb + at : zeros, to + i * 1024);
-          bring(there ? vb + at : zeros, values + i * 1024);
-        }
-        bring_word((second ? valid[1] : valid[0]) && k0 + (lane & 31) < u.k_hi ? at_scales : zeros, both);
+        for (int i = 0; i < C::NI; ++i) bring(base + lane_value(codes, g0 + 2 * i + lane / 32) + off[i] + i * 1024, codes_to + i * 1024);
       }
+      if constexpr (!VALUES) bring_word(sb + next, scales_to);
     } else {
+      // a unit's last keys, pages outside the cache, pages of any size: zeros where there is no key
 #pragma unroll
       for (int i = 0; i < C::NI; ++i) {
-        const int64_t at = codes[i] + chunk(row_of(i));
-        bring(valid[i] ? kb + at : zeros, to + i * 1024);
-        bring(valid[i] ? vb + at : zeros, values + i * 1024);
+        const int row = i * C::RPI + lane / C::CH;
+        const int64_t at = lane_value(codes, lane_of(row));
+        uint32_t from = off[i];
+        asm("" : "+v"(from));
+        bring(has(row) ? base + at + from + i * 1024 : zeros, codes_to + i * 1024);
       }
-      bring_word(valid[C::NI] ? sb + scales[C::NI] : zeros, both);
+      if constexpr (!VALUES) bring_word(has(lane) ? sb + next : zeros, scales_to);
     }
+    if constexpr (VALUES && PAGES == 1) find_scales(min(g0 + C::NG, kWave - C::NG), lane);
   }
 };
 
@@ -184,175 +212,377 @@ __device__ __forceinline__ void operands(const float (&x)[8], bf16x8 (&p)[NP]) {
   for (int i = 0; i < NP; ++i) p[i] = __builtin_bit_cast(bf16x8, w[i]);
 }
 
-__device__ __forceinline__ floatx16 product(bf16x8 x, bf16x8 y, floatx16 s) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, s, 0, 0, 0);
+__device__ __forceinline__ floatx4 product(bf16x8 x, bf16x8 y, floatx4 s) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, s, 0, 0, 0);
 }
 
-// WK streams of keys, 4 / WK blocks of 32 rows.
-template <int WK>
+// max and sum of the lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float quad_max(float x) {
+  const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return pair_max(fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return pair_sum(__uint_as_float(p[0]) + __uint_as_float(p[1]));
+}
+
+// NB blocks of 16 rows a wave, WK streams of keys, 4 / WK waves on other rows.
+template <typename T, int DP, int NB, int WK>
 struct Work4 {
-  static constexpr int WR = kAttendWaves / WK, R = 32 * WR, TK = 32 * WK;
-  static constexpr int kRuns = 512, kLeast = 1;
+  static constexpr int NP = sizeof(T) == 2 ? 1 : 3; // bfloat16 numbers that make one of T
+  static constexpr int WR = kAttendWaves / WK, R = 16 * NB * WR, TK = Codes<DP>::KEYS * WK;
+  static constexpr int kWaveLds = Codes<DP>::kStage + Codes<DP>::kRest;
+  static constexpr int kQueries = NB * Codes<DP>::NQ * NP * 1024;                 // of a wave
+  // passes of the streams' joining, what its outputs take, and with the references and sums
+  static constexpr int kPasses = NB * DP > 192 ? 2 : 1, kRows = WK > 1 ? kAttendWaves * NB * DP / 16 / kPasses * 1024 : 0;
+  static constexpr int kJoining = WK > 1 ? kRows + kAttendWaves * NB * 16 * 8 : 0;
+  static constexpr int kLds = std::max(kAttendWaves * kWaveLds + WR * kQueries, kJoining);
+  // workgroups a CU: as many as find registers, and LDS
+  static constexpr int kGroups = std::min(NB == 1 ? (DP == 64 ? 5 : 4) : NB == 2 && DP == 64 ? 3 : 2, 160 * 1024 / kLds);
+  static constexpr int kRuns = kGroups * kCUs, kLeast = 1, kCost = 3;
 };
 
-template <typename T, int DP, int WK, int PAGES>
+template <typename T, int DP, int NB, int WK, int PAGES>
 __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
-                                            Part<DP, Work4<WK>::R> *part) {
+                                            Part<DP, Work4<T, DP, NB, WK>::R> *part) {
   using C = Codes<DP>;
-  using W = Work4<WK>;
-  constexpr int NP = sizeof(T) == 2 ? 1 : 3;
+  using W = Work4<T, DP, NB, WK>;
+  constexpr int NP = W::NP;
   int tid = threadIdx.x;
   asm("" : "+v"(tid));                  // what follows from it is formed here, not kept in registers from piece to piece
   const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, half = lane >> 5;
-  const int block = wave % W::WR * 32, stream = wave / W::WR;
-  const Loader4<DP, PAGES> loader(a, u, lane);
-  unsigned char *const mine = lds + wave * C::kWaveLds;
-  float *const scale = reinterpret_cast<float *>(mine + C::kStages * C::kStage);
-  // rows of this wave, the positions of its first and last, and the keys that they see
-  const Row w = row_at(a, u, u.r0 + block + l32);
-  const int32_t last = min(u.r0 + block + 32, u.rows) - 1;
+  const int l16 = lane & 15, quarter = lane >> 4;
+  const int block = wave % W::WR * 16 * NB, stream = wave / W::WR;
+  unsigned char *const mine = lds + wave * W::kWaveLds;
+  float *const scale = reinterpret_cast<float *>(mine + C::kStage);
+  unsigned char *const queries = lds + kAttendWaves * W::kWaveLds + wave % W::WR * W::kQueries + lane * 16;
+  // the positions of this wave's first and last row, and the keys that its rows see
+  const int32_t last = min(u.r0 + block + 16 * NB, u.rows) - 1;
   const int32_t pos_first = u.ctx + (u.r0 + block) / a.G, pos_last = last >= u.r0 + block ? u.ctx + last / a.G : -1;
-  const int32_t lo = a.window > 0 ? w.pos - a.window : -1, lo_last = a.window > 0 ? pos_last - a.window : -1;
-  const int32_t begin = u.k_lo + tile * W::TK + stream * 32;
+  const int32_t lo_last = a.window > 0 ? pos_last - a.window : -1;
+  const int32_t begin = u.k_lo + tile * W::TK + stream * C::KEYS;
   const int32_t end = min(min(u.k_hi, u.k_lo + (tile + tiles) * W::TK), pos_last + 1);
   const int32_t stages = end > begin ? (end - begin + W::TK - 1) / W::TK : 0;
 
-  bare_barrier();                       // nobody uses the piece before any more
-  auto pages = loader.look_up(begin);   // of the stage that is brought next
-  auto load = [&](int32_t n) {
-    loader.load(begin + n * W::TK, pages, mine + n % C::kStages * C::kStage);
-    pages = loader.look_up(begin + (n + 1) * W::TK);
-  };
+  // The rows' queries, asked for ahead of everything else: step i of the scores takes elements quarter * DP / 4 + 8 i and on of each quarter's
+  // lanes, so that the codes of a key that lie in a row make all steps.
+  int32_t pos[NB];
+  u32x4 q[NB][C::NQ][sizeof(T) / 2];
 #pragma unroll
-  for (int n = 0; n < C::kStages - 1; ++n)
-    if (n < stages) load(n);
-
-  // Step i of the scores takes elements half * DP / 2 + 8 i and on of each half's lanes: 16 bytes of codes in a row make four steps.
-  bf16x8 qf[C::NQ][NP];
-  {
-    const T *q = reinterpret_cast<const T *>(a.q) + w.token * a.q_tok + w.head * a.q_head;
+  for (int b = 0; b < NB; ++b) {
+    const Row w = row_at(a, u, u.r0 + block + 16 * b + l16);
+    pos[b] = w.pos;
+    if (stream > 0) continue;
+    const T *from = reinterpret_cast<const T *>(a.q) + w.token * a.q_tok + w.head * a.q_head;
 #pragma unroll
     for (int i = 0; i < C::NQ; ++i) {
-      const int d = half * (DP / 2) + 8 * i;
-      const bool there = w.there && d < a.D;
-      if constexpr (NP == 1) {
-        qf[i][0] = __builtin_bit_cast(bf16x8, *(there ? reinterpret_cast<const u32x4 *>(q + d) : &kZeros));
-      } else {
-        const floatx4 x = __builtin_bit_cast(floatx4, *(there ? reinterpret_cast<const u32x4 *>(q + d) : &kZeros));
-        const floatx4 y = __builtin_bit_cast(floatx4, *(there ? reinterpret_cast<const u32x4 *>(q + d + 4) : &kZeros));
-        const float eight[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-        operands<NP, true>(eight, qf[i]);
-      }
+      const int d = quarter * (DP / 4) + 8 * i;
+#pragma unroll
+      for (int h = 0; h < (int) sizeof(T) / 2; ++h) q[b][i][h] = *(w.there && d < a.D ? reinterpret_cast<const u32x4 *>(from + d + 4 * h) : &kZeros);
     }
   }
-
-  // The register r of a lane's scores is key 16 half + r: the operand of the lane's weights and the codes of 16 keys that one transposing
-  // read brings then have the same order.  Lane l reads as key of the scores the one that comes out there.
-  const int key_row = ((l32 >> 2) & 1) * 16 + (l32 >> 3) * 4 + (l32 & 3);
-  const int value_row = half * 16 + (lane & 15);
-  floatx16 o[C::NO];
+  Loader4<DP, PAGES> loader(a, u, lane, begin, W::TK, mine + W::kWaveLds - 256);
+  bare_barrier();                       // nobody uses the piece before any more
+  loader.ask(loader.kEach, lane);
+  if (stages > 0) {
+    loader.template load<false>(0, mine);
+    loader.template load<true>(0, mine);
+  }
+  if (stream == 0) {
 #pragma unroll
-  for (int n = 0; n < C::NO; ++n) o[n] = floatx16{};
-  float ref = -INFINITY, sum = 0.f;
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < C::NQ; ++i) {
+        bf16x8 x[NP];
+        if constexpr (NP == 1) {
+          x[0] = __builtin_bit_cast(bf16x8, q[b][i][0]);
+        } else {
+          const floatx4 y = __builtin_bit_cast(floatx4, q[b][i][0]), z = __builtin_bit_cast(floatx4, q[b][i][1]);
+          const float eight[8] = {y[0], y[1], y[2], y[3], z[0], z[1], z[2], z[3]};
+          operands<NP, true>(eight, x);
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) *reinterpret_cast<bf16x8 *>(queries + ((b * C::NQ + i) * NP + p) * 1024) = x[p];
+      }
+  }
+  bare_barrier();
+
+  // Scores of 64 keys are four products of 16; register i of product t is, in a lane of quarter g, key 16 g + 4 t + i: the operand of the lane's
+  // weights and the codes of 16 keys that one transposing read brings then have the same order.
+  const int key_row = (l16 >> 2) * 16 + (l16 & 3), value_row = lane;
+  floatx4 o[NB][C::NM];
+  float ref[NB], sum[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+#pragma unroll
+    for (int m = 0; m < C::NM; ++m) o[b][m] = floatx4{};
+    ref[b] = -INFINITY;
+    sum[b] = 0.f;
+  }
 #pragma nounroll
   for (int32_t n = 0; n < stages; ++n) {
-    wait_lds();                         // the stage before is read
-    if (n + C::kStages - 1 < stages) load(n + C::kStages - 1);
-    const int32_t ahead = stages - 1 - n;
-    if (ahead >= 3) wait_vm<3 * C::kOps>();
-    else if (ahead == 2) wait_vm<2 * C::kOps>();
-    else if (ahead == 1) wait_vm<C::kOps>();
-    else wait_vm<0>();
-    const unsigned char *const codes = mine + n % C::kStages * C::kStage, *const values = codes + C::kBytes;
+    const bool more = n + 1 < stages;
+    wait_vm<C::NI>();                   // keys and scales are in, values may be on their way
+    const unsigned char *const kl = mine, *const vl = kl + C::kBytes;
+    // All codes of keys into registers, so that those of another stage may come into their place.
+    uint32_t kc[4][C::NQ];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int row = key_row + 4 * t;
+      if constexpr (C::NQ == 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(kl + row * C::RB + (code_swap<C::RB>(row, quarter) << 4));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kc[t][i] = x[i];
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(kl + row * C::RB + (code_swap<C::RB>(row, quarter >> 1) << 4) + (quarter & 1) * 8);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) kc[t][i] = x[i];
+      }
+    }
+    uint32_t both = reinterpret_cast<const uint32_t *>(kl + 2 * C::kBytes)[lane];
+    bf16x8 qf[2][NB][NP];               // queries of a step and of the next
+    auto ask = [&](int i) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int p = 0; p < NP; ++p) qf[i % 2][b][p] = *reinterpret_cast<const bf16x8 *>(queries + ((b * C::NQ + i) * NP + p) * 1024);
+    };
+    wait_lds();
+    ask(0);
+    if (more) loader.template load<false>(n + 1, mine);
     // scales as float32, those of keys with c; what is not finite is NaN, whatever the codes
     {
-      const uint32_t both = reinterpret_cast<const uint32_t *>(codes + 2 * C::kBytes)[l32];
-      const float s = __uint_as_float(half ? both & 0xffff0000u : both << 16);
-      scale[lane] = fmaf(s, 0.f, s) * (half ? 1.f : a.c);
+      const float x = __uint_as_float(both << 16), y = __uint_as_float(both & 0xffff0000u);
+      scale[lane] = fmaf(x, 0.f, x) * a.c;
+      scale[C::KEYS + lane] = fmaf(y, 0.f, y);
     }
-    u32x4 kc[C::NQ / 4];
+    floatx4 s[NB][4];
 #pragma unroll
-    for (int j = 0; j < C::NQ / 4; ++j)
-      kc[j] = *reinterpret_cast<const u32x4 *>(codes + key_row * C::RB + (code_swap<C::RB>(key_row, half * (C::NQ / 4) + j) << 4));
-    floatx16 s[1] = {floatx16{}};
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[b][t] = floatx4{};
+    floatx4 ks[4], vs[4];
 #pragma unroll
     for (int i = 0; i < C::NQ; ++i) {
-      const bf16x8 kf = decoded(kc[i / 4][i % 4]);
+      pin();
+      if (i + 1 < C::NQ) ask(i + 1);
+      else
 #pragma unroll
-      for (int p = NP - 1; p >= 0; --p) s[0] = product(kf, qf[i][p], s[0]);
+        for (int t = 0; t < 4; ++t) ks[t] = *reinterpret_cast<const floatx4 *>(scale + 16 * quarter + 4 * t);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bf16x8 kf = decoded(kc[t][i]);
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+          for (int b = 0; b < NB; ++b) s[b][t] = product(kf, qf[i % 2][b][p], s[b][t]);
+      }
     }
+    pin();
+    // Scores in log2 units: products with c s_k, rounded, so that those of one size have one weight wherever they stand.
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[0][r] *= scale[16 * half + r];
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b][t] *= ks[t];
     const int32_t k = begin + n * W::TK;
-    const bool edge = k + 31 > pos_first || k <= lo_last;
-    const int32_t from = lo - k - 16 * half, to = w.pos - k - 16 * half;      // registers that the row sees: from < r <= to
-    if (edge) {
+    const bool edge = k + C::KEYS - 1 > pos_first || k <= lo_last;
+    // Numbers in place of those of keys that a row does not see.
+    auto hide = [&](float x) {
+      int l = lane;
+      asm("" : "+v"(l));                // formed here, not kept in registers
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (r > to || r <= from) s[0][r] = -INFINITY;
+      for (int b = 0; b < NB; ++b) {
+        const int32_t to = pos[b] - k - (l >> 4) * 16, first = a.window > 0 ? to - a.window + 1 : 0;      // first <= 4 t + i <= to is seen
+        const uint32_t count = (uint32_t) max(to - first + 1, 0);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          pin();                        // not all comparisons ahead of all moves
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if ((uint32_t) (4 * t + i - first) >= count) s[b][t][i] = x;
+        }
+      }
+    };
+    if (edge) hide(-INFINITY);
+    float mx[NB];
+    bool ahead = false;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      float m[2] = {s[b][0][0], s[b][0][1]};
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = t ? 0 : 2; i < 4; ++i) m[i & 1] = fmaxf(m[i & 1], s[b][t][i]);
+      mx[b] = quad_max(fmaxf(m[0], m[1]));
+      ahead = ahead || mx[b] > ref[b] + kLag;
     }
-    (void) follow<C::NO, 1>(row_max<1>(s, 1.f), ref, sum, o, s, 1.f);
-    to_weights<1>(s, 1.f, minus_ref(ref), sum);
+    // The rows' references follow the maxima where one runs more than kLag ahead, see follow in pcg_attend_device.h.
+    if (__builtin_amdgcn_ballot_w64(ahead) != 0) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[0][r] *= scale[32 + 16 * half + r];
-    if (edge) {                         // a scale that is NaN stays out of rows that do not see its key
+      for (int b = 0; b < NB; ++b) {
+        const float now = fmaxf(ref[b], mx[b]), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[b] - now);
+        ref[b] = now;
+        sum[b] *= f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (r > to || r <= from) s[0][r] = 0.f;
+        for (int m = 0; m < C::NM; ++m) o[b][m] *= f;
+      }
     }
-    bf16x8 pf[2][NP];
+    pin();
+    if (more) wait_vm<C::NI + 1>();     // values are in, the next keys may be on their way
+    else wait_vm<0>();
+    // lane x of 16 reads 16 codes of key x, columns 16 m .., and gets back column x of the 16 keys
+    typedef int intx2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) intx2 lds8;
+    intx2 vc[C::NM];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      float eight[8];
+    for (int m = 0; m < C::NM; ++m)
+      vc[m] = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+          (lds8 *) (vl + value_row * C::RB + (code_swap<C::RB>(value_row, m >> 1) << 4) + (m & 1) * 8));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) eight[e] = s[0][8 * c + e];
-      operands<NP, false>(eight, pf[c]);
+    for (int t = 0; t < 4; ++t) vs[t] = *reinterpret_cast<const floatx4 *>(scale + C::KEYS + 16 * quarter + 4 * t);
+    pin();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const float minus = minus_ref(ref[b]);
+      float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[b][t][i] = __builtin_amdgcn_exp2f(s[b][t][i] + minus);
+          z[i] += s[b][t][i];
+        }
+      sum[b] += (z[0] + z[1]) + (z[2] + z[3]);
+      asm volatile("" : "+v"(sum[b]));  // formed here: weights that wait to be added take registers
     }
 #pragma unroll
-    for (int m = 0; m < C::NO; ++m) {
-      typedef int intx2 __attribute__((ext_vector_type(2)));
-      typedef __attribute__((address_space(3))) intx2 lds8;
-      // lane x of 16 reads 16 codes of key x, columns 16 .. of the block, and gets back column x of the 16 keys
-      const intx2 vc = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
-          (lds8 *) (values + value_row * C::RB + (code_swap<C::RB>(value_row, m) << 4) + ((lane >> 4) & 1) * 8));
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b][t] *= vs[t];
+    if (edge) hide(0.f);                // a scale that is NaN stays out of rows that do not see its key
+    bf16x8 pf[NB][2][NP];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const bf16x8 vf = decoded((uint32_t) vc[c]);
+        const float eight[8] = {s[b][2 * c][0], s[b][2 * c][1], s[b][2 * c][2], s[b][2 * c][3], s[b][2 * c + 1][0], s[b][2 * c + 1][1],
+                                s[b][2 * c + 1][2], s[b][2 * c + 1][3]};
+        operands<NP, false>(eight, pf[b][c]);
 #pragma unroll
-        for (int p = NP - 1; p >= 0; --p) o[m] = product(vf, pf[c][p], o[m]);
+        for (int p = 0; p < NP; ++p) {
+          u32x4 x = __builtin_bit_cast(u32x4, pf[b][c][p]);
+          asm volatile("" : "+v"(x));   // formed here too
+          pf[b][c][p] = __builtin_bit_cast(bf16x8, x);
+        }
+      }
+    wait_lds();
+    if (more) loader.template load<true>(n + 1, mine);
+    // two blocks of columns at a time, so that products that add to the same sums do not follow each other
+#pragma unroll
+    for (int m = 0; m < C::NM; m += 2) {
+      if (16 * m >= a.D) break;
+      pin();
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8 vf = decoded((uint32_t) vc[m + h][c]);
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[b][m + h] = product(vf, pf[b][c][p], o[b][m + h]);
+        }
+    }
+  }
+
+  // The streams' rows: outputs go to LDS in passes, and every wave joins and stores some columns of all of them.
+  bare_barrier();
+  constexpr int kColumns = C::NM / W::kPasses, kMine = kColumns / WK;       // blocks of 16 of a pass, and of a wave
+  static_assert(kMine >= 1, "");
+  floatx4 *const room = reinterpret_cast<floatx4 *>(lds) + wave % W::WR * (WK * NB * kColumns * kWave);
+  floatx2 *const sums = reinterpret_cast<floatx2 *>(lds + W::kRows) + wave % W::WR * (WK * NB * 16);
+  if constexpr (WK > 1) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const float all = quad_sum(sum[b]);
+      if (quarter == 0) sums[(stream * NB + b) * 16 + l16] = floatx2{ref[b], all};
+    }
+  }
+#pragma unroll
+  for (int pass = 0; pass < W::kPasses; ++pass) {
+    if constexpr (WK > 1) {
+      if (pass) bare_barrier();
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int m = 0; m < kColumns; ++m) room[((stream * NB + b) * kColumns + m) * kWave + lane] = o[b][pass * kColumns + m];
+      bare_barrier();
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      int32_t r = block + 16 * b + l16;
+      asm("" : "+v"(r));                // formed here, not kept in registers since the beginning
+      const Row w = row_at(a, u, u.r0 + r);
+      float now = ref[b], all = 0.f, f[WK];
+      if constexpr (WK > 1) {
+        floatx2 of[WK];
+#pragma unroll
+        for (int i = 0; i < WK; ++i) of[i] = sums[(i * NB + b) * 16 + l16];
+        now = of[0][0];
+#pragma unroll
+        for (int i = 1; i < WK; ++i) now = fmaxf(now, of[i][0]);
+#pragma unroll
+        for (int i = 0; i < WK; ++i) {
+          f[i] = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of[i][0] - now);
+          all += f[i] * of[i][1];
+        }
+      } else {
+        all = quad_sum(sum[b]);
+      }
+      if (part && quarter == 0 && stream == 0 && pass == 0 && w.there) {
+        part->ref[r] = now;
+        part->sum[r] = all;
+      }
+      const float inv = 1.f / all;
+      T *const out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
+#pragma unroll
+      for (int m = 0; m < kMine; ++m) {
+        const int at = stream * kMine + m, d = 16 * (pass * kColumns + at) + 4 * quarter;
+        floatx4 x;
+        if constexpr (WK > 1) {
+          x = floatx4{};
+#pragma unroll
+          for (int i = 0; i < WK; ++i) x += room[((i * NB + b) * kColumns + at) * kWave + lane] * f[i];
+        } else {
+          x = o[b][pass * kColumns + m];
+        }
+        if (!w.there) continue;
+        if (part) {
+          *reinterpret_cast<floatx4 *>(&part->o[r][d]) = x;
+          continue;
+        }
+        if (d >= a.D) continue;
+        // a row without a score above -infinity is zeros, also where a value was NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = all == 0.f ? 0.f : x[i] * inv;
+        if constexpr (sizeof(T) == 2) {
+          *reinterpret_cast<u32x2 *>(out + d) = u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{x[0], x[1]}), bf16x2)),
+                                                      __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{x[2], x[3]}), bf16x2))};
+        } else {
+          *reinterpret_cast<floatx4 *>(out + d) = x;
+        }
       }
     }
   }
-
-  // the streams' rows: the upper half of them to the lower one, and again
-  float *room = reinterpret_cast<float *>(lds);
-  bare_barrier();
-#pragma unroll
-  for (int n = WK / 2; n > 0; n /= 2) {
-    float *at = room + (stream % n * W::WR + wave % W::WR) * kRowsFloats<DP>;
-    if (stream >= n && stream < 2 * n) give_rows<DP>(at, lane, o, ref, sum);
-    bare_barrier();
-    if (stream < n) take_rows<DP>(at, lane, o, ref, sum);
-    if (n > 1) bare_barrier();
-  }
-  if (stream > 0) return;
-  sum = pair_sum(sum);
-  int32_t r = block + l32;
-  asm("" : "+v"(r));                    // formed here, not kept in registers since the beginning
-  const Row out = row_at(a, u, u.r0 + r);
-  if (part) store_part<DP, W::R>(part, r, half, out.there, o, ref, sum);
-  else store_row<T, DP>(a, out, half, o, sum);
 }
 
-template <typename T, int DP, int WK, int PAGES>
-__global__ __launch_bounds__(kAttendThreads, 2) void attend4_kernel(Attend4Args a, Join *join, Part<DP, Work4<WK>::R> *parts) {
-  using W = Work4<WK>;
-  constexpr int kRoom = WK > 1 ? WK / 2 * W::WR * kRowsFloats<DP> * 4 : 0, kLds = kAttendWaves * Codes<DP>::kWaveLds;
-  static_assert(kRoom <= kLds, "rows on their way between waves");
-  __shared__ __align__(16) unsigned char lds[kLds];
-  work_on_run<DP, W::R, W::TK, W::kLeast, kAttendWaves>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
-    codes_piece<T, DP, WK, PAGES>(a, u, tile, tiles, lds, part);
+template <typename T, int DP, int NB, int WK, int PAGES>
+__global__ __launch_bounds__(kAttendThreads, (Work4<T, DP, NB, WK>::kGroups)) void attend4_kernel(Attend4Args a, Join *join,
+                                                                                              Part<DP, Work4<T, DP, NB, WK>::R> *parts) {
+  using W = Work4<T, DP, NB, WK>;
+  __shared__ __align__(16) unsigned char lds[W::kLds];
+  work_on_run<DP, W::R, W::TK, W::kLeast, kAttendWaves, W::kCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
+    codes_piece<T, DP, NB, WK, PAGES>(a, u, tile, tiles, lds, part);
   });
 }
 
@@ -361,38 +591,61 @@ __global__ __launch_bounds__(kJoinThreads) void attend4_join_kernel(AttendArgs a
   join_parts<T, DP, R>(a, join, parts);
 }
 
-template <typename T, int DP, int WK>
+template <typename T, int DP, int NB, int WK>
 hipError_t go(const Attend4Args &a, void *workspace, hipStream_t stream) {
-  using W = Work4<WK>;
+  using W = Work4<T, DP, NB, WK>;
   Join *join = reinterpret_cast<Join *>(workspace);
   Part<DP, W::R> *parts = reinterpret_cast<Part<DP, W::R> *>(reinterpret_cast<char *>(workspace) + join_bytes(W::kRuns));
-  // 16 keys share a page, and lie within 32 bits of each other
-  if (a.page_size % 16 == 0 && a.k_tok < (int64_t) 1 << 27) attend4_kernel<T, DP, WK, 1><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
-  else attend4_kernel<T, DP, WK, 2><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
+  // 16 keys share a page, and their codes and scales lie within 32 bits of each other
+  if (a.page_size % 16 == 0 && a.k_tok < (int64_t) 1 << 27 && a.s_tok < (int64_t) 1 << 25) attend4_kernel<T, DP, NB, WK, 1><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
+  else attend4_kernel<T, DP, NB, WK, 2><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  attend4_join_kernel<T, DP, W::R><<<dim3(W::kRuns, W::R == 128 ? 8 : W::R / 4), kJoinThreads, 0, stream>>>(a, join, parts);
+  attend4_join_kernel<T, DP, W::R><<<dim3(W::kRuns, W::R >= 128 ? 8 : W::R / 4), kJoinThreads, 0, stream>>>(a, join, parts);
   return hipGetLastError();
+}
+
+// Calls f(T, NB, WK) as they fit `rows`: rows of a shared head of the longest request.
+template <int DP, bool BF16, typename F>
+auto by_rows(int64_t rows, F f) {
+  using std::integral_constant;
+  auto at = [&](auto nb, auto wk) { return f(nb, wk); };
+#define PCG_ROWS(NB, WK) at(integral_constant<int, NB>(), integral_constant<int, WK>())
+  if (rows <= 16) return PCG_ROWS(1, 4);
+  if constexpr (BF16) {
+    if (rows <= 32) return PCG_ROWS(2, 4);
+    if (rows <= 48) return PCG_ROWS(3, 4);
+    if (rows <= 64) return PCG_ROWS(2, 2);
+    return PCG_ROWS(2, 1);
+  } else {
+    if (rows <= 32) return PCG_ROWS(1, 2);
+    return PCG_ROWS(1, 1);
+  }
+#undef PCG_ROWS
+}
+
+template <int DP, bool BF16>
+size_t bytes(int64_t rows) {
+  return by_rows<DP, BF16>(rows, [](auto nb, auto wk) {
+    using T = std::conditional_t<BF16, uint16_t, float>;
+    using W = Work4<T, DP, decltype(nb)::value, decltype(wk)::value>;
+    return parts_bytes<T, DP, W::R>(W::kRuns);
+  });
 }
 
 template <typename T, int DP>
 hipError_t go_rows(const Attend4Args &a, int64_t longest, void *workspace, hipStream_t stream) {
-  const int64_t rows = longest * a.G;
-  if (rows <= 32) return go<T, DP, 4>(a, workspace, stream);
-  if (rows <= 64) return go<T, DP, 2>(a, workspace, stream);
-  return go<T, DP, 1>(a, workspace, stream);
-}
-
-template <int DP>
-size_t bytes(int64_t rows) {
-  if (rows <= 32) return parts_bytes<float, DP, 32>(Work4<4>::kRuns);
-  if (rows <= 64) return parts_bytes<float, DP, 64>(Work4<2>::kRuns);
-  return parts_bytes<float, DP, 128>(Work4<1>::kRuns);
+  return by_rows<DP, sizeof(T) == 2>(longest * a.G, [&](auto nb, auto wk) {
+    return go<T, DP, decltype(nb)::value, decltype(wk)::value>(a, workspace, stream);
+  });
 }
 
 }  // namespace
 
-size_t attend4_workspace_bytes(int32_t G, int32_t D, int64_t longest) { return D <= 64 ? bytes<64>(longest * G) : bytes<128>(longest * G); }
+size_t attend4_workspace_bytes(int32_t G, int32_t D, int64_t longest) {
+  const int64_t rows = longest * G;
+  return D <= 64 ? std::max(bytes<64, true>(rows), bytes<64, false>(rows)) : std::max(bytes<128, true>(rows), bytes<128, false>(rows));
+}
 
 hipError_t launch_cache4_attend(const Attend4Args &a, bool bf16, int64_t longest, void *workspace, hipStream_t stream) {
   if (bf16) return a.D <= 64 ? go_rows<uint16_t, 64>(a, longest, workspace, stream) : go_rows<uint16_t, 128>(a, longest, workspace, stream);

@@ -266,7 +266,7 @@ __device__ __forceinline__ int32_t unit_tiles(const AttendArgs &a, Unit &u) {
   return (u.k_hi - u.k_lo + TK - 1) / TK;
 }
 
-// All units (requests, their shared heads, their row blocks, in this order) in a row, kCost for what a unit costs beside its tiles
+// All units (requests, their shared heads, their row blocks, in this order) in a row, COST for what a unit costs beside its tiles
 // and then 1 for each of them, are cut into `runs` runs of a length, one a workgroup; the first `longer` are one longer than `each`.
 struct Run {
   int32_t runs, longer, index;
@@ -288,7 +288,7 @@ struct Run {
 // Every workgroup adds the requests up by itself, each wave its share of them, a request a lane or (with many row blocks) a row block
 // a lane: for 64 requests that takes two microseconds, less than a launch ahead would.  Lengths are whole numbers below 2^53 in
 // double, whose running sums go through DPP.
-template <int R, int TK, int LEAST, int NW>
+template <int R, int TK, int LEAST, int NW, int COST>
 __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsigned char *lds, Unit &u, int64_t &into) {
   double *sums = reinterpret_cast<double *>(lds);
   int32_t *found = reinterpret_cast<int32_t *>(sums + NW);
@@ -303,7 +303,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
       v.ctx = request_ctx(a, v.b);
     }
     v.r0 = 0;
-    one = v.rows > 0 && v.rows <= R ? unit_tiles<R, TK>(a, v) + kCost : 0;
+    one = v.rows > 0 && v.rows <= R ? unit_tiles<R, TK>(a, v) + COST : 0;
     for (uint64_t many = __builtin_amdgcn_ballot_w64(v.rows > R); many; many &= many - 1) {
       const int l = __ffsll((long long) many) - 1;
       Unit x;
@@ -312,7 +312,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
       double all = 0;
       for (int64_t r0 = (int64_t) lane * R; r0 < x.rows; r0 += kWave * R) {
         x.r0 = (int32_t) r0;
-        all += unit_tiles<R, TK>(a, x) + kCost;
+        all += unit_tiles<R, TK>(a, x) + COST;
       }
       all = wave_sum(all);
       if (lane == l) one = all;
@@ -374,7 +374,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
       for (int64_t c0 = 0; c0 < x.rows && x.rows > R; c0 += kWave * R) {
         const int64_t mine_r0 = c0 + (int64_t) lane * R;
         x.r0 = (int32_t) mine_r0;
-        const double t = mine_r0 < x.rows ? unit_tiles<R, TK>(a, x) + kCost : 0, blocks = wave_scan(t);
+        const double t = mine_r0 < x.rows ? unit_tiles<R, TK>(a, x) + COST : 0, blocks = wave_scan(t);
         const uint64_t in = __builtin_amdgcn_ballot_w64(blocks > ahead);
         if (in) {
           const int k = __ffsll((long long) in) - 1;
@@ -425,11 +425,11 @@ __device__ __forceinline__ void next_unit(const AttendArgs &a, Unit &u) {
 
 // Calls work(unit, first tile, tiles, part) for every unit or piece of one in this workgroup's run; part: NULL where the unit is
 // whole.  A workgroup has two places for parts: 1 for the unit that it begins and does not finish, 0 for one that another began.
-template <int DP, int R, int TK, int LEAST, int NW, typename Work>
+template <int DP, int R, int TK, int LEAST, int NW, int COST = kCost, typename Work>
 __device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *lds, Join *join, Part<DP, R> *parts, Work work) {
   Unit u;
   int64_t into = 0;
-  Run run = find_run<R, TK, LEAST, NW>(a, (int32_t) gridDim.x, lds, u, into);
+  Run run = find_run<R, TK, LEAST, NW, COST>(a, (int32_t) gridDim.x, lds, u, into);
   Join j{0, 0, 0, 0, 0};
   // Where a head's keys are read by several row blocks, the end of a unit that another run began comes last: the runs of an XCD then
   // begin with units from their first key on, and those of one head read the same keys at the same time, out of its L2 (us with
@@ -442,14 +442,14 @@ __device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *
     if (run.left > 0) {
       u = scalar(u);
       const int32_t all = scalar(unit_tiles<R, TK>(a, u));
-      const int64_t until = min((int64_t) all + kCost, into + run.left);       // in the unit's length
-      tile = into > kCost ? (int32_t) into - kCost : 0;
-      tiles = until > kCost ? (int32_t) until - kCost - tile : 0;
+      const int64_t until = min((int64_t) all + COST, into + run.left);       // in the unit's length
+      tile = into > COST ? (int32_t) into - COST : 0;
+      tiles = until > COST ? (int32_t) until - COST - tile : 0;
       run.left -= until - into;
       part = tiles == all ? nullptr : parts + 2 * (int64_t) run.index + (tile == 0);
       if (part && tile == 0 && tiles > 0) {
         // this run and those that begin ahead of the unit's end
-        j.parts = run.ahead_of(run.begin(run.index + 1) - run.left + all + kCost - until) - run.index;
+        j.parts = run.ahead_of(run.begin(run.index + 1) - run.left + all + COST - until) - run.index;
         j.head = u.head;
         j.r0 = u.r0;
         j.rows = u.rows;
