@@ -781,12 +781,12 @@ class KvCache(_Handle):
 
 def _rows(t: torch.Tensor, rows: int, heads: int, head_dim: int, dtype, dev, what: str):
     """Checks rows [rows, heads, head_dim] of a dtype and device; (token stride, head stride)."""
-    if t.shape != (rows, heads, head_dim) or t.dtype is not dtype or t.device != dev:
-        raise ValueError(f"{what} must be [{rows}, {heads}, {head_dim}], {dtype}, on {dev}")
-    tok, head, one = t.stride()
-    if one != 1:
+    if t.dtype is dtype and t.shape == (rows, heads, head_dim) and t.device == dev:
+        tok, head, one = t.stride()
+        if one == 1:
+            return tok, head
         raise ValueError(f"the last axis of {what} must be contiguous")
-    return tok, head
+    raise ValueError(f"{what} must be [{rows}, {heads}, {head_dim}], {dtype}, on {dev}")
 
 
 def cache_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
@@ -803,7 +803,7 @@ def cache_attend_workspace_bytes(B: int, rows: int, heads: int, kv_heads: int, h
     return lib().pcg_cache_attend_workspace_bytes(B, rows, heads, kv_heads, head_dim, longest)
 
 
-def _attend(name: str, cache, dtype: tuple, workspace_bytes, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor,
+def _attend(fn, name: str, cache, dtype: tuple, workspace_bytes, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor,
             q_start: torch.Tensor, longest: Optional[int], scale: Optional[float], window: int, out: Optional[torch.Tensor],
             workspace: Optional[torch.Tensor]) -> torch.Tensor:
     """Checks and makes the library's call `name` over a cache; `dtype`: the queries' type, where the cache does not say it."""
@@ -825,7 +825,7 @@ def _attend(name: str, cache, dtype: tuple, workspace_bytes, q: torch.Tensor, bl
         workspace = _workspace(dev, workspace_bytes(B, T, heads, cache.kv_heads, head_dim, longest))
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
-    _call(dev, name, getattr(lib(), name), cache._ref, *dtype, q.data_ptr(), *qs, heads, T, block_table.data_ptr(),
+    _call(dev, name, fn, cache._ref, *dtype, q.data_ptr(), *qs, heads, T, block_table.data_ptr(),
           block_table.stride(0), block_table.shape[1], lens.data_ptr(), q_start.data_ptr(), B, longest,
           head_dim ** -0.5 if scale is None else scale, _int31(window, "window"), out.data_ptr(), *os_, workspace.data_ptr(),
           workspace.numel())
@@ -840,7 +840,7 @@ def cache_attend(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, len
     seeing the keys up to itself, with ``window`` the last that many of them.  ``longest`` bounds the new tokens of a request
     (it decides how the work is cut; without it: the mean).  ``out`` must not overlap what is read.  ``scale`` is 1 / sqrt(head_dim) unless given.  Rows of ``out`` behind
     the last request's stay as they were (zeros where ``out`` is not given)."""
-    return _attend("pcg_cache_attend", cache, (), cache_attend_workspace_bytes, q, block_table, lens, q_start, longest, scale, window,
+    return _attend(lib().pcg_cache_attend, "pcg_cache_attend", cache, (), cache_attend_workspace_bytes, q, block_table, lens, q_start, longest, scale, window,
                    out, workspace)
 
 
@@ -870,32 +870,35 @@ class Rotation(_Handle):
         return cls(torch.cat([angle.cos(), angle.sin()], dim=1).float(), interleaved)
 
 
-def _append(name: str, cache, dtype: tuple, k, v, slots, rotation: Optional[Rotation], positions, q, q_out):
+def _append(fn, name: str, cache, dtype: tuple, k, v, slots, rotation: Optional[Rotation], positions, q, q_out):
     T, dev, of = slots.numel(), cache.device, k.dtype if dtype else cache.dtype
-    ks = _rows(k, T, cache.kv_heads, cache.head_dim, of, dev, "k")
-    vs = _rows(v, T, cache.kv_heads, cache.head_dim, of, dev, "v")
+    G, D = cache.kv_heads, cache.head_dim
+    ks, vs = _rows(k, T, G, D, of, dev, "k"), _rows(v, T, G, D, of, dev, "v")
     _int32(slots, T, dev, "slots")
-    if rotation is not None:
-        if rotation.device != dev:
-            raise ValueError(f"the rotation's table must be on {dev}")
-        if positions is None:
-            raise ValueError("a rotation needs positions")
-        _int32(positions, T, dev, "positions")
-    elif q is not None or positions is not None:
-        raise ValueError("queries and positions without a rotation")
-    heads, qs, os_ = 0, (0, 0), (0, 0)
-    if q is not None:
-        heads = q.shape[1]
-        qs = _rows(q, T, heads, cache.head_dim, of, dev, "q")
-        if q_out is None:
-            q_out = torch.zeros((T, heads, cache.head_dim), dtype=of, device=dev)
-        os_ = _rows(q_out, T, heads, cache.head_dim, of, dev, "q_out")
+    if rotation is None:
+        if q is not None or q_out is not None or positions is not None:
+            raise ValueError("queries or positions without a rotation")
+        _call(dev, name, fn, cache._ref, *dtype, None, None, None, 0, 0, 0, None, 0, 0, k.data_ptr(), *ks, v.data_ptr(), *vs, T,
+              slots.data_ptr())
+        return None
+    if rotation.device != dev or positions is None:
+        raise ValueError(f"a rotation needs positions, and its table must be on {dev}")
+    _int32(positions, T, dev, "positions")
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out without q")
+        _call(dev, name, fn, cache._ref, *dtype, rotation._ref, positions.data_ptr(), None, 0, 0, 0, None, 0, 0, k.data_ptr(), *ks,
+              v.data_ptr(), *vs, T, slots.data_ptr())
+        return None
+    heads = q.shape[1]
+    qs = _rows(q, T, heads, D, of, dev, "q")
+    if q_out is None:
+        q_out = torch.zeros((T, heads, D), dtype=of, device=dev)
+    os_ = qs if q_out is q else _rows(q_out, T, heads, D, of, dev, "q_out")
+    if heads >> 31:
         _sizes31(heads)
-    elif q_out is not None:
-        raise ValueError("q_out without q")
-    _call(dev, name, getattr(lib(), name), cache._ref, *dtype, None if rotation is None else rotation._ref,
-          None if rotation is None else positions.data_ptr(), None if q is None else q.data_ptr(), *qs, heads,
-          None if q is None else q_out.data_ptr(), *os_, k.data_ptr(), *ks, v.data_ptr(), *vs, T, slots.data_ptr())
+    _call(dev, name, fn, cache._ref, *dtype, rotation._ref, positions.data_ptr(), q.data_ptr(), *qs, heads, q_out.data_ptr(), *os_,
+          k.data_ptr(), *ks, v.data_ptr(), *vs, T, slots.data_ptr())
     return q_out
 
 
@@ -906,7 +909,7 @@ def cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     pages_step gives them), and values to their ``slots``; queries ``q`` [T, heads, head_dim], turned, to ``q_out``, which is returned (and
     may be ``q``).  Rows whose slot is negative, or whose position the table does not have, are left out, their queries too (zeros where
     ``q_out`` is not given)."""
-    return _append("pcg_cache_append", cache, (), k, v, slots, rotation, positions, q, q_out)
+    return _append(lib().pcg_cache_append, "pcg_cache_append", cache, (), k, v, slots, rotation, positions, q, q_out)
 
 
 @dataclass
@@ -946,7 +949,7 @@ def cache4_append(cache: KvCache4, k: torch.Tensor, v: torch.Tensor, slots: torc
                   positions: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
                   q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """``cache_append`` into a cache of 4 bits: every key and value of a head gets its scale and codes.  Rows are float32 or bfloat16."""
-    return _append("pcg_cache4_append", cache, (_dtype_code(k),), k, v, slots, rotation, positions, q, q_out)
+    return _append(lib().pcg_cache4_append, "pcg_cache4_append", cache, (_dtype_code(k),), k, v, slots, rotation, positions, q, q_out)
 
 
 def cache4_read(cache: KvCache4, slots: torch.Tensor, *, dtype: torch.dtype = torch.bfloat16, out=None):
@@ -971,7 +974,7 @@ def cache4_attend(cache: KvCache4, q: torch.Tensor, block_table: torch.Tensor, l
                   longest: Optional[int] = None, scale: Optional[float] = None, window: int = 0,
                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``cache_attend`` over a cache of 4 bits; queries and outputs are float32 or bfloat16."""
-    return _attend("pcg_cache4_attend", cache, (_dtype_code(q),), cache4_attend_workspace_bytes, q, block_table, lens, q_start, longest, scale,
+    return _attend(lib().pcg_cache4_attend, "pcg_cache4_attend", cache, (_dtype_code(q),), cache4_attend_workspace_bytes, q, block_table, lens, q_start, longest, scale,
                    window, out, workspace)
 
 

@@ -61,31 +61,43 @@ __device__ __forceinline__ void store(T *p, const float (&x)[N]) {
   }
 }
 
+// N / 2 numbers of a table's row.
+template <int N>
+__device__ __forceinline__ void load_half(const float *p, float (&x)[N]) {
+  if constexpr (N == 8) {
+    const float4 v = *reinterpret_cast<const float4 *>(p);
+    x[0] = v.x;
+    x[1] = v.y;
+    x[2] = v.z;
+    x[3] = v.w;
+  } else {
+    const float2 v = *reinterpret_cast<const float2 *>(p);
+    x[0] = v.x;
+    x[1] = v.y;
+  }
+}
+
 __device__ __forceinline__ void turn(float &x, float &y, float cs, float sn) {
   const double a = x, b = y, c = cs, s = sn;
   x = (float) fma(-b, s, a * c);
   y = (float) fma(a, s, b * c);
 }
 
-// Where token t goes; false: nowhere.
+// Where token t goes.  What it is made of is asked for ahead of anything that depends on it; a row of the rotation's table follows.
 struct Place {
+  int32_t number, position;
+  __device__ __forceinline__ Place(const AppendArgs &a, int64_t t) : number(a.slots[t]), position(a.table ? a.positions[t] : 0) {}
   int64_t page, slot;
-  const float *row;           // of the rotation's table
-};
-__device__ __forceinline__ bool place_of(const AppendArgs &a, int64_t t, Place &p) {
-  const int32_t slot = a.slots[t];
-  if (slot < 0) return false;
-  p.page = slot / a.page_size;
-  p.slot = slot - p.page * a.page_size;
-  p.row = nullptr;
-  if (p.page >= a.num_pages) return false;
-  if (a.table) {
-    const int32_t at = a.positions[t];
-    if (at < 0 || at >= a.places) return false;
-    p.row = a.table + (int64_t) at * a.table_stride;
+  const float *row;
+  // false: nowhere
+  __device__ __forceinline__ bool find(const AppendArgs &a) {
+    if (number < 0) return false;
+    page = number / a.page_size;
+    slot = number - page * a.page_size;
+    row = a.table ? a.table + (int64_t) position * a.table_stride : nullptr;
+    return page < a.num_pages && (!a.table || (uint32_t) position < (uint32_t) a.places);
   }
-  return true;
-}
+};
 
 // How a head is dealt to threads: `pairs` threads take E pairs each, or E elements with neighbours for pairs, then each takes E of
 // the elements behind `rot`.  A thread owns what it reads, so that rows may be rotated in place.
@@ -99,52 +111,59 @@ struct Deal {
   }
 };
 
-// Part `i` of a head, from `x` to `to`.  VEC: parts are whole and aligned, and so are those of the table.
+// Part `i` of a head at x.  VEC: parts are whole and aligned, and so are those of the table.
 template <typename T, bool VEC>
-__device__ __forceinline__ void rotate_part(const AppendArgs &a, const Deal<T> &deal, int32_t i, const float *row, const T *x, T *to) {
-  constexpr int E = Deal<T>::E;
-  const int32_t half = a.rot / 2;
-  if (a.interleaved) {
-    const int32_t d = i * E;
-    float v[E];
-    load<T, E>(x + d, v);
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      const int32_t j = (d + e) / 2;
-      if (j < half) turn(v[e], v[e + 1], row[j], row[half + j]);
-    }
-    store<T, E>(to + d, v);
-    return;
-  }
-  if (i < deal.pairs) {
-    const int32_t j = i * E;
+struct HeadPart {
+  static constexpr int E = Deal<T>::E;
+  const T *x;
+  int32_t at, other;          // first elements, other < 0: of pairs that are neighbours or of none
+  float u[E], v[E];
+  __device__ __forceinline__ HeadPart(const AppendArgs &a, const Deal<T> &deal, int32_t i, const T *x_) : x(x_) {
+    at = a.interleaved || i < deal.pairs ? i * E : a.rot + (i - deal.pairs) * E;
+    other = !a.interleaved && i < deal.pairs ? a.rot / 2 + at : -1;
     if constexpr (VEC) {
-      float u[E], v[E], c[E], s[E];
-      load<T, E>(x + j, u);
-      load<T, E>(x + half + j, v);
-      load<float, E>(row + j, c);
-      load<float, E>(row + half + j, s);
+      load<T, E>(x + at, u);
+      if (other >= 0) load<T, E>(x + other, v);
+    }
+  }
+  __device__ __forceinline__ void turn_to(const AppendArgs &a, const float *row, T *to) {
+    const int32_t half = a.rot / 2;
+    if constexpr (VEC) {
+      float c[E], s[E];
+      if (other >= 0) {
+        load<float, E>(row + at, c);
+        load<float, E>(row + half + at, s);
 #pragma unroll
-      for (int e = 0; e < E; ++e) turn(u[e], v[e], c[e], s[e]);
-      store<T, E>(to + j, u);
-      store<T, E>(to + half + j, v);
+        for (int e = 0; e < E; ++e) turn(u[e], v[e], c[e], s[e]);
+        store<T, E>(to + other, v);
+      } else if (at < a.rot) {
+        load_half<E>(row + at / 2, c);
+        load_half<E>(row + half + at / 2, s);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) turn(u[e], u[e + 1], c[e / 2], s[e / 2]);
+      }
+      store<T, E>(to + at, u);
+    } else if (other >= 0) {
+      for (int32_t e = at; e < min(at + E, half); ++e) {
+        float y = as_float<T>(x[e]), z = as_float<T>(x[half + e]);
+        turn(y, z, row[e], row[half + e]);
+        to[e] = as_type<T>(y);
+        to[half + e] = as_type<T>(z);
+      }
     } else {
-      for (int32_t e = j; e < min(j + E, half); ++e) {
-        float u = as_float<T>(x[e]), v = as_float<T>(x[half + e]);
-        turn(u, v, row[e], row[half + e]);
-        to[e] = as_type<T>(u);
-        to[half + e] = as_type<T>(v);
+      for (int32_t e = at; e < min(at + E, a.D); ++e) {
+        if (e >= a.rot) {
+          to[e] = x[e];
+          continue;
+        }
+        float y = as_float<T>(x[e]), z = as_float<T>(x[e + 1]);
+        turn(y, z, row[e / 2], row[half + e / 2]);
+        to[e++] = as_type<T>(y);
+        to[e] = as_type<T>(z);
       }
     }
-    return;
   }
-  const int32_t j = a.rot + (i - deal.pairs) * E;
-  if constexpr (VEC) {
-    *reinterpret_cast<uint4 *>(to + j) = *reinterpret_cast<const uint4 *>(x + j);
-  } else {
-    for (int32_t e = j; e < min(j + E, a.D); ++e) to[e] = x[e];
-  }
-}
+};
 
 struct Counts {
   int32_t token, part;                 // threads of a token, of a head
@@ -155,41 +174,40 @@ struct Counts {
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Counts n, Deal<T> deal) {
   constexpr int E = Deal<T>::E;
-  const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
   uint32_t t, i, head, part;
-  split_by(at, (uint32_t) n.token, n.magic_token, t, i);
+  split_by(blockIdx.x * kThreads + threadIdx.x, (uint32_t) n.token, n.magic_token, t, i);
   if (t >= a.T) return;
-  Place p;
-  if (!place_of(a, t, p)) return;
+  Place p(a, t);
   const int64_t row = t;
   const int32_t with_q = a.q ? a.heads : 0;
   if ((int32_t) i < (with_q + a.kv_heads) * n.part) {
     split_by(i, (uint32_t) n.part, n.magic_part, head, part);
-    if ((int32_t) head < with_q) {
-      rotate_part<T, VEC>(a, deal, (int32_t) part, p.row, reinterpret_cast<const T *>(a.q) + row * a.q_tok + head * a.q_head,
-                          reinterpret_cast<T *>(a.q_out) + row * a.o_tok + head * a.o_head);
-    } else {
-      head -= with_q;
-      rotate_part<T, VEC>(a, deal, (int32_t) part, p.row, reinterpret_cast<const T *>(a.k_new) + row * a.k_tok + head * a.k_head,
-                          reinterpret_cast<T *>(a.k) + p.page * a.page_stride + p.slot * a.slot_stride + head * a.head_stride);
-    }
+    const bool query = (int32_t) head < with_q;
+    const int64_t h = query ? head : head - with_q;
+    HeadPart<T, VEC> x(a, deal, (int32_t) part, query ? reinterpret_cast<const T *>(a.q) + row * a.q_tok + h * a.q_head
+                                                      : reinterpret_cast<const T *>(a.k_new) + row * a.k_tok + h * a.k_head);
+    if (!p.find(a)) return;
+    x.turn_to(a, p.row, query ? reinterpret_cast<T *>(a.q_out) + row * a.o_tok + h * a.o_head
+                              : reinterpret_cast<T *>(a.k) + p.page * a.page_stride + p.slot * a.slot_stride + h * a.head_stride);
     return;
   }
   i -= (with_q + a.kv_heads) * n.part;
   const int32_t parts = a.D / E;
   head = i / parts;
   const int64_t d = (int64_t) (i - head * parts) * E;
-  const T *from = reinterpret_cast<const T *>(a.v_new) + row * a.v_tok + head * a.v_head + d;
-  T *to = reinterpret_cast<T *>(a.v) + p.page * a.page_stride + p.slot * a.slot_stride + head * a.head_stride + d;
-  *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
+  const uint4 x = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(a.v_new) + row * a.v_tok + head * a.v_head + d);
+  if (!p.find(a)) return;
+  *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.v) + p.page * a.page_stride + p.slot * a.slot_stride + head * a.head_stride + d) = x;
 }
 
-// The largest of 16 lanes.
-__device__ __forceinline__ uint32_t max16(uint32_t x) {
-  x = max(x, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) x, 0x128, 0xf, 0xf, false));
-  x = max(x, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) x, 0x124, 0xf, 0xf, false));
-  x = max(x, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) x, 0x122, 0xf, 0xf, false));
-  return max(x, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) x, 0x121, 0xf, 0xf, false));
+// The largest of N lanes, 8 or 16.
+template <int N>
+__device__ __forceinline__ uint32_t max_of(uint32_t x) {
+  x = max(x, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) x, 0xb1, 0xf, 0xf, false));        // neighbours
+  x = max(x, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) x, 0x4e, 0xf, 0xf, false));        // pairs of four
+  x = max(x, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) x, 0x141, 0xf, 0xf, false));       // eight the other way round
+  if constexpr (N == 16) x = max(x, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) x, 0x140, 0xf, 0xf, false));
+  return x;
 }
 
 // The scale of numbers whose largest absolute value has these bits: a sixth of it in bfloat16, at most what 6 times is finite of.  (A
@@ -215,82 +233,107 @@ __device__ __forceinline__ uint32_t codes_of(const float (&x)[8], double inverse
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r[6], r[7], 1.f, 3);
 }
 
-// Eight rotated elements of a key from element d on.
+// Eight elements of a key from element d on, and their partners.
 template <typename T, bool VEC>
-__device__ __forceinline__ void rotated_eight(const AppendArgs &a, const float *row, const T *x, int32_t d, float (&v)[8]) {
-  load<T, 8>(x + d, v);
-  const int32_t half = a.rot / 2;
-  if (a.interleaved) {
+struct KeyEight {
+  const T *x;
+  int32_t d;
+  bool upper;                 // the second ones of their pairs
+  float v[8], u[8];
+  __device__ __forceinline__ KeyEight(const AppendArgs &a, const T *x_, int32_t d_) : x(x_), d(d_) {
+    load<T, 8>(x + d, v);
+    upper = d >= a.rot / 2;
+    if (VEC && !a.interleaved && d < a.rot) load<T, 8>(x + (upper ? d - a.rot / 2 : d + a.rot / 2), u);
+  }
+  __device__ __forceinline__ void turn_by(const AppendArgs &a, const float *row) {
+    const int32_t half = a.rot / 2;
+    if (a.interleaved) {
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const int32_t j = (d + e) / 2;
-      if (j < half) turn(v[e], v[e + 1], row[j], row[half + j]);
-    }
-  } else if constexpr (VEC) {
-    if (d >= a.rot) return;
-    const bool upper = d >= half;
-    const int32_t j = upper ? d - half : d;
-    float u[8], c[8], s[8];
-    load<T, 8>(x + (upper ? j : half + j), u);
-    load<float, 8>(row + j, c);
-    load<float, 8>(row + half + j, s);
-    // the upper one of a pair is turned by the other sign
+      for (int e = 0; e < 8; e += 2) {
+        const int32_t j = (d + e) / 2;
+        if (j < half) turn(v[e], v[e + 1], row[j], row[half + j]);
+      }
+    } else if constexpr (VEC) {
+      if (d >= a.rot) return;
+      const int32_t j = upper ? d - half : d;
+      float c[8], s[8];
+      load<float, 8>(row + j, c);
+      load<float, 8>(row + half + j, s);
+      // the upper one of a pair is turned by the other sign
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float) fma((double) u[e], (double) (upper ? s[e] : -s[e]), (double) v[e] * (double) c[e]);
-  } else {
+      for (int e = 0; e < 8; ++e) v[e] = (float) fma((double) u[e], (double) (upper ? s[e] : -s[e]), (double) v[e] * (double) c[e]);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (d + e >= a.rot) continue;
-      const bool upper = d + e >= half;
-      const int32_t j = upper ? d + e - half : d + e;
-      const float u = as_float<T>(x[upper ? j : half + j]), s = row[half + j];
-      v[e] = (float) fma((double) u, (double) (upper ? s : -s), (double) v[e] * (double) row[j]);
+      for (int e = 0; e < 8; ++e) {
+        if (d + e >= a.rot) continue;
+        const bool second = d + e >= half;
+        const int32_t j = second ? d + e - half : d + e;
+        const float w = as_float<T>(x[second ? j : half + j]), s = row[half + j];
+        v[e] = (float) fma((double) w, (double) (second ? s : -s), (double) v[e] * (double) row[j]);
+      }
     }
   }
-}
+};
 
-// Queries a part a thread in the first blocks; keys and values 16 lanes a head, eight elements each, in the others.
-template <typename T, bool VEC>
-__global__ __launch_bounds__(kThreads) void append4_kernel(AppendArgs a, Counts n, Deal<T> deal, uint32_t q_blocks) {
-  uint32_t t, i;
-  Place p;
-  if (blockIdx.x < q_blocks) {
-    uint32_t head, part;
-    split_by(blockIdx.x * kThreads + threadIdx.x, (uint32_t) n.token, n.magic_token, t, i);
-    if (t >= a.T || !place_of(a, t, p)) return;
-    split_by(i, (uint32_t) n.part, n.magic_part, head, part);
-    rotate_part<T, VEC>(a, deal, (int32_t) part, p.row, reinterpret_cast<const T *>(a.q) + (int64_t) t * a.q_tok + head * a.q_head,
-                        reinterpret_cast<T *>(a.q_out) + (int64_t) t * a.o_tok + head * a.o_head);
-    return;
-  }
-  const uint32_t group = ((blockIdx.x - q_blocks) * kThreads + threadIdx.x) / 16;
-  const int32_t lane = threadIdx.x & 15, d = 8 * lane;
-  t = group / (2 * a.kv_heads);
-  i = group - t * (2 * a.kv_heads);
-  if (t >= a.T || !place_of(a, t, p)) return;           // all 16 lanes
-  const bool value = (int32_t) i >= a.kv_heads;
-  const int64_t head = value ? i - a.kv_heads : i;
-  const T *x = value ? reinterpret_cast<const T *>(a.v_new) + (int64_t) t * a.v_tok + head * a.v_head
-                     : reinterpret_cast<const T *>(a.k_new) + (int64_t) t * a.k_tok + head * a.k_head;
-  float v[8] = {};
-  if (d < a.D) {
-    if (value || !p.row) load<T, 8>(x + d, v);
-    else rotated_eight<T, VEC>(a, p.row, x, d, v);
-  }
+// Scale and codes of a head's elements, eight a lane (v of lanes behind the last: zeros).
+template <int N>
+__device__ __forceinline__ uint16_t quantise(const float (&v)[8], uint32_t &codes) {
   uint32_t largest = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(v[e]) & 0x7fffffffu);
-  const uint16_t scale = scale_of(max16(largest));
+  const uint16_t scale = scale_of(max_of<N>(largest));
   const float s = as_float<uint16_t>(scale);
-  const uint32_t codes = s > 0.f ? codes_of(v, 1.0 / (double) s) : 0;          // all zero, or NaN
-  if (d < (a.D + 31) / 32 * 32) {
-    uint8_t *to = reinterpret_cast<uint8_t *>(value ? a.v : a.k) + p.page * a.page_stride + p.slot * a.slot_stride + head * a.head_stride;
-    *reinterpret_cast<uint32_t *>(to + 4 * lane) = codes;
-  }
-  if (lane == 0) a.scales[2 * (p.page * a.s_page + p.slot * a.s_slot + head * a.s_head) + (value ? 1 : 0)] = scale;
+  codes = s > 0.f ? codes_of(v, 1.0 / (double) s) : 0;          // all zero, or NaN
+  return scale;
 }
 
-// Eight elements of a key or value a thread.
+// Queries a part a thread in the first blocks; in the others N lanes a head of keys and values, eight elements of each a lane.  Neighbours
+// are the tokens of a head, or the heads of a token, as they lie closer in the cache (see launch_append).
+template <typename T, bool VEC, int N>
+__global__ __launch_bounds__(kThreads) void append4_kernel(AppendArgs a, Counts n, Deal<T> deal, uint32_t q_blocks, bool by_tokens) {
+  uint32_t t, i;
+  if (blockIdx.x < q_blocks) {
+    uint32_t head, part;
+    split_by(blockIdx.x * kThreads + threadIdx.x, (uint32_t) n.token, n.magic_token, t, i);
+    if (t >= a.T) return;
+    Place p(a, t);
+    split_by(i, (uint32_t) n.part, n.magic_part, head, part);
+    HeadPart<T, VEC> x(a, deal, (int32_t) part, reinterpret_cast<const T *>(a.q) + (int64_t) t * a.q_tok + head * a.q_head);
+    if (p.find(a)) x.turn_to(a, p.row, reinterpret_cast<T *>(a.q_out) + (int64_t) t * a.o_tok + head * a.o_head);
+    return;
+  }
+  const uint32_t group = ((blockIdx.x - q_blocks) * kThreads + threadIdx.x) / N;
+  const int32_t lane = threadIdx.x % N, d = 8 * lane;
+  if (by_tokens) {
+    i = group / (uint32_t) a.T;
+    t = group - i * (uint32_t) a.T;
+  } else {
+    t = group / (uint32_t) a.kv_heads;
+    i = group - t * (uint32_t) a.kv_heads;
+  }
+  if (t >= a.T || i >= (uint32_t) a.kv_heads) return;   // all N lanes
+  Place p(a, t);
+  const int64_t head = i, in = d < a.D ? d : 0;
+  KeyEight<T, VEC> key(a, reinterpret_cast<const T *>(a.k_new) + (int64_t) t * a.k_tok + head * a.k_head, in);
+  float value[8];
+  load<T, 8>(reinterpret_cast<const T *>(a.v_new) + (int64_t) t * a.v_tok + head * a.v_head + in, value);
+  if (!p.find(a)) return;                               // all N lanes
+  if (p.row) key.turn_by(a, p.row);
+  if (d >= a.D) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) key.v[e] = value[e] = 0.f;
+  }
+  uint32_t codes[2];
+  const uint32_t scales = (uint32_t) quantise<N>(key.v, codes[0]) | (uint32_t) quantise<N>(value, codes[1]) << 16;
+  const int64_t at = p.page * a.page_stride + p.slot * a.slot_stride + head * a.head_stride + 4 * lane;
+  if (d < (a.D + 31) / 32 * 32) {
+    *reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(a.k) + at) = codes[0];
+    *reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(a.v) + at) = codes[1];
+  }
+  if (lane == 0) reinterpret_cast<uint32_t *>(a.scales)[p.page * a.s_page + p.slot * a.s_slot + head * a.s_head] = scales;
+}
+
+// Eight elements of a key and of its value a thread.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void cache4_read_kernel(ReadArgs r, Counts n) {
   uint32_t t, i, head, part;
@@ -301,24 +344,21 @@ __global__ __launch_bounds__(kThreads) void cache4_read_kernel(ReadArgs r, Count
   if (slot < 0) return;
   const int64_t page = slot / r.page_size, at = slot - page * r.page_size;
   if (page >= r.num_pages) return;
-  const bool value = (int32_t) head >= r.kv_heads;
-  const int64_t h = value ? head - r.kv_heads : head;
-  const uint32_t w = *reinterpret_cast<const uint32_t *>((value ? r.v : r.k) + page * r.page_stride + at * r.slot_stride + h * r.head_stride +
-                                                         4 * part);
-  const uint16_t scale = r.scales[2 * (page * r.s_page + at * r.s_slot + h * r.s_head) + (value ? 1 : 0)];
-  float s = as_float<uint16_t>(scale);
-  s = fmaf(s, 0.f, s);                 // what is not finite is NaN
-  float x[8];
-  auto two = [&](floatx2 y, int e) {
-    x[e] = y[0] * s;
-    x[e + 1] = y[1] * s;
-  };
-  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), 0);
-  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1), 2);
-  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), 4);
-  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3), 6);
-  T *to = value ? reinterpret_cast<T *>(r.v_out) + (int64_t) t * r.v_tok + h * r.v_head : reinterpret_cast<T *>(r.k_out) + (int64_t) t * r.k_tok + h * r.k_head;
-  store<T, 8>(to + 8 * part, x);
+  const int64_t from = page * r.page_stride + at * r.slot_stride + head * r.head_stride + 4 * part;
+  const uint32_t codes[2] = {*reinterpret_cast<const uint32_t *>(r.k + from), *reinterpret_cast<const uint32_t *>(r.v + from)};
+  const uint32_t scales = reinterpret_cast<const uint32_t *>(r.scales)[page * r.s_page + at * r.s_slot + head * r.s_head];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float s = __uint_as_float(which ? scales & 0xffff0000u : scales << 16);
+    s = fmaf(s, 0.f, s);               // what is not finite is NaN
+    const floatx2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which], 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which], 1.f, 1),
+                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which], 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which], 1.f, 3)};
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = y[e / 2][e % 2] * s;
+    T *to = which ? reinterpret_cast<T *>(r.v_out) + (int64_t) t * r.v_tok + head * r.v_head : reinterpret_cast<T *>(r.k_out) + (int64_t) t * r.k_tok + head * r.k_head;
+    store<T, 8>(to + 8 * part, x);
+  }
 }
 
 uint32_t magic(int32_t d) { return d > 1 ? (uint32_t) (((uint64_t) 1 << 32) / (uint32_t) d) : UINT32_MAX; }
@@ -337,9 +377,16 @@ hipError_t go(const AppendArgs &a, hipStream_t stream) {
   if (a.scales) {
     n.token = a.q ? a.heads * deal.all : 1;
     n.magic_token = magic(n.token);
-    const uint32_t q_blocks = a.q ? blocks(a.T * n.token) : 0, kv_blocks = blocks(a.T * a.kv_heads * 32);
-    if (vec) append4_kernel<T, true><<<q_blocks + kv_blocks, kThreads, 0, stream>>>(a, n, deal, q_blocks);
-    else append4_kernel<T, false><<<q_blocks + kv_blocks, kThreads, 0, stream>>>(a, n, deal, q_blocks);
+    const int lanes = a.D <= 64 ? 8 : 16;
+    const uint32_t q_blocks = a.q ? blocks(a.T * n.token) : 0, all = q_blocks + blocks(a.T * a.kv_heads * lanes);
+    const bool by_tokens = a.slot_stride < a.head_stride;
+    if (lanes == 8) {
+      if (vec) append4_kernel<T, true, 8><<<all, kThreads, 0, stream>>>(a, n, deal, q_blocks, by_tokens);
+      else append4_kernel<T, false, 8><<<all, kThreads, 0, stream>>>(a, n, deal, q_blocks, by_tokens);
+    } else {
+      if (vec) append4_kernel<T, true, 16><<<all, kThreads, 0, stream>>>(a, n, deal, q_blocks, by_tokens);
+      else append4_kernel<T, false, 16><<<all, kThreads, 0, stream>>>(a, n, deal, q_blocks, by_tokens);
+    }
   } else {
     n.token = ((a.q ? a.heads : 0) + a.kv_heads) * deal.all + a.kv_heads * (a.D / E);
     n.magic_token = magic(n.token);
@@ -361,7 +408,7 @@ hipError_t launch_append(const AppendArgs &a, bool bf16, hipStream_t stream) { r
 hipError_t launch_cache4_read(const ReadArgs &r, bool bf16, hipStream_t stream) {
   Counts n;
   n.part = r.D / 8;
-  n.token = 2 * r.kv_heads * n.part;
+  n.token = r.kv_heads * n.part;
   n.magic_part = magic(n.part);
   n.magic_token = magic(n.token);
   if (bf16) cache4_read_kernel<uint16_t><<<blocks(r.T * n.token), kThreads, 0, stream>>>(r, n);

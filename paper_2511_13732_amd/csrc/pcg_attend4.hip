@@ -616,10 +616,10 @@ auto by_rows(int64_t rows, F f) {
     if (rows <= 32) return PCG_ROWS(2, 4);
     if (rows <= 48) return PCG_ROWS(3, 4);
     if (rows <= 64) return PCG_ROWS(2, 2);
-    return PCG_ROWS(2, 1);
+    if (rows > 96 && rows <= 128) return PCG_ROWS(2, 1);
+    return PCG_ROWS(3, 2);
   } else {
-    if (rows <= 32) return PCG_ROWS(1, 2);
-    return PCG_ROWS(1, 1);
+    return PCG_ROWS(1, 2);
   }
 #undef PCG_ROWS
 }
