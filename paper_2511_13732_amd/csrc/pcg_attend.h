@@ -27,6 +27,7 @@ struct AttendArgs {
 struct Attend4Args : AttendArgs {
   const uint32_t *scales;
   int64_t s_page, s_tok, s_head;
+  bool pairs;                      // heads lie closer together than a head's keys, and are of even number
 };
 
 size_t attend_workspace_bytes(int32_t G, int32_t D, int64_t longest);

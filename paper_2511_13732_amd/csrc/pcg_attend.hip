@@ -602,7 +602,7 @@ __global__ __launch_bounds__(kAttendThreads, (Thick<T, DP, WK>::kRuns / 256)) vo
   using W = Thick<T, DP, WK>;
   __shared__ __align__(16) unsigned char lds[W::kLds];
   __shared__ int odd;
-  work_on_run<DP, W::R, W::TK, W::kLeast, kAttendWaves>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
+  work_on_run<DP, W::R, W::TK, W::kLeast, kAttendWaves>(a, all_heads(a), lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
     thick_piece<T, DP, WK, PAGES, ONCE>(a, u, tile, tiles, lds, &odd, (int) blockIdx.x / kCUs, part);
   });
 }
@@ -808,7 +808,7 @@ __global__ __launch_bounds__(Thin<DP>::NW * kWave, (Thin<DP>::kRuns * Thin<DP>::
   __shared__ __align__(16) unsigned char lds[Thin<DP>::kLds];
   __shared__ int odd;
   if (threadIdx.x == 0) odd = 0;        // pieces come behind barriers
-  work_on_run<DP, 32, Thin<DP>::TK, kThinLeast, Thin<DP>::NW>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32> *part) {
+  work_on_run<DP, 32, Thin<DP>::TK, kThinLeast, Thin<DP>::NW>(a, all_heads(a), lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, 32> *part) {
     thin_piece<DP, PAGES>(a, u, tile, tiles, lds, &odd, part);
   });
 }

@@ -581,7 +581,22 @@ __global__ __launch_bounds__(kAttendThreads, (Work4<T, DP, NB, WK>::kGroups)) vo
                                                                                               Part<DP, Work4<T, DP, NB, WK>::R> *parts) {
   using W = Work4<T, DP, NB, WK>;
   __shared__ __align__(16) unsigned char lds[W::kLds];
-  work_on_run<DP, W::R, W::TK, W::kLeast, kAttendWaves, W::kCost>(a, lds, join, parts, [&](const Unit &u, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
+  // Where heads lie closer together than a head's keys, two workgroups on one XCD (8 blocks apart) work through the keys of two neighbours at
+  // the same time: memory is read in pieces of 128 bytes, or of 64 that are neighbours.
+  Heads deal = all_heads(a);
+  if (a.pairs) {
+    deal.first = (int32_t) (deal.block / 8 % 2);
+    deal.step = 2;
+    deal.heads /= 2;
+    deal.block = deal.block / 16 * 8 + deal.block % 8;
+    deal.count /= 2;
+    join += deal.first * deal.count;
+    parts += 2 * (int64_t) deal.first * deal.count;
+  }
+  work_on_run<DP, W::R, W::TK, W::kLeast, kAttendWaves, W::kCost>(a, deal, lds, join, parts,
+                                                                  [&](const Unit &unit, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
+    Unit u = unit;
+    u.head = deal.first + u.head * deal.step;
     codes_piece<T, DP, NB, WK, PAGES>(a, u, tile, tiles, lds, part);
   });
 }

@@ -266,6 +266,18 @@ __device__ __forceinline__ int32_t unit_tiles(const AttendArgs &a, Unit &u) {
   return (u.k_hi - u.k_lo + TK - 1) / TK;
 }
 
+// Which shared heads a workgroup's runs are of (first, first + step, ..: `heads` of them, numbered from 0 in units), and how many workgroups
+// there are for those, of which it is number `block`.
+struct Heads {
+  int32_t first, step, heads;
+  uint32_t block;
+  int32_t count;
+};
+// All workgroups are for all heads.
+__device__ __forceinline__ Heads all_heads(const AttendArgs &a) {
+  return Heads{0, 1, a.heads_kv, blockIdx.x, (int32_t) gridDim.x};
+}
+
 // All units (requests, their shared heads, their row blocks, in this order) in a row, COST for what a unit costs beside its tiles
 // and then 1 for each of them, are cut into `runs` runs of a length, one a workgroup; the first `longer` are one longer than `each`.
 struct Run {
@@ -284,12 +296,12 @@ struct Run {
   }
 };
 
-// Finds this workgroup's run, of `count` at most, LEAST long at least (but for the last): its first unit and how far into it.
+// Finds this workgroup's run, of deal.count at most, LEAST long at least (but for the last): its first unit and how far into it.
 // Every workgroup adds the requests up by itself, each wave its share of them, a request a lane or (with many row blocks) a row block
 // a lane: for 64 requests that takes two microseconds, less than a launch ahead would.  Lengths are whole numbers below 2^53 in
 // double, whose running sums go through DPP.
 template <int R, int TK, int LEAST, int NW, int COST>
-__device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsigned char *lds, Unit &u, int64_t &into) {
+__device__ __forceinline__ Run find_run(const AttendArgs &a, const Heads &deal, unsigned char *lds, Unit &u, int64_t &into) {
   double *sums = reinterpret_cast<double *>(lds);
   int32_t *found = reinterpret_cast<int32_t *>(sums + NW);
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -317,7 +329,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
       all = wave_sum(all);
       if (lane == l) one = all;
     }
-    return wave_scan(one * a.heads_kv);
+    return wave_scan(one * deal.heads);
   };
   Unit v;
   double one, upto = 0, mine = 0;
@@ -336,10 +348,10 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
     sum += x;
   }
   const int64_t total = scalar((int64_t) sum);
-  run.runs = (int32_t) min((int64_t) count, (total + LEAST - 1) / LEAST);
+  run.runs = (int32_t) min((int64_t) deal.count, (total + LEAST - 1) / LEAST);
   // An XCD (every eighth workgroup) takes runs that follow each other: those of a shared head find its keys in its L2.
   const int32_t eighth = (run.runs + 7) / 8;
-  run.index = (int32_t) blockIdx.x / 8 < eighth ? (int32_t) (blockIdx.x % 8) * eighth + (int32_t) blockIdx.x / 8 : run.runs;
+  run.index = (int32_t) deal.block / 8 < eighth ? (int32_t) (deal.block % 8) * eighth + (int32_t) deal.block / 8 : run.runs;
   run.left = 0;
   if (run.index >= run.runs) return run;
   // a quotient of numbers below 2^53, off by one at most in double
@@ -360,7 +372,7 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
       }
       const int l = __ffsll((long long) past) - 1;
       const double length = read_lane(one, l);
-      ahead -= read_lane(upto, l) - length * a.heads_kv;
+      ahead -= read_lane(upto, l) - length * deal.heads;
       int32_t head = (int32_t) (ahead / length);      // off by one at most
       if (head * length > ahead) --head;
       if (ahead - head * length >= length) ++head;
@@ -410,11 +422,11 @@ __device__ __forceinline__ Run find_run(const AttendArgs &a, int32_t count, unsi
 
 // The unit behind u.
 template <int R>
-__device__ __forceinline__ void next_unit(const AttendArgs &a, Unit &u) {
+__device__ __forceinline__ void next_unit(const AttendArgs &a, int32_t heads, Unit &u) {
   u.r0 += R;
   if (u.r0 < u.rows) return;
   u.r0 = 0;
-  if (++u.head < a.heads_kv) return;
+  if (++u.head < heads) return;
   u.head = 0;
   do {
     if (++u.b >= a.B) return;
@@ -426,10 +438,10 @@ __device__ __forceinline__ void next_unit(const AttendArgs &a, Unit &u) {
 // Calls work(unit, first tile, tiles, part) for every unit or piece of one in this workgroup's run; part: NULL where the unit is
 // whole.  A workgroup has two places for parts: 1 for the unit that it begins and does not finish, 0 for one that another began.
 template <int DP, int R, int TK, int LEAST, int NW, int COST = kCost, typename Work>
-__device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *lds, Join *join, Part<DP, R> *parts, Work work) {
+__device__ __forceinline__ void work_on_run(const AttendArgs &a, const Heads &deal, unsigned char *lds, Join *join, Part<DP, R> *parts, Work work) {
   Unit u;
   int64_t into = 0;
-  Run run = find_run<R, TK, LEAST, NW, COST>(a, (int32_t) gridDim.x, lds, u, into);
+  Run run = find_run<R, TK, LEAST, NW, COST>(a, deal, lds, u, into);
   Join j{0, 0, 0, 0, 0};
   // Where a head's keys are read by several row blocks, the end of a unit that another run began comes last: the runs of an XCD then
   // begin with units from their first key on, and those of one head read the same keys at the same time, out of its L2 (us with
@@ -450,7 +462,7 @@ __device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *
       if (part && tile == 0 && tiles > 0) {
         // this run and those that begin ahead of the unit's end
         j.parts = run.ahead_of(run.begin(run.index + 1) - run.left + all + COST - until) - run.index;
-        j.head = u.head;
+        j.head = deal.first + u.head * deal.step;
         j.r0 = u.r0;
         j.rows = u.rows;
         j.first = u.first;
@@ -479,11 +491,11 @@ __device__ __forceinline__ void work_on_run(const AttendArgs &a, unsigned char *
     }
     if (tiles > 0) work(u, tile, tiles, part);
     into = 0;
-    if (run.left > 0) next_unit<R>(a, u);
+    if (run.left > 0) next_unit<R>(a, deal.heads, u);
   }
   if (threadIdx.x != 0) return;
   if (run.index < run.runs) join[run.index] = j;
-  if ((int32_t) blockIdx.x >= run.runs) join[blockIdx.x] = Join{0, 0, 0, 0, 0};
+  if ((int32_t) deal.block >= run.runs) join[deal.block] = Join{0, 0, 0, 0, 0};
 }
 
 // Rows of a wave on their way to another through LDS: 32 rows' outputs (not divided), references and sums.

@@ -402,6 +402,7 @@ int pcg_cache4_attend(const pcg_kv4_cache *cache, pcg_dtype dt, const void *q, i
   a.s_page = c.scale_page_stride;
   a.s_tok = c.scale_slot_stride;
   a.s_head = c.scale_head_stride;
+  a.pairs = c.kv_heads % 2 == 0 && c.head_stride < c.slot_stride;
   take_table(a, block_table, table_stride, max_blocks, lens, c.page_size, c.num_pages);
   return finish(launch_cache4_attend(a, dt == PCG_BF16, longest, workspace, (hipStream_t) hip_stream));
 }
