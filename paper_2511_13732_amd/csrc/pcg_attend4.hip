@@ -508,71 +508,84 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
       if (quarter == 0) sums[(stream * NB + b) * 16 + l16] = floatx2{ref[b], all};
     }
   }
+  auto give = [&](int pass) {
 #pragma unroll
-  for (int pass = 0; pass < W::kPasses; ++pass) {
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int m = 0; m < kColumns; ++m) room[((stream * NB + b) * kColumns + m) * kWave + lane] = o[b][pass * kColumns + m];
+    bare_barrier();
+  };
+  if constexpr (WK > 1) give(0);
+  // Where each row's outputs go, and what the streams' are to be multiplied by; a row without a score above -infinity is zeros, also where a value
+  // was NaN.
+  float f[NB][WK];
+  char *to[NB];
+  bool there[NB], zero[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    int32_t r = block + 16 * b + l16;
+    asm("" : "+v"(r));                  // formed here, not kept in registers since the beginning
+    const Row w = row_at(a, u, u.r0 + r);
+    there[b] = w.there;
+    float now = ref[b], all = 0.f;
+    f[b][0] = 1.f;
     if constexpr (WK > 1) {
-      if (pass) bare_barrier();
+      floatx2 of[WK];
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int i = 0; i < WK; ++i) of[i] = sums[(i * NB + b) * 16 + l16];
+      now = of[0][0];
 #pragma unroll
-        for (int m = 0; m < kColumns; ++m) room[((stream * NB + b) * kColumns + m) * kWave + lane] = o[b][pass * kColumns + m];
-      bare_barrier();
-    }
+      for (int i = 1; i < WK; ++i) now = fmaxf(now, of[i][0]);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      int32_t r = block + 16 * b + l16;
-      asm("" : "+v"(r));                // formed here, not kept in registers since the beginning
-      const Row w = row_at(a, u, u.r0 + r);
-      float now = ref[b], all = 0.f, f[WK];
-      if constexpr (WK > 1) {
-        floatx2 of[WK];
-#pragma unroll
-        for (int i = 0; i < WK; ++i) of[i] = sums[(i * NB + b) * 16 + l16];
-        now = of[0][0];
-#pragma unroll
-        for (int i = 1; i < WK; ++i) now = fmaxf(now, of[i][0]);
-#pragma unroll
-        for (int i = 0; i < WK; ++i) {
-          f[i] = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of[i][0] - now);
-          all += f[i] * of[i][1];
-        }
-      } else {
-        all = quad_sum(sum[b]);
+      for (int i = 0; i < WK; ++i) {
+        f[b][i] = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of[i][0] - now);
+        all = fmaf(f[b][i], of[i][1], all);
       }
-      if (part && quarter == 0 && stream == 0 && pass == 0 && w.there) {
+    } else {
+      all = quad_sum(sum[b]);
+    }
+    zero[b] = !part && all == 0.f;
+    if (part) {
+      to[b] = reinterpret_cast<char *>(part->o[r] + 4 * quarter);
+      if (quarter == 0 && stream == 0 && w.there) {
         part->ref[r] = now;
         part->sum[r] = all;
       }
+    } else {
+      to[b] = reinterpret_cast<char *>(reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head + 4 * quarter);
       const float inv = 1.f / all;
-      T *const out = reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head;
 #pragma unroll
-      for (int m = 0; m < kMine; ++m) {
-        const int at = stream * kMine + m, d = 16 * (pass * kColumns + at) + 4 * quarter;
-        floatx4 x;
+      for (int i = 0; i < WK; ++i) f[b][i] *= inv;
+    }
+  }
+#pragma unroll
+  for (int pass = 0; pass < W::kPasses; ++pass) {
+    if (WK > 1 && pass) {
+      bare_barrier();
+      give(pass);
+    }
+#pragma unroll
+    for (int m = 0; m < kMine; ++m)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int at = stream * kMine + m, d = 16 * (pass * kColumns + at);
+        floatx4 x = floatx4{};
         if constexpr (WK > 1) {
-          x = floatx4{};
 #pragma unroll
-          for (int i = 0; i < WK; ++i) x += room[((i * NB + b) * kColumns + at) * kWave + lane] * f[i];
+          for (int i = 0; i < WK; ++i)
+            x = __builtin_elementwise_fma(room[((i * NB + b) * kColumns + at) * kWave + lane], floatx4{f[b][i], f[b][i], f[b][i], f[b][i]}, x);
         } else {
-          x = o[b][pass * kColumns + m];
+          x = o[b][pass * kColumns + m] * f[b][0];
         }
-        if (!w.there) continue;
-        if (part) {
-          *reinterpret_cast<floatx4 *>(&part->o[r][d]) = x;
-          continue;
-        }
-        if (d >= a.D) continue;
-        // a row without a score above -infinity is zeros, also where a value was NaN
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = all == 0.f ? 0.f : x[i] * inv;
-        if constexpr (sizeof(T) == 2) {
-          *reinterpret_cast<u32x2 *>(out + d) = u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{x[0], x[1]}), bf16x2)),
-                                                      __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{x[2], x[3]}), bf16x2))};
+        if (zero[b]) x = floatx4{};
+        if (!there[b] || (!part && d + 4 * quarter >= a.D)) continue;
+        if (part || sizeof(T) == 4) {
+          *reinterpret_cast<floatx4 *>(to[b] + d * 4) = x;
         } else {
-          *reinterpret_cast<floatx4 *>(out + d) = x;
+          *reinterpret_cast<u32x2 *>(to[b] + d * 2) = u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{x[0], x[1]}), bf16x2)),
+                                                            __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{x[2], x[3]}), bf16x2))};
         }
       }
-    }
   }
 }
 
