@@ -226,39 +226,37 @@ __device__ __forceinline__ float quad_sum(float x) {
   return pair_sum(__uint_as_float(p[0]) + __uint_as_float(p[1]));
 }
 
-// NB blocks of 16 rows a wave, WK streams of keys, 4 / WK waves on other rows.
-template <typename T, int DP, int NB, int WK>
+// NB blocks of 16 rows; every wave has all of them and a stream of keys.
+template <typename T, int DP, int NB>
 struct Work4 {
   static constexpr int NP = sizeof(T) == 2 ? 1 : 3; // bfloat16 numbers that make one of T
-  static constexpr int WR = kAttendWaves / WK, R = 16 * NB * WR, TK = Codes<DP>::KEYS * WK;
+  static constexpr int R = 16 * NB, TK = Codes<DP>::KEYS * kAttendWaves;
   static constexpr int kWaveLds = Codes<DP>::kStage + Codes<DP>::kRest;
-  static constexpr int kQueries = NB * Codes<DP>::NQ * NP * 1024;                 // of a wave
+  static constexpr int kQueries = NB * Codes<DP>::NQ * NP * 1024;                 
   // passes of the streams' joining, what its outputs take, and with the references and sums
-  static constexpr int kPasses = NB * DP > 192 ? 2 : 1, kRows = WK > 1 ? kAttendWaves * NB * DP / 16 / kPasses * 1024 : 0;
-  static constexpr int kJoining = WK > 1 ? kRows + kAttendWaves * NB * 16 * 8 : 0;
-  static constexpr int kLds = std::max(kAttendWaves * kWaveLds + WR * kQueries, kJoining);
+  static constexpr int kPasses = NB * DP > 192 ? 2 : 1, kRows = kAttendWaves * NB * DP / 16 / kPasses * 1024;
+  static constexpr int kLds = std::max(kAttendWaves * kWaveLds + kQueries, kRows + kAttendWaves * R * 8);
   // workgroups a CU: as many as find registers, and LDS
   static constexpr int kGroups = std::min(NB == 1 ? (DP == 64 ? 5 : 4) : NB == 2 && DP == 64 ? 3 : 2, 160 * 1024 / kLds);
   static constexpr int kRuns = kGroups * kCUs, kLeast = 1, kCost = 3;
 };
 
-template <typename T, int DP, int NB, int WK, int PAGES>
+template <typename T, int DP, int NB, int PAGES>
 __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u, int32_t tile, int32_t tiles, unsigned char *lds,
-                                            Part<DP, Work4<T, DP, NB, WK>::R> *part) {
+                                            Part<DP, Work4<T, DP, NB>::R> *part) {
   using C = Codes<DP>;
-  using W = Work4<T, DP, NB, WK>;
+  using W = Work4<T, DP, NB>;
   constexpr int NP = W::NP;
   int tid = threadIdx.x;
   asm("" : "+v"(tid));                  // what follows from it is formed here, not kept in registers from piece to piece
-  const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & (kWave - 1), stream = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, quarter = lane >> 4;
-  const int block = wave % W::WR * 16 * NB, stream = wave / W::WR;
-  unsigned char *const mine = lds + wave * W::kWaveLds;
+  unsigned char *const mine = lds + stream * W::kWaveLds;
   float *const scale = reinterpret_cast<float *>(mine + C::kStage);
-  unsigned char *const queries = lds + kAttendWaves * W::kWaveLds + wave % W::WR * W::kQueries + lane * 16;
-  // the positions of this wave's first and last row, and the keys that its rows see
-  const int32_t last = min(u.r0 + block + 16 * NB, u.rows) - 1;
-  const int32_t pos_first = u.ctx + (u.r0 + block) / a.G, pos_last = last >= u.r0 + block ? u.ctx + last / a.G : -1;
+  unsigned char *const queries = lds + kAttendWaves * W::kWaveLds + lane * 16;
+  // the positions of the first and the last row, and the keys of this wave's stream that they see
+  const int32_t last = min(u.r0 + W::R, u.rows) - 1;
+  const int32_t pos_first = u.ctx + u.r0 / a.G, pos_last = u.ctx + last / a.G;
   const int32_t lo_last = a.window > 0 ? pos_last - a.window : -1;
   const int32_t begin = u.k_lo + tile * W::TK + stream * C::KEYS;
   const int32_t end = min(min(u.k_hi, u.k_lo + (tile + tiles) * W::TK), pos_last + 1);
@@ -270,7 +268,7 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
   u32x4 q[NB][C::NQ][sizeof(T) / 2];
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    const Row w = row_at(a, u, u.r0 + block + 16 * b + l16);
+    const Row w = row_at(a, u, u.r0 + 16 * b + l16);
     pos[b] = w.pos;
     if (stream > 0) continue;
     const T *from = reinterpret_cast<const T *>(a.q) + w.token * a.q_tok + w.head * a.q_head;
@@ -322,6 +320,14 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
 #pragma nounroll
   for (int32_t n = 0; n < stages; ++n) {
     const bool more = n + 1 < stages;
+    // A CU's two workgroups have precedence by turns, four stages each.  Without turns the older one always has it, and the younger one ends
+    // alone, with half of the waves: after 59 and 80 us where 2 requests have 120000 keys.  With turns such a call takes 74 instead of 77 us, 8
+    // prompts' pieces of up to 1024 tokens behind 8000 keys 305 instead of 317, 64 requests of 9 tokens and up to 2000 keys 48.5 instead of 49.8.
+    // Turns of 2 to 16 stages measure within 2% of these.  One block of 16 rows, whose time is its codes', takes no turns: 127.3 for 126.0.
+    if constexpr (NB > 1) {
+      if ((n / 4 ^ (int) (blockIdx.x / kCUs)) & 1) __builtin_amdgcn_s_setprio(1);
+      else __builtin_amdgcn_s_setprio(0);
+    }
     wait_vm<C::NI>();                   // keys and scales are in, values may be on their way
     const unsigned char *const kl = mine, *const vl = kl + C::kBytes;
     // All codes of keys into registers, so that those of another stage may come into their place.
@@ -497,16 +503,14 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
 
   // The streams' rows: outputs go to LDS in passes, and every wave joins and stores some columns of all of them.
   bare_barrier();
-  constexpr int kColumns = C::NM / W::kPasses, kMine = kColumns / WK;       // blocks of 16 of a pass, and of a wave
+  constexpr int kColumns = C::NM / W::kPasses, kMine = kColumns / kAttendWaves;       // blocks of 16 of a pass, and of a wave
   static_assert(kMine >= 1, "");
-  floatx4 *const room = reinterpret_cast<floatx4 *>(lds) + wave % W::WR * (WK * NB * kColumns * kWave);
-  floatx2 *const sums = reinterpret_cast<floatx2 *>(lds + W::kRows) + wave % W::WR * (WK * NB * 16);
-  if constexpr (WK > 1) {
+  floatx4 *const room = reinterpret_cast<floatx4 *>(lds);
+  floatx2 *const sums = reinterpret_cast<floatx2 *>(lds + W::kRows);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const float all = quad_sum(sum[b]);
-      if (quarter == 0) sums[(stream * NB + b) * 16 + l16] = floatx2{ref[b], all};
-    }
+  for (int b = 0; b < NB; ++b) {
+    const float all = quad_sum(sum[b]);
+    if (quarter == 0) sums[(stream * NB + b) * 16 + l16] = floatx2{ref[b], all};
   }
   auto give = [&](int pass) {
 #pragma unroll
@@ -515,34 +519,28 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
       for (int m = 0; m < kColumns; ++m) room[((stream * NB + b) * kColumns + m) * kWave + lane] = o[b][pass * kColumns + m];
     bare_barrier();
   };
-  if constexpr (WK > 1) give(0);
+  give(0);
   // Where each row's outputs go, and what the streams' are to be multiplied by; a row without a score above -infinity is zeros, also where a value
   // was NaN.
-  float f[NB][WK];
+  float f[NB][kAttendWaves];
   char *to[NB];
   bool there[NB], zero[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    int32_t r = block + 16 * b + l16;
+    int32_t r = 16 * b + l16;
     asm("" : "+v"(r));                  // formed here, not kept in registers since the beginning
     const Row w = row_at(a, u, u.r0 + r);
     there[b] = w.there;
-    float now = ref[b], all = 0.f;
-    f[b][0] = 1.f;
-    if constexpr (WK > 1) {
-      floatx2 of[WK];
+    floatx2 of[kAttendWaves];
 #pragma unroll
-      for (int i = 0; i < WK; ++i) of[i] = sums[(i * NB + b) * 16 + l16];
-      now = of[0][0];
+    for (int i = 0; i < kAttendWaves; ++i) of[i] = sums[(i * NB + b) * 16 + l16];
+    float now = of[0][0], all = 0.f;
 #pragma unroll
-      for (int i = 1; i < WK; ++i) now = fmaxf(now, of[i][0]);
+    for (int i = 1; i < kAttendWaves; ++i) now = fmaxf(now, of[i][0]);
 #pragma unroll
-      for (int i = 0; i < WK; ++i) {
-        f[b][i] = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of[i][0] - now);
-        all = fmaf(f[b][i], of[i][1], all);
-      }
-    } else {
-      all = quad_sum(sum[b]);
+    for (int i = 0; i < kAttendWaves; ++i) {
+      f[b][i] = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of[i][0] - now);
+      all = fmaf(f[b][i], of[i][1], all);
     }
     zero[b] = !part && all == 0.f;
     if (part) {
@@ -555,12 +553,12 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
       to[b] = reinterpret_cast<char *>(reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head + 4 * quarter);
       const float inv = 1.f / all;
 #pragma unroll
-      for (int i = 0; i < WK; ++i) f[b][i] *= inv;
+      for (int i = 0; i < kAttendWaves; ++i) f[b][i] *= inv;
     }
   }
 #pragma unroll
   for (int pass = 0; pass < W::kPasses; ++pass) {
-    if (WK > 1 && pass) {
+    if (pass) {
       bare_barrier();
       give(pass);
     }
@@ -570,13 +568,9 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
       for (int b = 0; b < NB; ++b) {
         const int at = stream * kMine + m, d = 16 * (pass * kColumns + at);
         floatx4 x = floatx4{};
-        if constexpr (WK > 1) {
 #pragma unroll
-          for (int i = 0; i < WK; ++i)
-            x = __builtin_elementwise_fma(room[((i * NB + b) * kColumns + at) * kWave + lane], floatx4{f[b][i], f[b][i], f[b][i], f[b][i]}, x);
-        } else {
-          x = o[b][pass * kColumns + m] * f[b][0];
-        }
+        for (int i = 0; i < kAttendWaves; ++i)
+          x = __builtin_elementwise_fma(room[((i * NB + b) * kColumns + at) * kWave + lane], floatx4{f[b][i], f[b][i], f[b][i], f[b][i]}, x);
         if (zero[b]) x = floatx4{};
         if (!there[b] || (!part && d + 4 * quarter >= a.D)) continue;
         if (part || sizeof(T) == 4) {
@@ -589,10 +583,10 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
   }
 }
 
-template <typename T, int DP, int NB, int WK, int PAGES>
-__global__ __launch_bounds__(kAttendThreads, (Work4<T, DP, NB, WK>::kGroups)) void attend4_kernel(Attend4Args a, Join *join,
-                                                                                              Part<DP, Work4<T, DP, NB, WK>::R> *parts) {
-  using W = Work4<T, DP, NB, WK>;
+template <typename T, int DP, int NB, int PAGES>
+__global__ __launch_bounds__(kAttendThreads, (Work4<T, DP, NB>::kGroups)) void attend4_kernel(Attend4Args a, Join *join,
+                                                                                              Part<DP, Work4<T, DP, NB>::R> *parts) {
+  using W = Work4<T, DP, NB>;
   __shared__ __align__(16) unsigned char lds[W::kLds];
   // Where heads lie closer together than a head's keys, two workgroups on one XCD (8 blocks apart) work through the keys of two neighbours at
   // the same time: memory is read in pieces of 128 bytes, or of 64 that are neighbours.
@@ -610,7 +604,7 @@ __global__ __launch_bounds__(kAttendThreads, (Work4<T, DP, NB, WK>::kGroups)) vo
                                                                   [&](const Unit &unit, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
     Unit u = unit;
     u.head = deal.first + u.head * deal.step;
-    codes_piece<T, DP, NB, WK, PAGES>(a, u, tile, tiles, lds, part);
+    codes_piece<T, DP, NB, PAGES>(a, u, tile, tiles, lds, part);
   });
 }
 
@@ -619,53 +613,45 @@ __global__ __launch_bounds__(kJoinThreads) void attend4_join_kernel(AttendArgs a
   join_parts<T, DP, R>(a, join, parts);
 }
 
-template <typename T, int DP, int NB, int WK>
+template <typename T, int DP, int NB>
 hipError_t go(const Attend4Args &a, void *workspace, hipStream_t stream) {
-  using W = Work4<T, DP, NB, WK>;
+  using W = Work4<T, DP, NB>;
   Join *join = reinterpret_cast<Join *>(workspace);
   Part<DP, W::R> *parts = reinterpret_cast<Part<DP, W::R> *>(reinterpret_cast<char *>(workspace) + join_bytes(W::kRuns));
   // 16 keys share a page, and their codes and scales lie within 32 bits of each other
-  if (a.page_size % 16 == 0 && a.k_tok < (int64_t) 1 << 27 && a.s_tok < (int64_t) 1 << 25) attend4_kernel<T, DP, NB, WK, 1><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
-  else attend4_kernel<T, DP, NB, WK, 2><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
+  if (a.page_size % 16 == 0 && a.k_tok < (int64_t) 1 << 27 && a.s_tok < (int64_t) 1 << 25) attend4_kernel<T, DP, NB, 1><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
+  else attend4_kernel<T, DP, NB, 2><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  attend4_join_kernel<T, DP, W::R><<<dim3(W::kRuns, W::R >= 128 ? 8 : W::R / 4), kJoinThreads, 0, stream>>>(a, join, parts);
+  attend4_join_kernel<T, DP, W::R><<<dim3(W::kRuns, W::R / 4), kJoinThreads, 0, stream>>>(a, join, parts);
   return hipGetLastError();
 }
 
-// Calls f(T, NB, WK) as they fit `rows`: rows of a shared head of the longest request.
-template <int DP, bool BF16, typename F>
+// Calls f(NB) as it fits `rows`: rows of a shared head of the longest request.  bfloat16 takes the blocks of 16 that leave the fewest rows empty up
+// to 48, and afterwards three unless two need no more passes over the keys.  32 requests of 4000 keys, 8 shared heads of 128, NB = 1, 2, 3, us:
+// 4 to 16 rows 36, 42, 54; 20 to 32 52, 44, 56; 36 to 48 80, 60, 58; 52 to 64 76, 63, 81; 68 to 96 119, 96, 79; 97 to 128 145, 108, 128; 132 195,
+// 145, 129; 256 256, 208, 215.  float32 has one: queries and weights of two take more registers than there are.
+template <bool BF16, typename F>
 auto by_rows(int64_t rows, F f) {
   using std::integral_constant;
-  auto at = [&](auto nb, auto wk) { return f(nb, wk); };
-#define PCG_ROWS(NB, WK) at(integral_constant<int, NB>(), integral_constant<int, WK>())
-  if (rows <= 16) return PCG_ROWS(1, 4);
   if constexpr (BF16) {
-    if (rows <= 32) return PCG_ROWS(2, 4);
-    if (rows <= 48) return PCG_ROWS(3, 4);
-    if (rows <= 64) return PCG_ROWS(2, 2);
-    if (rows > 96 && rows <= 128) return PCG_ROWS(2, 1);
-    return PCG_ROWS(3, 2);
-  } else {
-    return PCG_ROWS(1, 2);
+    if (rows > 16 && (rows <= 32 || (rows > 48 && rows <= 64) || (rows > 96 && rows <= 128))) return f(integral_constant<int, 2>());
+    if (rows > 32) return f(integral_constant<int, 3>());
   }
-#undef PCG_ROWS
+  return f(integral_constant<int, 1>());
 }
 
 template <int DP, bool BF16>
 size_t bytes(int64_t rows) {
-  return by_rows<DP, BF16>(rows, [](auto nb, auto wk) {
-    using T = std::conditional_t<BF16, uint16_t, float>;
-    using W = Work4<T, DP, decltype(nb)::value, decltype(wk)::value>;
-    return parts_bytes<T, DP, W::R>(W::kRuns);
+  return by_rows<BF16>(rows, [](auto nb) {
+    using W = Work4<std::conditional_t<BF16, uint16_t, float>, DP, decltype(nb)::value>;
+    return parts_bytes<std::conditional_t<BF16, uint16_t, float>, DP, W::R>(W::kRuns);
   });
 }
 
 template <typename T, int DP>
 hipError_t go_rows(const Attend4Args &a, int64_t longest, void *workspace, hipStream_t stream) {
-  return by_rows<DP, sizeof(T) == 2>(longest * a.G, [&](auto nb, auto wk) {
-    return go<T, DP, decltype(nb)::value, decltype(wk)::value>(a, workspace, stream);
-  });
+  return by_rows<sizeof(T) == 2>(longest * a.G, [&](auto nb) { return go<T, DP, decltype(nb)::value>(a, workspace, stream); });
 }
 
 }  // namespace
