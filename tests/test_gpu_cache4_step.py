@@ -249,9 +249,9 @@ def test_two_recorded_calls_share_a_workspace(dtype):
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             call(out)
-        jobs.append((graph, out, out.clone()))
+        jobs.append((graph, out, out.clone(), call))       # a replay reads what the call was made with
     for order in ((0, 1), (1, 0), (0, 0), (1, 1)):
-        for _, out, _ in jobs:
+        for _, out, _, _ in jobs:
             out.zero_()
         for j in order:
             jobs[j][0].replay()
