@@ -7,9 +7,15 @@
 // bfloat16 numbers each, which hold all of their 24 bits: three products of the fast kind, exact in every term, where one of float32
 // takes sixteen times as long.
 //
-// Every wave has up to 48 rows, in blocks of 16 that share decoded keys and values, and a stream of keys of its own, which it brings into its own
-// part of LDS ahead of their use: nothing is shared in the loop, and no wave waits for another one in it.  Rows, units, runs and parts are those
-// of pcg_attend.hip.
+// The four waves of a workgroup have the same rows, one to three blocks of 16 that share decoded keys and values, and a stream of keys each, which
+// a wave brings into its own part of LDS ahead of their use: nothing is shared in the loop, and no wave waits for another one in it.  The
+// streams are joined at a piece's end.  Rows, units, runs and parts are those of pcg_attend.hip.
+//
+// What bounds it (bf16, 32 / 8 heads of 128; first kernel, then the joining of parts).  One block: memory, 128 requests of 3800 keys on average
+// 112 to 119 + 5 us for 509 MB, 4.5 TB/s.  Three blocks: issue.  A stage of 64 keys is 96 products, 48 exponentials, 128 conversions of codes and
+// about 300 other vector instructions, which add up on a SIMD: 1.5 us at 2.35 GHz, 2.1 at the 1.6 that the chip holds with all CUs busy.
+// 64 requests of 1260 keys with 9 tokens 43 to 45 + 6.7 us, 2 requests of 115000 72 + 8, pieces of prompts, 2844 tokens, 330 + 9 one at a time and
+// 306 in a row (696 TFLOP/s).  Few keys: waits one after the other, the run, the pages, the first keys, the joining: 1 request of 1500 keys 8.4 + 3.5.
 #include <algorithm>
 #include <type_traits>
 
@@ -232,7 +238,7 @@ struct Work4 {
   static constexpr int NP = sizeof(T) == 2 ? 1 : 3; // bfloat16 numbers that make one of T
   static constexpr int R = 16 * NB, TK = Codes<DP>::KEYS * kAttendWaves;
   static constexpr int kWaveLds = Codes<DP>::kStage + Codes<DP>::kRest;
-  static constexpr int kQueries = NB * Codes<DP>::NQ * NP * 1024;                 
+  static constexpr int kQueries = NB * Codes<DP>::NQ * NP * 1024;
   // passes of the streams' joining, what its outputs take, and with the references and sums
   static constexpr int kPasses = NB * DP > 192 ? 2 : 1, kRows = kAttendWaves * NB * DP / 16 / kPasses * 1024;
   static constexpr int kLds = std::max(kAttendWaves * kWaveLds + kQueries, kRows + kAttendWaves * R * 8);
@@ -593,7 +599,7 @@ __global__ __launch_bounds__(kAttendThreads, (Work4<T, DP, NB>::kGroups)) void a
   using W = Work4<T, DP, NB>;
   __shared__ __align__(16) unsigned char lds[W::kLds];
   // Where heads lie closer together than a head's keys, two workgroups on one XCD (8 blocks apart) work through the keys of two neighbours at
-  // the same time: memory is read in pieces of 128 bytes, or of 64 that are neighbours.
+  // the same time: memory is read in pieces of 128 bytes, or of 64 that are neighbours (128 requests of 3800 keys 118 us, 185 without).
   Heads deal = all_heads(a);
   if (a.pairs) {
     deal.first = (int32_t) (deal.block / 8 % 2);
@@ -612,6 +618,8 @@ __global__ __launch_bounds__(kAttendThreads, (Work4<T, DP, NB>::kGroups)) void a
   });
 }
 
+// Joins the parts of units that runs cut: as many reads as there are parts, a few microseconds in a launch of its own (3.5 us where there is next
+// to nothing, 6.7 for the parts of 512 runs of 36 rows, 19 MB).
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(kJoinThreads) void attend4_join_kernel(AttendArgs a, const Join *join, const Part<DP, R> *parts) {
   join_parts<T, DP, R>(a, join, parts);
@@ -622,8 +630,10 @@ hipError_t go(const Attend4Args &a, void *workspace, hipStream_t stream) {
   using W = Work4<T, DP, NB>;
   Join *join = reinterpret_cast<Join *>(workspace);
   Part<DP, W::R> *parts = reinterpret_cast<Part<DP, W::R> *>(reinterpret_cast<char *>(workspace) + join_bytes(W::kRuns));
-  // 16 keys share a page, and their codes and scales lie within 32 bits of each other
-  if (a.page_size % 16 == 0 && a.k_tok < (int64_t) 1 << 27 && a.s_tok < (int64_t) 1 << 25) attend4_kernel<T, DP, NB, 1><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
+  // Places by groups of 16 keys where these share a page and lie within 32 bits of each other: pieces of prompts 306 us, 338 with places key by
+  // key; 2 requests of 115000 keys 77 and 84, 64 of 1260 48.6 and 50.2.
+  if (a.page_size % 16 == 0 && a.k_tok < (int64_t) 1 << 27 && a.s_tok < (int64_t) 1 << 25)
+    attend4_kernel<T, DP, NB, 1><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
   else attend4_kernel<T, DP, NB, 2><<<W::kRuns, kAttendThreads, 0, stream>>>(a, join, parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
