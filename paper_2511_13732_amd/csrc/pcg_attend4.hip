@@ -408,7 +408,8 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
       asm("" : "+v"(l));                // formed here, not kept in registers
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const int32_t to = pos[b] - k - (l >> 4) * 16, first = a.window > 0 ? to - a.window + 1 : 0;      // first <= 4 t + i <= to is seen
+        // first <= 4 t + i <= to is seen; a window may be as long as numbers go
+        const int32_t here = k + (l >> 4) * 16, to = pos[b] - here, first = a.window > 0 ? max(pos[b] - a.window, -1) + 1 - here : 0;
         const uint32_t count = (uint32_t) max(to - first + 1, 0);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {

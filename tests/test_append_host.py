@@ -183,6 +183,36 @@ def test_tensors_that_do_not_fit_are_refused():
             pcg.cache4_attend(four, **{**good, **bad})
 
 
+def test_objects_whose_fields_are_replaced_name_the_new_ones():
+    new = lambda n, dtype=torch.uint8: torch.zeros((4, 16, 2, n), dtype=dtype)  # noqa: E731
+    cache = pcg.KvCache4(new(32), new(32), new(2, torch.bfloat16), 64)
+    k, v, s = new(32), new(32), new(2, torch.bfloat16)
+    cache.k, cache.v, cache.scales = k, v, s
+    r = cache._ref.contents
+    assert (r.k, r.v, r.scales) == (k.data_ptr(), v.data_ptr(), s.data_ptr())
+    cache.head_dim = 40
+    assert cache._ref.contents.head_dim == 40
+    turn, table = pcg.Rotation(torch.zeros(9, 64)), torch.zeros(5, 32)
+    turn.table = table
+    turn.interleaved = True
+    r = turn._ref.contents
+    assert (r.table, r.positions, r.dim, r.interleaved) == (table.data_ptr(), 5, 32, 1) and (turn.positions, turn.dim) == (5, 32)
+
+
+def test_sizes_that_the_library_would_take_for_others_are_refused():
+    """Beyond 2^31, on a device that holds no memory."""
+    far = 1 << 32
+    new = lambda *s, dtype=torch.uint8: torch.empty(s, dtype=dtype, device="meta")  # noqa: E731
+    for shape in ((far, 1, 1), (1, far, 1), (1, 1, far)):
+        with pytest.raises(ValueError):
+            pcg.KvCache4(new(*shape, 32), new(*shape, 32), new(*shape, 2, dtype=torch.bfloat16), 64)
+    with pytest.raises(ValueError):
+        pcg.KvCache4(new(1, 1, 1, far // 2), new(1, 1, 1, far // 2), new(1, 1, 1, 2, dtype=torch.bfloat16), far)
+    for shape in ((far, 2), (1, far)):
+        with pytest.raises(ValueError):
+            pcg.Rotation(new(*shape, dtype=torch.float32))
+
+
 # ------------------------------------------------------------------ the plain forms, by hand
 
 def test_plain_rotation_by_hand():

@@ -334,3 +334,17 @@ def test_pages_far_behind_each_other(four, page_size):
     lens, starts = (torch.tensor(x, dtype=torch.int32).cuda() for x in ([n - 3], [0, 3]))
     out = (pcg.cache4_attend if four else pcg.cache_attend)(cache, q_out[n - 3:], table, lens, starts, longest=3)
     (check if four else attention.check)(out, attention.attend_rows(q_out[n - 3:], kk, vv, n - 3, D ** -0.5), dt)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_windows_longer_than_any_request(dtype):
+    """As far as numbers of 32 bits go: what every row sees is what it sees without one, to the bit."""
+    dt, H, G, D = DTYPES[dtype], 8, 2, 64
+    ctx, new = [0, 700, 90], [40, 3, 12]
+    cache, table, _ = make_cache([c + n for c, n in zip(ctx, new)], 16, G, D, "heads", 9)
+    st = starts_of(new)
+    q = (1.5 * torch.randn((st[-1], H, D), generator=gen(1))).to(dt).cuda()
+    lens, starts = (torch.tensor(x, dtype=torch.int32).cuda() for x in (ctx, st))
+    want = pcg.cache4_attend(cache, q, table, lens, starts, longest=40)
+    for window in (703, (1 << 31) - 1, (1 << 31) - 2, (1 << 31) - 64, 1 << 30):
+        assert torch.equal(pcg.cache4_attend(cache, q, table, lens, starts, longest=40, window=window), want), window
