@@ -171,7 +171,7 @@ struct Counts {
 };
 
 // A part of a head a thread: queries (if any), keys, values.  Bound by memory: everything is read and written once, 16 bytes at a time, with
-// nothing between but four products in double a pair.  16 prompts of up to 2048 tokens, 3 x 16 heads of 64, float32, take 34.9 us for 182 MB, 5.2
+// nothing between but four products in double a pair.  16 prompts of up to 2048 tokens, 16 / 8 heads of 64, float32, take 34.9 us for 182 MB, 5.2
 // TB/s; 576 rows of a step 5.3 us, the waits for a slot, the row and the table's row.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Counts n, Deal<T> deal) {
