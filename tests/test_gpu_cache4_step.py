@@ -336,6 +336,30 @@ def test_pages_far_behind_each_other(four, page_size):
     (check if four else attention.check)(out, attention.attend_rows(q_out[n - 3:], kk, vv, n - 3, D ** -0.5), dt)
 
 
+@pytest.mark.parametrize("apart", [1 << 27, (1 << 27) - 16])
+def test_slots_far_behind_each_other(apart):
+    """Slots of a page so far from each other that 16 of them do not fit 32 bits, and just fit."""
+    dt, H, G, D, n, page_size = torch.bfloat16, 4, 2, 64, 40, 16
+    row = D // 2
+    room = torch.empty(3 * page_size * apart, dtype=torch.uint8, device="cuda")
+
+    def view(x, at, width, unit):
+        return x.as_strided((3, page_size, G, width), (page_size * apart // unit, apart // unit, row // unit, 1), at // unit)
+    cache = pcg.KvCache4(view(room, 0, row, 1), view(room, 1024, row, 1), view(room.view(torch.bfloat16), 2048, 2, 2), D)
+    table = torch.tensor([[2, 0, 1]], dtype=torch.int32).cuda()
+    at = torch.arange(n)
+    slots = (table[0].cpu().long()[at // page_size] * page_size + at % page_size).to(torch.int32).cuda()
+    rotation = pcg.Rotation.of(n, D, "cuda")
+    q, k, v = (torch.randn((n, h, D), generator=gen(i)).to(dt).cuda() for i, h in enumerate((H, G, G)))
+    q_out = pcg.cache4_append(cache, k, v, slots, rotation=rotation, positions=at.to(torch.int32).cuda(), q=q)
+    kk, vv = (ref.values(*ref.quantise(x)) for x in (ref.rotate(k, rotation.table.cpu(), False), v.cpu().float()))
+    for got, x in zip(pcg.cache4_read(cache, slots, dtype=torch.float32), (kk, vv)):
+        assert torch.equal(got.cpu().double(), x)
+    lens, starts = (torch.tensor(x, dtype=torch.int32).cuda() for x in ([n - 3], [0, 3]))
+    out = pcg.cache4_attend(cache, q_out[n - 3:], table, lens, starts, longest=3)
+    check(out, attention.attend_rows(q_out[n - 3:], kk, vv, n - 3, D ** -0.5), dt)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_windows_longer_than_any_request(dtype):
     """As far as numbers of 32 bits go: what every row sees is what it sees without one, to the bit."""
