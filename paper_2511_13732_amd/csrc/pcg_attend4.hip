@@ -246,9 +246,11 @@ struct Work4 {
   // less on its way from memory, and LDS has room for three of float32 and 128 elements.  us with 2, 3, 4, 5, at 128 requests of 4000 keys, 8
   // shared heads, 4 rows: bf16 of 64 elements 63, 64, 63, 67, of 128 106, 115, 107, 107 (32 requests 33, 36, 37, 37); float32 of 64 84, 80, 69, 76.
   static constexpr int kGroups = std::min(NB == 1 ? (DP == 64 ? 4 : NP == 1 ? 2 : 3) : NB == 2 && DP == 64 ? 3 : 2, 160 * 1024 / kLds);
-  // What a unit's beginning and end cost, in tiles of 256 keys.  us with 1, 3, 5: 32 requests of 3500 keys, 12 heads, float32, 26.7, 28.8, 30.9;
-  // 128 of 6000, one token, 123.5, 126.3, 126.5; 64 of 2000, 9 tokens (three blocks) 51.6, 48.4, 47.4; pieces of prompts 305 with 3, 316 with 5.
-  static constexpr int kRuns = kGroups * kCUs, kLeast = 1, kCost = NB == 1 ? 1 : 3;
+  // What a unit's beginning and end cost, in tiles of 256 keys.  One block, us with 1, 3, 5: 32 requests of 3500 keys, 12 heads, float32, 26.7, 28.8,
+  // 30.9; 128 of 6000, one token, 123.5, 126.3, 126.5.  More blocks, with 1, 2, 3, 4, 6: 64 requests of 2000 keys and 9 tokens 51.6, 48.9, 48.5, 48.5,
+  // 47.4; with 2, 3, 4, 6: pieces of prompts 303, 306, 310, 321; requests of up to 1000, 2000 and 4000 keys (128, 8, 32), 64 rows a head 77.5, 81.1,
+  // 82.7, 82.1, 21.9, 24.0, 24.3, 23.4 and 54.1, 55.7, 53.6, 56.6.
+  static constexpr int kRuns = kGroups * kCUs, kLeast = 1, kCost = NB == 1 ? 1 : 2;
 };
 
 template <typename T, int DP, int NB, int PAGES>
