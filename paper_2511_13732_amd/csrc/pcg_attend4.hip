@@ -39,6 +39,23 @@ __device__ __forceinline__ void bring_four(const char *const (&base)[4], const u
                "{m0}"(lds_address(to)) : "memory");
 }
 
+// The kernel's first argument as it lies in memory: what is read of it behind such a call is read there and not kept in scalar registers
+// since the beginning, which the loop over stages has too few of (pieces of prompts 302 us with arguments kept, 295 with those of a piece's beginning
+// and end read there, 290 with those of the loop apart as well).
+__device__ __forceinline__ const Attend4Args &arguments() {
+  typedef const Attend4Args __attribute__((address_space(4))) Args;
+  Args *p = (Args *) __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const Attend4Args *) p;
+}
+
+// A number on its own, not as the part of a group that it was loaded with.
+template <typename X>
+__device__ __forceinline__ X apart(X x) {
+  asm("" : "+s"(x));
+  return x;
+}
+
 template <int DP>
 struct Codes {
   static constexpr int RB = DP / 2;                 // bytes of a key
@@ -85,6 +102,7 @@ struct Loader4 {
   int64_t codes, scales;      // where this lane's group or key lies
   uint64_t there;             // lanes whose group or key there is
   int64_t next;               // scales of this lane's key of the next stage
+  const uint32_t scale_off;   // from the first key of a group to this lane's
 
   __device__ __forceinline__ int row_of(int i) const { return i * C::RPI + lane / C::CH; }
   __device__ __forceinline__ int chunk(int row) const {
@@ -92,7 +110,8 @@ struct Loader4 {
     return ch * 32 < a.D ? ch * 16 : 0;
   }
   __device__ __forceinline__ Loader4(const Attend4Args &a_, const Unit &u_, int lane_, int32_t begin_, int32_t step_, unsigned char *ids_)
-      : a(a_), u(u_), lane(lane_), begin(begin_), step(step_), ids(ids_), table(a_.table + (int64_t) u_.b * a_.table_stride) {
+      : a(a_), u(u_), lane(lane_), begin(begin_), step(step_), ids(ids_), table(a_.table + (int64_t) u_.b * a_.table_stride),
+        scale_off((uint32_t) (lane_ & 15) * (uint32_t) a_.s_tok * 4) {
     kb = reinterpret_cast<const char *>(a.k) + (int64_t) u.head * a.k_head;
     vb = reinterpret_cast<const char *>(a.v) + (int64_t) u.head * a.k_head;
     sb = reinterpret_cast<const char *>(a.scales + (int64_t) u.head * a.s_head);
@@ -129,7 +148,7 @@ struct Loader4 {
 
   // Those of the key lane of the stage whose groups begin with g0.
   __device__ __forceinline__ void find_scales(int g0, int lane) {
-    next = lane_value(scales, g0 + lane / 16) + (uint32_t) (lane & 15) * (uint32_t) a.s_tok * 4;
+    next = lane_value(scales, g0 + lane / 16) + scale_off;
   }
 
   // Codes and scales of the keys of stage n (stages come in order), or afterwards the codes of its values.
@@ -329,6 +348,15 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
     ref[b] = -INFINITY;
     sum[b] = 0.f;
   }
+  // Arguments that the loop uses, each for itself: the arguments as a whole do not find scalar registers, and come back in groups of eight.
+  const int32_t head_dim = apart(a.D), window = apart(a.window);
+  const float score = apart(a.c);
+  // compared where it is used: the results of all comparisons would be kept
+  auto columns = [&] {
+    int32_t d = head_dim;
+    asm("" : "+s"(d));
+    return d;
+  };
 #pragma nounroll
   for (int32_t n = 0; n < stages; ++n) {
     const bool more = n + 1 < stages;
@@ -371,7 +399,7 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
     // scales as float32, those of keys with c; what is not finite is NaN, whatever the codes
     {
       const float x = __uint_as_float(both << 16), y = __uint_as_float(both & 0xffff0000u);
-      scale[lane] = fmaf(x, 0.f, x) * a.c;
+      scale[lane] = fmaf(x, 0.f, x) * score;
       scale[C::KEYS + lane] = fmaf(y, 0.f, y);
     }
     floatx4 s[NB][4];
@@ -411,7 +439,7 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         // first <= 4 t + i <= to is seen; a window may be as long as numbers go
-        const int32_t here = k + (l >> 4) * 16, to = pos[b] - here, first = a.window > 0 ? max(pos[b] - a.window, -1) + 1 - here : 0;
+        const int32_t here = k + (l >> 4) * 16, to = pos[b] - here, first = window > 0 ? max(pos[b] - window, -1) + 1 - here : 0;
         const uint32_t count = (uint32_t) max(to - first + 1, 0);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -499,7 +527,7 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
     // two blocks of columns at a time, so that products that add to the same sums do not follow each other
 #pragma unroll
     for (int m = 0; m < C::NM; m += 2) {
-      if (16 * m >= a.D) break;
+      if (16 * m >= columns()) break;
       pin();
 #pragma unroll
       for (int c = 0; c < 2; ++c)
@@ -514,6 +542,7 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
     }
   }
 
+  const Attend4Args &e = arguments();
   // The streams' rows: outputs go to LDS in passes, and every wave joins and stores some columns of all of them.
   bare_barrier();
   constexpr int kColumns = C::NM / W::kPasses, kMine = kColumns / kAttendWaves;       // blocks of 16 of a pass, and of a wave
@@ -542,7 +571,7 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
   for (int b = 0; b < NB; ++b) {
     int32_t r = 16 * b + l16;
     asm("" : "+v"(r));                  // formed here, not kept in registers since the beginning
-    const Row w = row_at(a, u, u.r0 + r);
+    const Row w = row_at(e, u, u.r0 + r);
     there[b] = w.there;
     floatx2 of[kAttendWaves];
 #pragma unroll
@@ -563,7 +592,7 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
         part->sum[r] = all;
       }
     } else {
-      to[b] = reinterpret_cast<char *>(reinterpret_cast<T *>(a.out) + w.token * a.o_tok + w.head * a.o_head + 4 * quarter);
+      to[b] = reinterpret_cast<char *>(reinterpret_cast<T *>(e.out) + w.token * e.o_tok + w.head * e.o_head + 4 * quarter);
       const float inv = 1.f / all;
 #pragma unroll
       for (int i = 0; i < kAttendWaves; ++i) f[b][i] *= inv;
@@ -585,7 +614,7 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
         for (int i = 0; i < kAttendWaves; ++i)
           x = __builtin_elementwise_fma(room[((i * NB + b) * kColumns + at) * kWave + lane], floatx4{f[b][i], f[b][i], f[b][i], f[b][i]}, x);
         if (zero[b]) x = floatx4{};
-        if (!there[b] || (!part && d + 4 * quarter >= a.D)) continue;
+        if (!there[b] || (!part && d + 4 * quarter >= e.D)) continue;
         if (part || sizeof(T) == 4) {
           *reinterpret_cast<floatx4 *>(to[b] + d * 4) = x;
         } else {
@@ -617,7 +646,7 @@ __global__ __launch_bounds__(kAttendThreads, (Work4<T, DP, NB>::kGroups)) void a
                                                                   [&](const Unit &unit, int32_t tile, int32_t tiles, Part<DP, W::R> *part) {
     Unit u = unit;
     u.head = deal.first + u.head * deal.step;
-    codes_piece<T, DP, NB, PAGES>(a, u, tile, tiles, lds, part);
+    codes_piece<T, DP, NB, PAGES>(arguments(), u, tile, tiles, lds, part);
   });
 }
 
