@@ -12,10 +12,10 @@
 // streams are joined at a piece's end.  Rows, units, runs and parts are those of pcg_attend.hip.
 //
 // What bounds it (bf16, 32 / 8 heads of 128; first kernel, then the joining of parts).  One block: memory, 128 requests of 3800 keys on average
-// 112 to 119 + 5 us for 509 MB, 4.5 TB/s.  Three blocks: issue.  A stage of 64 keys is 96 products, 48 exponentials, 128 conversions of codes and
-// about 300 other vector instructions, which add up on a SIMD: 1.5 us at 2.35 GHz, 2.1 at the 1.6 that the chip holds with all CUs busy.
-// 64 requests of 1260 keys with 9 tokens 43 to 45 + 6.7 us, 2 requests of 115000 72 + 8, pieces of prompts, 2844 tokens, 330 + 9 one at a time and
-// 306 in a row (696 TFLOP/s).  Few keys: waits one after the other, the run, the pages, the first keys, the joining: 1 request of 1500 keys 8.4 + 3.5.
+// 112 to 117 + 5 us for 509 MB, 4.5 TB/s.  Three blocks: issue.  A stage of 64 keys is 96 products, 48 exponentials, 128 conversions of codes and
+// about 300 other vector instructions, which add up on a SIMD: 1.55 us at 2.35 GHz, 2.2 at the 1.6 to 1.75 that the chip holds with all CUs busy.
+// 64 requests of 1260 keys with 9 tokens 43 to 44 + 6.7 us, 2 requests of 115000 69 + 9, pieces of prompts, 2844 tokens, 317 to 326 + 10 one at a
+// time and 290 in a row (734 TFLOP/s).  Few keys: waits one after the other, the run, the pages, the first keys, the joining: 1 request of 1500 keys 8.1 + 3.4.
 #include <algorithm>
 #include <type_traits>
 
