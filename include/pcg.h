@@ -665,7 +665,8 @@ int pcg_cache4_read(const pcg_kv4_cache *cache, pcg_dtype dt, void *k_out, int64
  * rounded to dt; with PCG_BF16 a weight times its value's scale is rounded to bfloat16 where it multiplies codes, with PCG_F32 all 24 bits of it and
  * of the queries are multiplied.  A value that is NaN makes all elements of its head NaN in the rows that see it.  A key's scale
  * times `scale` log2 e has to stay within float32.  Everything else as there.
- *   workspace     DEVICE, >= pcg_cache4_attend_workspace_bytes(B, T, heads, kv_heads, head_dim, longest)
+ *   workspace     DEVICE, >= pcg_cache4_attend_workspace_bytes(B, T, heads, kv_heads, head_dim, longest), which is
+ *                 the same for any B, T, heads and longest
  */
 int pcg_cache4_attend(const pcg_kv4_cache *cache, pcg_dtype dt, const void *q, int64_t q_tok_stride, int64_t q_head_stride,
                       int32_t heads, int64_t T, const int32_t *block_table, int64_t table_stride, int32_t max_blocks,

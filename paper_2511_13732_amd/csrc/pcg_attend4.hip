@@ -673,39 +673,40 @@ hipError_t go(const Attend4Args &a, void *workspace, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Calls f(NB) as it fits `rows`: rows of a shared head of the longest request.  bfloat16 takes the blocks of 16 that leave the fewest rows empty up
-// to 48, and afterwards three unless two need no more passes over the keys.  32 requests of 4000 keys, 8 shared heads of 128, NB = 1, 2, 3, us:
-// 4 to 16 rows 36, 42, 54; 20 to 32 52, 44, 56; 36 to 48 80, 60, 58; 52 to 64 76, 63, 81; 68 to 96 119, 96, 79; 97 to 128 145, 108, 128; 132 195,
-// 145, 129; 256 256, 208, 215.  float32 has one: queries and weights of two take more registers than there are.
+// Calls f(NB) as it fits `rows`: rows of a shared head of the longest request, of which there are `heads` in all requests.  bfloat16 takes the
+// blocks of 16 that leave the fewest rows empty up to 48, and afterwards three unless two need no more passes over the keys.  32 requests of 4000
+// keys, 8 shared heads of 128, NB = 1, 2, 3, us: 4 to 16 rows 36, 42, 54; 20 to 32 52, 44, 56; 36 to 48 80, 60, 58; 52 to 64 76, 63, 81; 68 to 96
+// 119, 96, 79; 97 to 128 145, 108, 128; 132 195, 145, 129; 256 256, 208, 215.  float32 has no registers for three, and two are fewer workgroups: they
+// pay where there is work for all.  NB = 1, 2, heads of 128, us: 32 requests of 4000 keys, 20 rows 68, 62, 48 rows 86, 96, 64 124, 98, 128 224, 180;
+// 8 of 2000, 20 rows 24, 26, 64 28, 33, 256 70, 67, 1024 224, 203.
 template <bool BF16, typename F>
-auto by_rows(int64_t rows, F f) {
+auto by_rows(int64_t rows, int64_t heads, F f) {
   using std::integral_constant;
   if constexpr (BF16) {
     if (rows > 16 && (rows <= 32 || (rows > 48 && rows <= 64) || (rows > 96 && rows <= 128))) return f(integral_constant<int, 2>());
     if (rows > 32) return f(integral_constant<int, 3>());
+  } else {
+    if (rows > 16 && (rows <= 32 || rows > 48) && heads * ((rows + 15) / 16) >= 2 * kCUs) return f(integral_constant<int, 2>());
   }
   return f(integral_constant<int, 1>());
 }
 
-template <int DP, bool BF16>
-size_t bytes(int64_t rows) {
-  return by_rows<BF16>(rows, [](auto nb) {
-    using W = Work4<std::conditional_t<BF16, uint16_t, float>, DP, decltype(nb)::value>;
-    return parts_bytes<std::conditional_t<BF16, uint16_t, float>, DP, W::R>(W::kRuns);
-  });
+template <typename T, int DP, int NB>
+size_t bytes() { return parts_bytes<T, DP, Work4<T, DP, NB>::R>(Work4<T, DP, NB>::kRuns); }
+// What any call takes, so that what is enough for the longest chunks and the most requests is enough for others.
+template <int DP>
+size_t most() {
+  return std::max({bytes<uint16_t, DP, 1>(), bytes<uint16_t, DP, 2>(), bytes<uint16_t, DP, 3>(), bytes<float, DP, 1>(), bytes<float, DP, 2>()});
 }
 
 template <typename T, int DP>
 hipError_t go_rows(const Attend4Args &a, int64_t longest, void *workspace, hipStream_t stream) {
-  return by_rows<sizeof(T) == 2>(longest * a.G, [&](auto nb) { return go<T, DP, decltype(nb)::value>(a, workspace, stream); });
+  return by_rows<sizeof(T) == 2>(longest * a.G, (int64_t) a.B * a.heads_kv, [&](auto nb) { return go<T, DP, decltype(nb)::value>(a, workspace, stream); });
 }
 
 }  // namespace
 
-size_t attend4_workspace_bytes(int32_t G, int32_t D, int64_t longest) {
-  const int64_t rows = longest * G;
-  return D <= 64 ? std::max(bytes<64, true>(rows), bytes<64, false>(rows)) : std::max(bytes<128, true>(rows), bytes<128, false>(rows));
-}
+size_t attend4_workspace_bytes(int32_t D) { return D <= 64 ? most<64>() : most<128>(); }
 
 hipError_t launch_cache4_attend(const Attend4Args &a, bool bf16, int64_t longest, void *workspace, hipStream_t stream) {
   if (bf16) return a.D <= 64 ? go_rows<uint16_t, 64>(a, longest, workspace, stream) : go_rows<uint16_t, 128>(a, longest, workspace, stream);

@@ -374,7 +374,7 @@ int pcg_cache_attend(const pcg_kv_cache *cache, const void *q, int64_t q_tok_str
 size_t pcg_cache4_attend_workspace_bytes(int32_t B, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                          int64_t longest) {
   if (B < 0 || T < 0 || longest < 0 || longest >= kInt31 || check_heads(heads, kv_heads, head_dim)) return 0;
-  return attend4_workspace_bytes(heads / kv_heads, head_dim, longest);
+  return attend4_workspace_bytes(head_dim);
 }
 
 int pcg_cache4_attend(const pcg_kv4_cache *cache, pcg_dtype dt, const void *q, int64_t q_tok_stride, int64_t q_head_stride,
@@ -390,7 +390,7 @@ int pcg_cache4_attend(const pcg_kv4_cache *cache, pcg_dtype dt, const void *q, i
                              window, out, out_tok_stride, out_head_stride))
     return rc;
   if (int rc = check_table(c.page_size, T, block_table, table_stride, max_blocks, lens, B, workspace, workspace_bytes,
-                           attend4_workspace_bytes(heads / c.kv_heads, c.head_dim, longest)))
+                           attend4_workspace_bytes(c.head_dim)))
     return rc;
   if (B == 0 || T == 0) return PCG_OK;
   a.k = c.k;

@@ -126,6 +126,8 @@ def test_the_workspace_is_what_the_helper_says():
     for longest in (2, 10, 20):
         need = pcg.cache4_attend_workspace_bytes(2, 4, 4, 2, 64, longest)
         assert need > 0 and attend4(wsb=need - 1, longest=longest) == WS_SMALL
+    # what is enough for one call is enough for smaller and larger ones
+    assert len({pcg.cache4_attend_workspace_bytes(B, 999, 8 * G, G, 128, longest) for B in (1, 300) for G in (1, 8) for longest in (1, 6, 8, 400)}) == 1
     for bad in ((-1, 4, 4, 2, 64, 2), (2, -4, 4, 2, 64, 2), (2, 4, 3, 2, 64, 2), (2, 4, 4, 2, 60, 2), (2, 4, 4, 2, 64, -2), (2, 4, 4, 2, 64, 1 << 31)):
         assert pcg.cache4_attend_workspace_bytes(*bad) == 0
 

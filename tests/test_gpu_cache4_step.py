@@ -372,3 +372,35 @@ def test_windows_longer_than_any_request(dtype):
     want = pcg.cache4_attend(cache, q, table, lens, starts, longest=40)
     for window in (703, (1 << 31) - 1, (1 << 31) - 2, (1 << 31) - 64, 1 << 30):
         assert torch.equal(pcg.cache4_attend(cache, q, table, lens, starts, longest=40, window=window), want), window
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("page_size,D,window", [(16, 128, 0), (7, 40, 0), (32, 64, 50), (5, 72, 70)])
+@pytest.mark.parametrize("longest", [10, 30])
+def test_many_shared_heads(dtype, page_size, D, window, longest):
+    """Work for the whole chip out of few requests, 20 and 60 rows a shared head at most."""
+    dt, H, G = DTYPES[dtype], 256, 128
+    ctx, new = [90, 0, 41, 130], [longest, 1, 9, longest - 2]
+    cache, table, rows = make_cache([c + n for c, n in zip(ctx, new)], page_size, G, D, "heads", D)
+    st = starts_of(new)
+    q = (1.5 * torch.randn((st[-1], H, D), generator=gen(2))).to(dt).cuda()
+    lens, starts = (torch.tensor(x, dtype=torch.int32).cuda() for x in (ctx, st))
+
+    def call():
+        return pcg.cache4_attend(cache, q, table, lens, starts, longest=longest, window=window)
+    out = call()
+    for b in range(4):
+        at = list(range(st[b], st[b + 1], 4)) + [st[b + 1] - 1]
+        for t in at:
+            check(out[t:t + 1], attention.attend_rows(q[t:t + 1], *rows[b], ctx[b] + t - st[b], D ** -0.5, window), dt, (b, t))
+    # the last token's key or value of one shared head is NaN: its own row's heads there are, and nothing else changes
+    for i, head in ((0, 5), (1, 127)):
+        j = ctx[3] + new[3] - 1
+        where = (int(table[3, j // page_size]), j % page_size, head, i)
+        was = cache.scales[where].clone()
+        cache.scales[where] = float("nan")
+        got = call()
+        struck = torch.zeros(got.shape, dtype=torch.bool, device="cuda")
+        struck[-1, 2 * head:2 * head + 2] = True
+        assert torch.isnan(got[struck]).all() and torch.equal(got[~struck], out[~struck])
+        cache.scales[where] = was
