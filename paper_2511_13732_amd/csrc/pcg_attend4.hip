@@ -543,7 +543,10 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
   }
 
   const Attend4Args &e = arguments();
-  // The streams' rows: outputs go to LDS in passes, and every wave joins and stores some columns of all of them.
+  // The streams' rows: outputs go to LDS in passes, and every wave joins and stores some columns of all of them.  They come where other
+  // waves' stages and pages were: nothing may be on its way into LDS any more.  The loop ends with such a wait; a wave without a stage has not
+  // been in it, and the pages that it asked for may not be in yet.
+  wait_vm<0>();
   bare_barrier();
   constexpr int kColumns = C::NM / W::kPasses, kMine = kColumns / kAttendWaves;       // blocks of 16 of a pass, and of a wave
   static_assert(kMine >= 1, "");
