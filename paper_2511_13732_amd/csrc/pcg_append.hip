@@ -212,13 +212,17 @@ __device__ __forceinline__ uint32_t max_of(uint32_t x) {
   return x;
 }
 
-// The scale of numbers whose largest absolute value has these bits: a sixth of it in bfloat16, at most what 6 times is finite of.  (A
-// float32 quotient by 6 never falls on the middle of two bfloat16 numbers unless the exact one does, so that rounding it again is
-// rounding once.)  NaN where a number is not finite: its bits are then at least those of infinity.
+// The scale of numbers whose largest absolute value has these bits: a sixth of it in bfloat16, at most what 6 times is finite of.  Rounded to
+// float32 and then to bfloat16 it would be rounded twice where it is subnormal: the quotient there may come to lie in the middle of two
+// bfloat16 numbers.  A quotient that is not exact is therefore made the odd one of the two float32 numbers that it lies between (the rest of the
+// division, which is exact, says on which side of the rounded one it lies), and an odd one is never such a middle.  NaN where a number is not
+// finite: its bits are then at least those of infinity.
 constexpr float kMostScale = 0x1.54p125f;
 __device__ __forceinline__ uint16_t scale_of(uint32_t largest) {
   if (largest >= 0x7f800000u) return 0x7fc0;
-  return as_type<uint16_t>(fminf(__uint_as_float(largest) / 6.f, kMostScale));
+  const float x = __uint_as_float(largest), nearest = x / 6.f, rest = fmaf(-6.f, nearest, x);
+  const uint32_t below = __float_as_uint(nearest) - (rest < 0.f);
+  return as_type<uint16_t>(fminf(__uint_as_float(below | (rest != 0.f)), kMostScale));
 }
 
 // Codes of eight numbers, the nearest to each quotient by the scale, ties to the even code: v_cvt_scalef32_pk_fp4_f32 of the float32
