@@ -66,7 +66,6 @@ struct Codes {
   static constexpr int NG = KEYS / 16;              // groups of 16 keys
   static constexpr int kBytes = KEYS * RB;
   static constexpr int kStage = 2 * kBytes + 256;   // codes of keys, of values, scales
-  static constexpr int kOps = 2 * NI + 1;           // loads of a stage
   static constexpr int kRest = 8 * KEYS + 256;      // the scales in use as float32, pages of stages to come
   static constexpr int NQ = DP / 32, NM = DP / 16;  // steps of the scores, blocks of 16 columns
 };
@@ -157,7 +156,7 @@ struct Loader4 {
     int lane = this->lane;
     asm("" : "+v"(lane));               // what follows from it is formed here, not kept in registers
     if (!VALUES && n > 0 && n % kEach == 0) {
-      if constexpr (PAGES == 2) wait_vm<C::kOps>();          // asked for with the stage before; elsewhere many waits ago
+      // asked for ahead of the keys of a stage before, which have been waited for
       place(n, reinterpret_cast<const int32_t *>(ids)[lane], lane);
       wait_lds();
       ask(n + kEach, lane);
@@ -368,7 +367,9 @@ __device__ __forceinline__ void codes_piece(const Attend4Args &a, const Unit &u,
       if ((n / 4 ^ (int) (blockIdx.x / kCUs)) & 1) __builtin_amdgcn_s_setprio(1);
       else __builtin_amdgcn_s_setprio(0);
     }
-    wait_vm<C::NI>();                   // keys and scales are in, values may be on their way
+    // Loads come in in their order: pages for later stages (if any), a stage's keys, its scales, its values.  Keys, scales and the pages ahead of
+    // them are in, the values may be on their way.
+    wait_vm<C::NI>();
     const unsigned char *const kl = mine, *const vl = kl + C::kBytes;
     // All codes of keys into registers, so that those of another stage may come into their place.
     uint32_t kc[4][C::NQ];
