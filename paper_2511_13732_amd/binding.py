@@ -864,7 +864,9 @@ class Rotation(_Handle):
 
     @classmethod
     def of(cls, positions: int, dim: int, device, base: float = 10000.0, interleaved: bool = False) -> "Rotation":
-        """The table of the angles position * base^(-2 i / dim), formed in double."""
+        """The table of the angles position * base^(-2 i / dim), formed in double; dim even."""
+        if positions < 1 or dim < 2 or dim % 2:
+            raise ValueError(f"positions must be at least 1, dim even and at least 2, got {positions} and {dim}")
         at = torch.arange(dim // 2, dtype=torch.float64, device=device)
         angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * base ** (-2.0 * at / dim)
         return cls(torch.cat([angle.cos(), angle.sin()], dim=1).float(), interleaved)

@@ -185,6 +185,17 @@ def test_tensors_that_do_not_fit_are_refused():
             pcg.cache4_attend(four, **{**good, **bad})
 
 
+def test_tables_of_an_odd_number_of_elements_are_refused():
+    """An odd dim would give the angles of one more element, and pairs of one less."""
+    assert pcg.Rotation.of(3, 6, "cpu").dim == 6
+    for dim in (1, 7, 0, -2):
+        with pytest.raises(ValueError):
+            pcg.Rotation.of(3, dim, "cpu")
+    for positions in (0, -1):
+        with pytest.raises(ValueError):
+            pcg.Rotation.of(positions, 6, "cpu")
+
+
 def test_objects_whose_fields_are_replaced_name_the_new_ones():
     new = lambda n, dtype=torch.uint8: torch.zeros((4, 16, 2, n), dtype=dtype)  # noqa: E731
     cache = pcg.KvCache4(new(32), new(32), new(2, torch.bfloat16), 64)
