@@ -663,8 +663,9 @@ int pcg_cache4_read(const pcg_kv4_cache *cache, pcg_dtype dt, void *k_out, int64
 /*
  * pcg_cache_attend over a cache of 4 bits; queries and outputs are of type dt.  Keys and values are the scale * code that the cache stands for, not
  * rounded to dt; with PCG_BF16 a weight times its value's scale is rounded to bfloat16 where it multiplies codes, with PCG_F32 all 24 bits of it and
- * of the queries are multiplied.  A value that is NaN makes all elements of its head NaN in the rows that see it.  A key's scale
- * times `scale` log2 e has to stay within float32.  Everything else as there.
+ * of the queries are multiplied (of numbers below 2^-110 in absolute value the multiples of 2^-133 in them, the step of the smallest bfloat16).  A
+ * value that is NaN makes all elements of its head NaN in the rows that see it.  A key's scale times `scale` log2 e, and six times the sum of the
+ * absolute values of a query, have to stay within float32.  Everything else as there.
  *   workspace     DEVICE, >= pcg_cache4_attend_workspace_bytes(B, T, heads, kv_heads, head_dim, longest), which is
  *                 the same for any B, T, heads and longest
  */
