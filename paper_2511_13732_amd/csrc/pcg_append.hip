@@ -172,7 +172,7 @@ struct Counts {
 
 // A part of a head a thread: queries (if any), keys, values.  Bound by memory: everything is read and written once, 16 bytes at a time, with
 // nothing between but four products in double a pair.  16 prompts of up to 2048 tokens, 16 / 8 heads of 64, float32, take 34.9 us for 182 MB, 5.2
-// TB/s; 576 rows of a step 5.3 us, the waits for a slot, the row and the table's row.
+// TB/s; 24 of up to 3000, 32 / 8 heads of 128, bf16, 109 to 117 us for 605 MB, halves and neighbours alike; 576 rows of a step 5.3 us, the waits for a slot, the row and the table's row.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Counts n, Deal<T> deal) {
   constexpr int E = Deal<T>::E;
@@ -295,8 +295,9 @@ __device__ __forceinline__ uint16_t quantise(const float (&v)[8], uint32_t &code
 
 // Queries a part a thread in the first blocks; in the others N lanes a head of keys and values, eight elements of each a lane: a scale is the
 // maximum of a head, which the lanes form among themselves, and a lane's eight codes are a word.  Bound by memory: 24 prompts, 24000
-// tokens, 32 / 8 heads of 128, bf16 with queries, take 115 to 124 us for 532 MB, 4.3 to 4.6 TB/s; a step's 576 rows 5.7 us, which are the waits for a
-// slot, a row and a table's row one after the other.  Neighbours are the heads of a token, whose rows are read in a row; tokens of a head, which
+// tokens, 32 / 8 heads of 128, bf16 with queries, take 108 to 124 us for 531 MB, 4.3 to 4.9 TB/s, 12200 of float32 94 us for 519 MB; pairs that are
+// neighbours, whose table is read number by number, 138 and 117; heads of 72, whose halves are no whole pieces, 245 us for 299 MB; a step's 576 rows
+// 5.7 us, which are the waits for a slot, a row and a table's row one after the other.  Neighbours are the heads of a token, whose rows are read in a row; tokens of a head, which
 // would be written in a row where the cache has a head's slots together, measure the same (138.4 us for 136.3, with the way back).
 template <typename T, bool VEC, int N>
 __global__ __launch_bounds__(kThreads) void append4_kernel(AppendArgs a, Counts n, Deal<T> deal, uint32_t q_blocks) {

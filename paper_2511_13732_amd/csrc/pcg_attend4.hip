@@ -4,8 +4,8 @@
 // and one for its value.  Codes are exact in bfloat16, so that the products of pcg_attend.hip are made of them as they stand,
 //   S^T = C_k Q^T,  score = c s_k S        O^T = C_v^T (s_v P)^T
 // and the scales meet scores and weights, one multiplication each, and never the elements.  float32 queries and weights are three
-// bfloat16 numbers each, which hold all of their 24 bits: three products of the fast kind, exact in every term, where one of float32
-// takes sixteen times as long.
+// bfloat16 numbers each, which hold all of their 24 bits (from 2^-110 on; the smallest bfloat16 is 2^-133): three products of the fast kind, exact
+// in every term, where one of float32 takes sixteen times as long.
 //
 // The four waves of a workgroup have the same rows, one to three blocks of 16 that share decoded keys and values, and a stream of keys each, which
 // a wave brings into its own part of LDS ahead of their use: nothing is shared in the loop, and no wave waits for another one in it.  The
@@ -13,9 +13,12 @@
 //
 // What bounds it (bf16, 32 / 8 heads of 128; first kernel, then the joining of parts).  One block: memory, 128 requests of 3800 keys on average
 // 112 to 117 + 5 us for 509 MB, 4.5 TB/s.  Three blocks: issue.  A stage of 64 keys is 96 products, 48 exponentials, 128 conversions of codes and
-// about 300 other vector instructions, which add up on a SIMD: 1.55 us at 2.35 GHz, 2.2 at the 1.6 to 1.75 that the chip holds with all CUs busy.
-// 64 requests of 1260 keys with 9 tokens 43 to 44 + 6.7 us, 2 requests of 115000 69 + 9, pieces of prompts, 2844 tokens, 317 to 326 + 10 one at a
-// time and 290 in a row (734 TFLOP/s).  Few keys: waits one after the other, the run, the pages, the first keys, the joining: 1 request of 1500 keys 8.1 + 3.4.
+// about 300 other vector instructions, whose times one after the other are 1.55 us at 2.35 GHz, 2.2 at the 1.6 to 1.75 that the chip holds with all
+// CUs busy; a SIMD's two waves take 4 a stage, so that not much of it overlaps.  (Some does: float32 with two blocks, three times the products and
+// the cutting of their operands, takes 180 us where bfloat16 takes 108.  How much could was not measured.)  64 requests of 1260 keys with 9 tokens
+// 43 to 44 + 6.7 us, 2 requests of 115000 69 + 9 (in a row 71 to 77 from one card to another), pieces of prompts, 2844 tokens, 317 to 326 + 10 one
+// at a time and 289 to 298 in a row (715 to 735 TFLOP/s).  Windows of 1000 keys, bfloat16: 64 requests of 9 tokens 42, 128 of one token behind up
+// to 6000 keys 40.5 for 137 MB, pieces of prompts 109.  Few keys: waits one after the other, the run, the pages, the first keys, the joining: 1 request of 1500 keys 8.1 + 3.4.
 #include <algorithm>
 #include <type_traits>
 
